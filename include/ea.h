@@ -277,6 +277,110 @@ ea_status ea_compress_layer_fp8(const ea_params* p, const void* q_win, int64_t w
                                 int64_t n_keep, int32_t order_free, float* scores_out, int32_t* idx_out,
                                 int32_t* perm_out, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- A model's step over the cache: its blocks, its new rows, its attention -------------------
+ *
+ * What a serving loop does between two compress passes, over the caches that the passes above work on.
+ * A step adds tokens to the sequences of a batch, one each while they generate and stretches of a
+ * prompt while they are read.  The tokens of all sequences stand packed in one tensor: those of
+ * sequence b are cu_tokens[b] .. cu_tokens[b+1] - 1, and a tensor with room for more (n_tokens of
+ * them, as a captured graph needs) leaves its rows from cu_tokens[B] on unread and unwritten.
+ * Lengths live on the device, so a step needs no word from it: `n` and `max_new` below are bounds
+ * that the host knows.  After a compress pass a row's number is no longer its token's position;
+ * positions are therefore inputs of their own. */
+
+/* Block tables, slot maps and the list of free blocks, from the lengths of the sequences before and
+ * after (growth by a step's tokens, or the cut of a compress pass):
+ *   pg            block_table [B, max_blocks] is WRITTEN by this call only: of sequence b the entries
+ *                 ceil(len_old / block_size) .. ceil(len_new / block_size) - 1 where it grows; entries of
+ *                 blocks that it gives back stay as they were
+ *   len_old, len_new  [B] int32: rows held now and wanted (negative ones count as 0)
+ *   free_list     [num_blocks] int32, in and out: the first *free_in of it are free, taken from the end
+ *   free_in, free_out  [1] int32
+ *   len_out       [B] int32: len_new where the sequence was served, else len_old
+ *   cu_tokens     [B + 1] int32: prefix sums of max(0, len_new - len_old), served or not
+ *   slots, pos    [n_tokens] int64 / int32: of the i-th new token of sequence b the pool row
+ *                 block * block_size + offset that its row len_old + i has, and its position seen[b] + i;
+ *                 slots is -1 for the tokens of a sequence that was not served and from cu_tokens[B] on,
+ *                 where pos is left as it was.  Both may be NULL where n_tokens is 0.
+ *   seen          [B] int32: tokens the sequence has seen so far; NULL: len_old
+ * All are DEVICE pointers (int32: 4-byte aligned, slots 8).  Blocks given back come first and are
+ * taken again first, sequences in order; a sequence is served if the blocks wanted up to and with it
+ * are there and its table row has room for it (one that wants no block always is).  Growing by a step
+ * and going back restores list and count.  len_out, free_out, cu_tokens, slots and pos must not
+ * overlap the inputs: a loop keeps two of each and swaps them.  One launch, no scratch.
+ * EA_ERR_UNSUPPORTED beyond EA_BLOCK_TABLES_MAX_BATCH sequences, for block sizes that are not a power of
+ * two in [16, 65536], and for more than 2^31 - 1 blocks.  p: batch only is used. */
+#define EA_BLOCK_TABLES_MAX_BATCH 4096
+ea_status ea_block_tables(const ea_params* p, const ea_paged* pg, const int32_t* len_old, const int32_t* len_new,
+                          int32_t* free_list, const int32_t* free_in, int32_t* len_out, int32_t* free_out,
+                          int32_t* cu_tokens, int64_t n_tokens, int64_t* slots, int32_t* pos,
+                          const int32_t* seen, void* stream);
+
+/* A step's new rows as the projections leave them, in p->dtype: token t of q [Hq, d], k and v
+ * [Hkv, d] starts at q + t * q_stride, ... (strides in elements, multiples of 16 bytes; 0 = dense). */
+typedef struct {
+  const void* q;          /* DEVICE, or NULL: no queries to rotate                               */
+  const void* k;          /* DEVICE                                                              */
+  const void* v;          /* DEVICE                                                              */
+  int64_t q_stride, k_stride, v_stride;
+  int64_t n_tokens;
+  const int32_t* pos;     /* DEVICE [n_tokens]: positions; read where inv_freq is given           */
+  const double* inv_freq; /* DEVICE fp64 [d/2], or NULL: rows are stored as they are (q NULL then) */
+} ea_new_rows;
+
+/* The rotary embedding (Eq. 1, angles in fp64, rotation in fp32, rounded once) of a step's queries and
+ * keys, and the store of its keys and values into the cache, in one launch:
+ *   ea_append_paged  into the pools, row slots[t] of every KV head (slots of ea_block_tables).  A token
+ *                    whose slot is outside the pools (-1) is left out: nothing of it is read or written.
+ *   ea_append        into contiguous caches [B, Hkv, n_cap, d] whose heads may have different lengths
+ *                    (ea_compress_layer_adaptive): lengths [B, Hkv] int32 DEVICE count the new rows in, so
+ *                    the i-th of sequence b's m tokens becomes row lengths[b, h] - m + i.  Rows outside
+ *                    [0, n_cap) are left out.  cu_tokens [B + 1] DEVICE as written by ea_block_tables.
+ *   ea_append_fp8    the same into e4m3 bytes: k / k_scale[b, h] and v / v_scale[b, h] (NULL = 1), rounded
+ *                    to nearest even, saturating at +-448.  p->dtype EA_BF16, head_dim 128 or 256.
+ * q_out [n_tokens, Hq, d] receives the rotated queries (with new->q; it may be q itself if that is dense).
+ * k, v and q must not overlap the cache.  Two tokens with the same slot: either may be stored.
+ * p->rope_layout as everywhere; horizon, epsilon and the window's fields are not used. */
+ea_status ea_append_paged(const ea_params* p, const ea_new_rows* rows, const int64_t* slots, void* k_pool, void* v_pool,
+                          const ea_paged* pg, void* q_out, void* stream);
+ea_status ea_append(const ea_params* p, const ea_new_rows* rows, const int32_t* cu_tokens, const int32_t* lengths, void* k,
+                    void* v, int64_t n_cap, void* q_out, void* stream);
+ea_status ea_append_fp8(const ea_params* p, const ea_new_rows* rows, const int32_t* cu_tokens, const int32_t* lengths,
+                        void* k8, void* v8, const float* k_scale, const float* v_scale, int64_t n_cap, void* q_out,
+                        void* stream);
+
+/* Attention of a step's tokens over what is cached (Eq. 2-3), the new rows among it: with m tokens of
+ * sequence b in the step, token i (0 .. m-1) of query head g sees the rows j < len - (m - 1 - i) of its KV
+ * head h, len = lengths[b] (paged) or lengths[b, h]:
+ *   out = sum_j softmax_j(q . k_j / sqrt(d)) v_j,   lse = ln sum_j exp(q . k_j / sqrt(d)).
+ * A token that sees no row gets zeros and -inf.  Rows from len on are never looked at, whatever they hold.
+ *   q, out [n_tokens, Hq, d] in p->dtype (q_stride in the step, out dense), lse [n_tokens, Hq] fp32 or NULL
+ *   n      no length is larger (HOST; larger ones count as n); 0 <= n <= 2^26
+ * ea_attend: contiguous caches, bf16 or fp32; ea_attend_paged: bf16 pools; ea_attend_fp8: e4m3 bytes with
+ * per-head scales as in ea_score_fp8 (q and out bf16, head_dim 128 or 256).
+ * bf16: products of the bf16 values with fp32 sums; weights reach the second product as bf16 numbers,
+ * sums and maxima stay fp32.  fp32: everything in fp32.
+ * The result does not depend on n_tokens, but how a long head is cut, and so the last bits, may depend on
+ * n, max_new and n_tokens.  Same call, same bits.  `ws`: ea_attend_workspace_bytes(), 256-byte aligned, the
+ * rules of the other calls; that function returns 0 for invalid arguments and at least 256 otherwise.
+ * out must not overlap q or the cache. */
+typedef struct {
+  const int32_t* cu_tokens; /* DEVICE [B + 1], ascending from 0                                      */
+  int64_t n_tokens;         /* tokens that q, out and lse have room for                              */
+  int64_t max_new;          /* no sequence adds more (HOST); tokens beyond that many may be left out  */
+  int64_t q_stride;         /* elements from token to token of q, a multiple of 16 bytes; 0 = Hq * d   */
+} ea_step;
+size_t ea_attend_workspace_bytes(const ea_params* p, const ea_step* step, int64_t n);
+ea_status ea_attend(const ea_params* p, const void* q, const ea_step* step, const void* k, const void* v,
+                    const int32_t* lengths, int64_t n, int64_t n_cap, void* out, float* lse, void* ws, size_t ws_bytes,
+                    void* stream);
+ea_status ea_attend_paged(const ea_params* p, const void* q, const ea_step* step, const void* k_pool, const void* v_pool,
+                          const ea_paged* pg, const int32_t* lengths, int64_t n, void* out, float* lse, void* ws,
+                          size_t ws_bytes, void* stream);
+ea_status ea_attend_fp8(const ea_params* p, const void* q, const ea_step* step, const void* k8, const void* v8,
+                        const float* k_scale, const float* v_scale, const int32_t* lengths, int64_t n, int64_t n_cap,
+                        void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* Listing 1: int(n * (1 - ratio)) in IEEE double, truncated toward zero; -1 if ratio is
  * outside [0, 1] or n < 0.  Host only. */
 int64_t ea_n_keep(int64_t n, double ratio);

@@ -29,6 +29,17 @@ class EaPaged(ctypes.Structure):
                 ("max_blocks", ctypes.c_int32), ("num_blocks", ctypes.c_int64)]
 
 
+class EaNewRows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("n_tokens", ctypes.c_int64),
+                ("pos", ctypes.c_void_p), ("inv_freq", ctypes.c_void_p)]
+
+
+class EaStep(ctypes.Structure):
+    _fields_ = [("cu_tokens", ctypes.c_void_p), ("n_tokens", ctypes.c_int64), ("max_new", ctypes.c_int64),
+                ("q_stride", ctypes.c_int64)]
+
+
 def lib_path():
     """In-tree libea.so; the environment variable EA_LIBRARY names another build of it."""
     return os.environ.get("EA_LIBRARY") or os.path.join(_HERE, "libea.so")
@@ -94,6 +105,23 @@ def load_library():
     lib.ea_compress_layer_fp8.restype = ctypes.c_int
     lib.ea_compress_layer_fp8.argtypes = [P, VP, I64, I64, VP, I64, VP, VP, VP, VP, I64, I64, I64, ctypes.c_int32,
                                           VP, VP, VP, VP, SZ, VP]
+    NR, ST = ctypes.POINTER(EaNewRows), ctypes.POINTER(EaStep)
+    lib.ea_block_tables.restype = ctypes.c_int
+    lib.ea_block_tables.argtypes = [P, PG, VP, VP, VP, VP, VP, VP, VP, I64, VP, VP, VP, VP]
+    lib.ea_append_paged.restype = ctypes.c_int
+    lib.ea_append_paged.argtypes = [P, NR, VP, VP, VP, PG, VP, VP]
+    lib.ea_append.restype = ctypes.c_int
+    lib.ea_append.argtypes = [P, NR, VP, VP, VP, VP, I64, VP, VP]
+    lib.ea_append_fp8.restype = ctypes.c_int
+    lib.ea_append_fp8.argtypes = [P, NR, VP, VP, VP, VP, VP, VP, I64, VP, VP]
+    lib.ea_attend_workspace_bytes.restype = SZ
+    lib.ea_attend_workspace_bytes.argtypes = [P, ST, I64]
+    lib.ea_attend.restype = ctypes.c_int
+    lib.ea_attend.argtypes = [P, VP, ST, VP, VP, VP, I64, I64, VP, VP, VP, SZ, VP]
+    lib.ea_attend_paged.restype = ctypes.c_int
+    lib.ea_attend_paged.argtypes = [P, VP, ST, VP, VP, PG, VP, I64, VP, VP, VP, SZ, VP]
+    lib.ea_attend_fp8.restype = ctypes.c_int
+    lib.ea_attend_fp8.argtypes = [P, VP, ST, VP, VP, VP, VP, VP, I64, I64, VP, VP, VP, SZ, VP]
     lib.ea_compress_layer_timed.restype = ctypes.c_int
     lib.ea_compress_layer_timed.argtypes = [P, VP, I64, I64, VP, I64, VP, VP, I64, I64, I64, VP, SZ, VP,
                                             ctypes.POINTER(ctypes.c_float)]
@@ -297,6 +325,74 @@ def compress_layer_fp8(p, q_win, window, q_pos0, inv_freq, t_next, k8, v8, k_sca
                                                 _ptr(v_scale), int(n), int(n_cap), int(n_keep_), int(order_free),
                                                 _ptr(scores_out), _ptr(idx_out), _ptr(perm_out), _ptr(ws),
                                                 _nbytes(ws), _stream(stream)), "ea_compress_layer_fp8")
+
+
+def block_tables(p, pg, len_old, len_new, free_list, free_in, len_out, free_out, cu_tokens, n_tokens=0, slots=None, pos=None,
+                 seen=None, stream=None):
+    """Writes the block table that pg points at, too."""
+    _check(load_library().ea_block_tables(ctypes.byref(p), ctypes.byref(pg), _ptr(len_old), _ptr(len_new), _ptr(free_list),
+                                          _ptr(free_in), _ptr(len_out), _ptr(free_out), _ptr(cu_tokens), int(n_tokens),
+                                          _ptr(slots), _ptr(pos), _ptr(seen), _stream(stream)), "ea_block_tables")
+
+
+def _token_stride(t):
+    """Elements from one token to the next of t [n_tokens, heads, d]; a token's heads have to stand together."""
+    if t.stride(-1) != 1 or t.stride(-2) != t.shape[-1]:
+        raise ValueError("the heads of a token must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def make_new_rows(q, k, v, pos=None, inv_freq=None):
+    """ea_new_rows for tensors q (or None) [n_tokens, Hq, d], k, v [n_tokens, Hkv, d]; views into one projection's rows will do."""
+    def ptr(t):
+        return None if t is None else t.data_ptr()
+    r = EaNewRows(ptr(q), ptr(k), ptr(v), 0 if q is None else _token_stride(q), _token_stride(k), _token_stride(v), k.shape[0],
+                  ptr(pos), ptr(inv_freq))
+    r.tensors = (q, k, v, pos, inv_freq)      # alive as long as the addresses are kept
+    return r
+
+
+def append_paged(p, rows, slots, k_pool, v_pool, pg, q_out=None, stream=None):
+    _check(load_library().ea_append_paged(ctypes.byref(p), ctypes.byref(rows), _ptr(slots), _ptr(k_pool), _ptr(v_pool),
+                                          ctypes.byref(pg), _ptr(q_out), _stream(stream)), "ea_append_paged")
+
+
+def append(p, rows, cu_tokens, lengths, k, v, n_cap, q_out=None, stream=None):
+    _check(load_library().ea_append(ctypes.byref(p), ctypes.byref(rows), _ptr(cu_tokens), _ptr(lengths), _ptr(k), _ptr(v),
+                                    int(n_cap), _ptr(q_out), _stream(stream)), "ea_append")
+
+
+def append_fp8(p, rows, cu_tokens, lengths, k8, v8, k_scale, v_scale, n_cap, q_out=None, stream=None):
+    _check(load_library().ea_append_fp8(ctypes.byref(p), ctypes.byref(rows), _ptr(cu_tokens), _ptr(lengths), _ptr(k8), _ptr(v8),
+                                        _ptr(k_scale), _ptr(v_scale), int(n_cap), _ptr(q_out), _stream(stream)), "ea_append_fp8")
+
+
+def make_step(cu_tokens, n_tokens, max_new, q_stride=0):
+    """ea_step for a tensor of prefix sums [B + 1] int32 on the device."""
+    s = EaStep(cu_tokens.data_ptr(), int(n_tokens), int(max_new), int(q_stride))
+    s.tensors = (cu_tokens,)
+    return s
+
+
+def attend_workspace_bytes(p, step, n):
+    return int(load_library().ea_attend_workspace_bytes(ctypes.byref(p), ctypes.byref(step), int(n)))
+
+
+def attend(p, q, step, k, v, lengths, n, n_cap, out, lse, ws, stream=None):
+    _check(load_library().ea_attend(ctypes.byref(p), _ptr(q), ctypes.byref(step), _ptr(k), _ptr(v), _ptr(lengths), int(n),
+                                    int(n_cap), _ptr(out), _ptr(lse), _ptr(ws), _nbytes(ws), _stream(stream)), "ea_attend")
+
+
+def attend_paged(p, q, step, k_pool, v_pool, pg, lengths, n, out, lse, ws, stream=None):
+    _check(load_library().ea_attend_paged(ctypes.byref(p), _ptr(q), ctypes.byref(step), _ptr(k_pool), _ptr(v_pool),
+                                          ctypes.byref(pg), _ptr(lengths), int(n), _ptr(out), _ptr(lse), _ptr(ws), _nbytes(ws),
+                                          _stream(stream)), "ea_attend_paged")
+
+
+def attend_fp8(p, q, step, k8, v8, k_scale, v_scale, lengths, n, n_cap, out, lse, ws, stream=None):
+    _check(load_library().ea_attend_fp8(ctypes.byref(p), _ptr(q), ctypes.byref(step), _ptr(k8), _ptr(v8), _ptr(k_scale),
+                                        _ptr(v_scale), _ptr(lengths), int(n), int(n_cap), _ptr(out), _ptr(lse), _ptr(ws),
+                                        _nbytes(ws), _stream(stream)), "ea_attend_fp8")
 
 
 N_STAGES = 6

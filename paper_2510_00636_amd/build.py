@@ -13,7 +13,8 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libea.so")
 SOURCES = ["ea_host.cpp", "ea_api.hip", "ea_stats.hip", "ea_score.hip", "ea_score_d64.hip", "ea_score_d128.hip", "ea_score_d128b.hip",
            "ea_score_d256.hip", "ea_score_fp8.hip", "ea_score_fp8b.hip", "ea_score_hw.hip", "ea_select.hip",
-           "ea_compact.hip", "ea_baselines.hip", "ea_frontend.hip"]
+           "ea_compact.hip", "ea_baselines.hip", "ea_frontend.hip", "ea_serve.hip", "ea_step.hip", "ea_attend_rows.hip",
+           "ea_attend_tile.hip", "ea_attend_f32.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 instructions are switched off for the device pass (the host pass warns that it
 # does not know the feature; harmless)
@@ -26,11 +27,14 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-mllvm", "-amdgpu-atomic-optimizer-strategy=None",
          "-mllvm", "-amdgpu-mfma-vgpr-form"]
+# The attention kernels' weights are powers of two of numbers up to 8: denormal ones are zeros there, which makes exp2f the
+# one instruction that it is (else six, with the scaling that denormal results need).
+MORE = {f: ["-fgpu-flush-denormals-to-zero"] for f in ("ea_attend_rows.hip", "ea_attend_tile.hip", "ea_attend_f32.hip")}
 
 
 def _compile(src):
     obj = os.path.join(OBJ, src + ".o")
-    cmd = [HIPCC, *FLAGS, "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj]
+    cmd = [HIPCC, *FLAGS, *MORE.get(src, []), "-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("hipcc failed on %s:\n%s\n%s" % (src, r.stdout, r.stderr))

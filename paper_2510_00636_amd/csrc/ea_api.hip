@@ -327,22 +327,6 @@ ea_status ea_compact(const ea_params* p, const void* k, const void* v, int64_t n
 
 // ea_paged -> PageMap, validated on the host (the table's entries are device memory: the kernels
 // clamp them into the pool)
-static ea_status check_paged(const Dims& d, const ea_paged* pg, int64_t n, PageMap* pm) {
-  if (!pg || !pg->block_table || ((uintptr_t)pg->block_table & 3u)) return EA_ERR_INVALID_ARG;
-  const int64_t bs = pg->block_size;
-  if (bs < 16 || bs > 65536 || (bs & (bs - 1)) != 0) return EA_ERR_UNSUPPORTED;
-  if (pg->max_blocks < 1 || pg->num_blocks < 1 || pg->num_blocks > ((int64_t)1 << 31)) return EA_ERR_INVALID_ARG;
-  if ((int64_t)pg->max_blocks * bs < n) return EA_ERR_INVALID_ARG;
-  if (d.dtype != EA_BF16) return EA_ERR_UNSUPPORTED;
-  pm->table = pg->block_table;
-  pm->sh = 0;
-  while (((int64_t)1 << pm->sh) < bs) ++pm->sh;
-  pm->max_blocks = pg->max_blocks;
-  pm->hkv = d.Hkv;
-  pm->num_blocks = pg->num_blocks;
-  return EA_OK;
-}
-
 // unordered: the order-free compaction (perm_out then receives the source row of every position)
 // pm: the caches are block pools (n_cap is then not used)
 static ea_status compress_impl(const ea_params* p, const void* q_win, int64_t window,

@@ -1,0 +1,305 @@
+// Attention of long stretches of new tokens (prompts read in pieces): the matrix cores bound it.
+//
+// A workgroup takes 128 (token, head) rows of a KV head, 32 for each wavefront, and walks the keys in tiles that all four share
+// through LDS, the next tile requested while one is worked on.  S^T = K Q^T and O^T = V^T P^T by v_mfma_f32_32x32x16_bf16: a
+// lane then holds half of the keys of its row, and what it holds is, as it stands, the operand of the second product if V^T has
+// its keys in the same order.  V^T comes out of the row-major tile by ds_read_b64_tr_b16.
+#include "ea_attend.h"
+
+namespace ea {
+
+namespace {
+
+constexpr int kM = kAttendTileRows;
+using s16x4 = short __attribute__((ext_vector_type(4)));
+
+// LDS rows: K's start four banks apart (16-byte reads of eight rows at a time), V's sixteen (transposing reads of four rows,
+// 64 bytes of each)
+template <int D> constexpr int k_pitch() { return D * 2 + 16; }
+template <int D> constexpr int v_pitch() { return D * 2 + 64; }
+template <int D> constexpr int tile_keys() { return D == 256 ? 32 : 64; }
+template <int D> constexpr int buffer_bytes() { return tile_keys<D>() * (k_pitch<D>() + v_pitch<D>()); }
+
+}  // namespace
+
+template <int D, bool FP8>
+__global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_tile(AttendArgs a) {
+  constexpr int kN = tile_keys<D>(), kKt = kN / 32, kSteps = D / 16, kCt = D / 32;
+  constexpr int kRowBytes = D * (FP8 ? 1 : 2);
+  constexpr int kPer = 1024 / kRowBytes;                 // rows that a wavefront's load covers
+  constexpr int kPasses = kN / (4 * kPer);               // of the workgroup's loads over a tile
+  constexpr int kChunks = kRowBytes / 16;
+  extern __shared__ char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n32 = lane & 31, hi = lane >> 5;
+
+  // ---- which tile: heads next to each other (they run on different dies), the last tiles, which see most keys, first
+  const int h = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
+  const int split = rest % a.plan.nsplit, item = a.plan.tiles - 1 - rest / a.plan.nsplit;
+  // sequence b's tiles start at floor(cu[b] G / 128) + b: as many as it can have up to there
+  int b = -1;
+  for (int base = 0; base < a.B; base += 64) {
+    const int i = base + lane;
+    const uint64_t le = __ballot(i < a.B && first_token(a, i < a.B ? i : 0) * a.G / kM + i <= item);
+    b += __builtin_popcountll(le);
+    if (~le) break;
+  }
+  if (b < 0) return;
+  const int t0 = __builtin_amdgcn_readfirstlane(first_token(a, b));
+  const int m = __builtin_amdgcn_readfirstlane(first_token(a, b + 1)) - t0;
+  const int rows = m * a.G, row0 = (item - (t0 * a.G / kM + b)) * kM;
+  if (row0 >= rows || (a.only_long && rows <= a.short_rows)) return;
+  const int len = __builtin_amdgcn_readfirstlane(rows_of(a, b, h));
+  const int last_row = min(row0 + kM, rows) - 1;
+  int key_hi = len - (m - 1 - last_row / a.G);           // keys that the tile's last token sees
+  key_hi = key_hi < 0 ? 0 : key_hi;
+  const int key_lo = split * a.plan.chunk;
+  if (a.plan.nsplit > 1) {
+    if (key_lo >= key_hi && split > 0) return;
+    key_hi = min(key_hi, key_lo + a.plan.chunk);
+  }
+  const int unit = b * a.Hkv + h;
+
+  const int row = row0 + wave * 32 + n32, tok = row / a.G, hd = row - tok * a.G;
+  const bool in = row < rows;
+  const int vis = in ? len - (m - 1 - tok) : len;
+  const int vis_min = len - (m - 1 - (row0 + wave * 32) / a.G);      // of the wavefront's rows
+  bf16x8 q[kSteps];
+  {
+    const __bf16* src = (const __bf16*)a.q + (long long)(t0 + (in ? tok : 0)) * a.q_stride + (h * a.G + (in ? hd : 0)) * D;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      bf16x8 w = *(const bf16x8*)(src + s * 16 + hi * 8);
+      if (!in) w = (bf16x8)(__bf16)0.0f;
+      q[s] = w;
+    }
+  }
+  const float qk = a.scale * (FP8 && a.kscale ? a.kscale[unit] : 1.0f);
+
+  // ---- loads of a tile: pass i of wavefront w covers rows (4 i + w) kPer ..
+  int entries = 0, window = key_lo;
+  auto load_window = [&](int from) {
+    const int r = from + lane * 16;
+    entries = table_entry(a, b, r < len ? r : len > 0 ? len - 1 : 0);
+    window = from;
+  };
+  u32x4 kraw[kPasses], vraw[kPasses];
+  auto request = [&](int at) {
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      const int r0 = at + (4 * i + wave) * kPer, sub = r0 & ~15;
+      const int from = sub < len ? sub : (len - 1) & ~15;
+      const int e = __builtin_amdgcn_readlane(entries, (from - window) >> 4);
+      int r = r0 - sub + lane / kChunks;
+      r = min(r, len - 1 - from);
+      const long long at_byte = row_base(a, b, h, from, e) * kRowBytes;
+      const int off = r * kRowBytes + lane % kChunks * 16;
+      kraw[i] = *(const u32x4*)((const char*)a.k + at_byte + off);
+      vraw[i] = *(const u32x4*)((const char*)a.v + at_byte + off);
+    }
+  };
+  auto stage = [&](int at, char* buf) {
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      const int r = (4 * i + wave) * kPer + lane / kChunks, c = lane % kChunks;
+      const uint32_t keep = at + r >= key_hi ? 0u : ~0u;       // rows behind the last one weigh nothing, whatever they hold
+      const u32x4 v = vraw[i] & keep;
+      char* kd = buf + r * k_pitch<D>() + c * (FP8 ? 32 : 16);
+      char* vd = buf + kN * k_pitch<D>() + r * v_pitch<D>() + c * (FP8 ? 32 : 16);
+      if constexpr (FP8) {
+        *(uint4*)kd = widen_fp8(make_uint2(kraw[i].x, kraw[i].y));
+        *(uint4*)(kd + 16) = widen_fp8(make_uint2(kraw[i].z, kraw[i].w));
+        *(uint4*)vd = widen_fp8(make_uint2(v.x, v.y));
+        *(uint4*)(vd + 16) = widen_fp8(make_uint2(v.z, v.w));
+      } else {
+        *(u32x4*)kd = kraw[i];
+        *(u32x4*)vd = v;
+      }
+    }
+  };
+
+  f32x16 o[kCt];
+#pragma unroll
+  for (int c = 0; c < kCt; ++c) o[c] = (f32x16)0.0f;
+  float mx = -__builtin_inff(), l = 0.0f;
+  if (key_lo < key_hi) {
+    load_window(key_lo);
+    request(key_lo);
+    stage(key_lo, lds);
+    if (key_lo + kN < key_hi) request(key_lo + kN);
+    __syncthreads();
+  }
+  int buf = 0;
+  for (int key = key_lo; key < key_hi; key += kN, buf ^= 1) {
+    const char* kt = lds + buf * buffer_bytes<D>();
+    const char* vt = kt + kN * k_pitch<D>();
+    f32x16 s[kKt];
+#pragma unroll
+    for (int t = 0; t < kKt; ++t) {
+      s[t] = (f32x16)0.0f;
+#pragma unroll
+      for (int c = 0; c < kSteps; ++c) {
+        const bf16x8 w = *(const bf16x8*)(kt + (t * 32 + n32) * k_pitch<D>() + c * 32 + hi * 16);
+        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[c], s[t], 0, 0, 0);
+      }
+    }
+    // key of s[t][r]: t 32 + (r / 4) 8 + hi 4 + r % 4
+    if constexpr (FP8)
+#pragma unroll
+      for (int t = 0; t < kKt; ++t) s[t] *= qk;
+    if (key + kN > vis_min)
+#pragma unroll
+      for (int t = 0; t < kKt; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (key + t * 32 + (r >> 2) * 8 + hi * 4 + (r & 3) >= vis) s[t][r] = -__builtin_inff();
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < kKt; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+    if constexpr (!FP8) top *= qk;
+    // the maximum that weights are taken against moves only when a row's passes it by more than 2^8
+    if (__any(top > mx + 8.0f)) {
+      top = fmaxf(max_xor32(top), mx);
+      const float f = mx == -__builtin_inff() ? 0.0f : pow2(mx - top);
+      mx = top;
+      l *= f;
+#pragma unroll
+      for (int c = 0; c < kCt; ++c) o[c] *= f;
+    }
+    const float from = mx == -__builtin_inff() ? 0.0f : mx;
+    uint32_t p[kKt][8];
+#pragma unroll
+    for (int t = 0; t < kKt; ++t)
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const float x = FP8 ? pow2(s[t][2 * r] - from) : pow2(fmaf(s[t][2 * r], qk, -from));
+        const float y = FP8 ? pow2(s[t][2 * r + 1] - from) : pow2(fmaf(s[t][2 * r + 1], qk, -from));
+        l += x + y;
+        p[t][r] = pack_bf16(x, y);
+      }
+#pragma unroll
+    for (int kb = 0; kb < kKt * 2; ++kb) {
+      const uint32_t* pw = &p[kb >> 1][(kb & 1) * 4];
+      const bf16x8 pv = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+#pragma unroll
+      for (int c = 0; c < kCt; ++c) {
+        // lanes 16 j .. of a group of 16 read four rows of 16 channels, and get one channel of the four rows each
+        const int i = lane & 15, half = (lane >> 4) & 1;
+        const char* at = vt + (kb * 16 + 4 * hi + (i >> 2)) * v_pitch<D>() + (c * 32 + half * 16 + (i & 3) * 4) * 2;
+        using lds_s16x4 = __attribute__((address_space(3))) s16x4;
+        const s16x4 w0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at));
+        const s16x4 w1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * v_pitch<D>()));
+        const uint2 u0 = __builtin_bit_cast(uint2, w0), u1 = __builtin_bit_cast(uint2, w1);
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(u0.x, u0.y, u1.x, u1.y)), pv, o[c], 0, 0, 0);
+      }
+    }
+    const int next = key + kN;
+    if (next < key_hi) {
+      stage(next, lds + (buf ^ 1) * buffer_bytes<D>());
+      if (next + kN < key_hi) {
+        if (next + kN - window >= 1024) load_window(next + kN);
+        request(next + kN);
+      }
+      __syncthreads();
+    }
+  }
+
+  l = sum_halves(l);
+  if (!in) return;
+  const long long at = (long long)(t0 + tok) * a.Hq + h * a.G + hd;
+  // channel c 32 + (r / 4) 8 + hi 4 + r % 4 is o[c][r]
+  if (a.plan.nsplit == 1) {
+    const bool any = l > 0.0f || l != l;
+    const float f = (FP8 && a.vscale ? a.vscale[unit] : 1.0f) / l;
+    __bf16* dst = (__bf16*)a.out + at * D;
+#pragma unroll
+    for (int c = 0; c < kCt; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *(uint2*)(dst + c * 32 + r * 2 + hi * 4) = any ? make_uint2(pack_bf16(o[c][r] * f, o[c][r + 1] * f), pack_bf16(o[c][r + 2] * f, o[c][r + 3] * f))
+                                                       : make_uint2(0u, 0u);
+    if (a.lse && hi == 0) a.lse[at] = natural_lse(mx, l);
+  } else {
+    const long long slot = (long long)split * a.n_tokens * a.Hq + at;
+    float* po = (float*)(a.ws + a.plan.split_o) + slot * D;
+#pragma unroll
+    for (int c = 0; c < kCt; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *(float4*)(po + c * 32 + r * 2 + hi * 4) = make_float4(o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]);
+    if (hi == 0) ((float2*)(a.ws + a.plan.split_ml))[slot] = make_float2(mx, l);
+  }
+}
+
+// The splits of every (token, head) row together: D / 4 threads each.
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
+  constexpr int kLanes = D / 4;
+  const long long at = (long long)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
+  const int c = threadIdx.x % kLanes;
+  const int token = (int)(at / a.Hq), head = (int)(at - (long long)token * a.Hq), h = head / a.G;
+  // the token's sequence: tokens behind the last one are nobody's
+  int lo = 0, hi = a.B;
+  if (token >= first_token(a, a.B) || token < first_token(a, 0)) return;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first_token(a, mid) <= token) lo = mid; else hi = mid;
+  }
+  const int t0 = first_token(a, lo), m = first_token(a, lo + 1) - t0;
+  if (token >= t0 + m || (a.only_long && m * a.G <= a.short_rows)) return;
+  const int vis = rows_of(a, lo, h) - (m - 1 - (token - t0));
+  int n = (vis + a.plan.chunk - 1) / a.plan.chunk;
+  n = n < 1 ? 0 : n > a.plan.nsplit ? a.plan.nsplit : n;
+  const float* po = (const float*)(a.ws + a.plan.split_o);
+  const float2* ml = (const float2*)(a.ws + a.plan.split_ml);
+  const long long step = (long long)a.n_tokens * a.Hq;
+  float top = -__builtin_inff(), sum = 0.0f;
+  for (int i = 0; i < n; ++i) top = fmaxf(top, ml[i * step + at].x);
+  const float from = top == -__builtin_inff() ? 0.0f : top;
+  float4 acc = make_float4(0, 0, 0, 0);
+  for (int i = 0; i < n; ++i) {
+    const float2 w = ml[i * step + at];
+    const float4 x = *(const float4*)(po + (i * step + at) * D + c * 4);
+    const float f = pow2(w.x - from);
+    sum += w.y * f;
+    acc.x += x.x * f; acc.y += x.y * f; acc.z += x.z * f; acc.w += x.w * f;
+  }
+  const bool any = sum > 0.0f || sum != sum;
+  const float f = any ? (a.vscale ? a.vscale[lo * a.Hkv + h] : 1.0f) / sum : 0.0f;
+  if (F32)
+    *(float4*)((float*)a.out + at * D + c * 4) = any ? make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f) : make_float4(0, 0, 0, 0);
+  else
+    *(uint2*)((__bf16*)a.out + at * D + c * 4) =
+        any ? make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f)) : make_uint2(0u, 0u);
+  if (a.lse && c == 0) a.lse[at] = natural_lse(top, sum);
+}
+
+hipError_t launch_attend_join(const AttendArgs& a, bool f32, hipStream_t st) {
+  const long long rows = (long long)a.n_tokens * a.Hq, per = 256 / (a.D / 4);
+  const unsigned grid = (unsigned)((rows + per - 1) / per);
+#define EA_CASE(DD) \
+  if (a.D == DD) { if (f32) k_attend_join<DD, true><<<grid, 256, 0, st>>>(a); else k_attend_join<DD, false><<<grid, 256, 0, st>>>(a); }
+  EA_CASE(64) EA_CASE(128) EA_CASE(256)
+#undef EA_CASE
+  return hipGetLastError();
+}
+
+template <int D, bool FP8>
+static hipError_t tile_of_type(const AttendArgs& a, hipStream_t st) {
+  static LdsOptIn opt;
+  hipError_t e = opt.ensure((const void*)k_attend_tile<D, FP8>, 2 * buffer_bytes<D>());
+  if (e != hipSuccess) return e;
+  k_attend_tile<D, FP8><<<(unsigned)(a.plan.tiles * a.plan.nsplit * a.Hkv), 256, 2 * buffer_bytes<D>(), st>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess || a.plan.nsplit == 1) return e;
+  return launch_attend_join(a, false, st);
+}
+
+hipError_t launch_attend_tile(const AttendArgs& a, const Dims& d, hipStream_t st) {
+  if (d.kv_fp8) return d.D == 128 ? tile_of_type<128, true>(a, st) : tile_of_type<256, true>(a, st);
+  return d.D == 64 ? tile_of_type<64, false>(a, st) : d.D == 128 ? tile_of_type<128, false>(a, st) : tile_of_type<256, false>(a, st);
+}
+
+}  // namespace ea

@@ -54,6 +54,23 @@ struct PageMap {
   long long num_blocks;
 };
 
+// Attention of a step's tokens: how a call is cut, and where its workspace holds what.
+constexpr int kAttendGroup = 128;       // keys of a group of the row kernel, whose workgroups take whole ones
+constexpr int kAttendTileRows = 128;    // (token, head) rows of a workgroup of the tile kernel
+constexpr int kAttendF32Rows = 16;      // and of the fp32 kernel
+constexpr int kAttendShares = 512;      // most workgroups of the row kernel
+constexpr int64_t kAttendMaxTokens = (int64_t)1 << 24;
+struct AttendPlan {
+  int rows, tile;     // the row kernel serves sequences of few (token, head) rows per KV head, the tile (or fp32) kernel the others
+  int mt;             // 16-row operands of the row kernel
+  int short_rows;     // most (token, head) rows of a sequence that is the row kernel's
+  int shares;         // its workgroups
+  int piece_rows;     // rows reserved for a partial result
+  int tiles;          // of the tile kernel, per KV head
+  int nsplit, chunk;  // stretches of keys that workgroups of their own take there, and keys of each
+  size_t info, part_o, part_ml, split_o, split_ml, total;
+};
+
 struct WsLayout {
   size_t tab, qproj, mu, sigma, frags, post, logits, vnorm, part, lse, scores, idx, base, hist, pool_hist, blk, flags, total;
 };
@@ -175,6 +192,11 @@ inline int64_t f32_span(int64_t heads, int64_t n, int64_t slots) {
   }
   return best * 64;
 }
+
+// what a call of at most n rows per head launches; n_tokens and max_new as in ea_step
+AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t max_new, int num_cu);
+ea_status check_step(const Dims& d, const ea_step* step, int64_t n);
+ea_status check_paged(const Dims& d, const ea_paged* pg, int64_t n, PageMap* pm);
 
 // fragments per head of the triangular Sigma tiling, and per pass
 inline int frags_per_head(int D) { int njt = D / 32; return njt * (njt + 1); }

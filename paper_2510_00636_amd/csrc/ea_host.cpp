@@ -304,6 +304,79 @@ WsLayout make_ws_layout(const Dims& d, int64_t n, int64_t window) {
   return w;
 }
 
+ea_status check_paged(const Dims& d, const ea_paged* pg, int64_t n, PageMap* pm) {
+  if (!pg || !pg->block_table || ((uintptr_t)pg->block_table & 3u)) return EA_ERR_INVALID_ARG;
+  const int64_t bs = pg->block_size;
+  if (bs < 16 || bs > 65536 || (bs & (bs - 1)) != 0) return EA_ERR_UNSUPPORTED;
+  if (pg->max_blocks < 1 || pg->num_blocks < 1 || pg->num_blocks > ((int64_t)1 << 31)) return EA_ERR_INVALID_ARG;
+  if ((int64_t)pg->max_blocks * bs < n) return EA_ERR_INVALID_ARG;
+  if (d.dtype != EA_BF16) return EA_ERR_UNSUPPORTED;
+  pm->table = pg->block_table;
+  pm->sh = 0;
+  while (((int64_t)1 << pm->sh) < bs) ++pm->sh;
+  pm->max_blocks = pg->max_blocks;
+  pm->hkv = d.Hkv;
+  pm->num_blocks = pg->num_blocks;
+  return EA_OK;
+}
+
+ea_status check_step(const Dims& d, const ea_step* step, int64_t n) {
+  if (!step || !step->cu_tokens || ((uintptr_t)step->cu_tokens & 3u)) return EA_ERR_INVALID_ARG;
+  if (step->n_tokens < 0 || step->max_new < 1 || n < 0 || n > kMaxN) return EA_ERR_INVALID_ARG;
+  if (step->n_tokens > kAttendMaxTokens) return EA_ERR_UNSUPPORTED;
+  const int64_t dense = (int64_t)d.Hq * d.D, per16 = d.dtype == EA_BF16 ? 8 : 4;
+  if (step->q_stride != 0 && (step->q_stride < dense || step->q_stride % per16 != 0)) return EA_ERR_INVALID_ARG;
+  if (step->q_stride > ((int64_t)1 << 40)) return EA_ERR_INVALID_ARG;
+  return EA_OK;
+}
+
+AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t max_new, int num_cu) {
+  AttendPlan a = {};
+  const bool f32 = d.dtype != EA_BF16;
+  if (max_new > n_tokens) max_new = n_tokens;
+  const int64_t most = max_new * d.G;         // (token, head) rows of a sequence and KV head
+  a.mt = most > 16 && most <= 32 && d.D <= 128 ? 2 : 1;
+  a.piece_rows = 16 * a.mt;
+  a.short_rows = (int)(most < a.piece_rows ? most : a.piece_rows);
+  // one sequence is one kernel's; of several that may be long some may be short
+  a.rows = !f32 && a.short_rows >= d.G && (most <= a.piece_rows || d.B > 1);
+  a.tile = f32 || most > a.piece_rows;
+  a.shares = 2 * num_cu < kAttendShares ? 2 * num_cu : kAttendShares;
+  a.nsplit = 1;
+  const int64_t unit_rows = f32 ? kAttendF32Rows : kAttendTileRows;
+  // sequence b's tiles start at floor(first token G / unit_rows) + b
+  a.tiles = (int)(n_tokens * d.G / unit_rows + d.B);
+  // enough workgroups for two per CU: keys in stretches where the tiles are few
+  const int64_t step = 64, busy = (n_tokens * d.G + unit_rows - 1) / unit_rows * d.Hkv, slots = 2 * (int64_t)num_cu;
+  int64_t cut = busy > 0 ? slots / busy : 1;
+  const int64_t most_cuts = (n + 511) / 512;
+  if (cut > most_cuts) cut = most_cuts;
+  if (cut < 1) cut = 1;
+  int64_t chunk = ((n + cut - 1) / cut + step - 1) / step * step;
+  if (chunk < step) chunk = step;
+  a.chunk = (int)chunk;
+  a.nsplit = (int)((n + chunk - 1) / chunk);
+  if (a.nsplit < 1) a.nsplit = 1;
+  size_t o = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = o;
+    o = align_up(o + bytes, 256);
+    return at;
+  };
+  if (a.rows) {
+    a.info = take((size_t)d.units() * 2 * sizeof(int32_t));
+    a.part_o = take((size_t)a.shares * 2 * a.piece_rows * d.D * sizeof(float));
+    a.part_ml = take((size_t)a.shares * 2 * a.piece_rows * 2 * sizeof(float));
+  }
+  if (a.tile && a.nsplit > 1) {
+    const size_t rows = (size_t)a.nsplit * (size_t)n_tokens * d.Hq;
+    a.split_o = take(rows * d.D * sizeof(float));
+    a.split_ml = take(rows * 2 * sizeof(float));
+  }
+  a.total = o < 256 ? 256 : o;
+  return a;
+}
+
 }  // namespace ea
 
 extern "C" {

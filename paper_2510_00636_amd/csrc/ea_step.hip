@@ -1,0 +1,313 @@
+// What a model's step does to its cache before attention: the blocks that its tokens need, and their rows.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "ea_step.h"
+
+namespace ea {
+
+// ------------------------------------------------------------------------------- block tables
+// Everything follows from the lengths: prefix sums of the blocks wanted, the blocks given back and the tokens, which every
+// workgroup makes for itself (48 KiB of LDS for the largest batch), so that none waits for another.  The i-th block taken is
+// the i-th one given back, or else comes off the list's end; one given back and not taken goes onto it.  What is read (table
+// entries in front of the old ends, the list below its old end) is nowhere written, so the launch needs no order within.
+namespace {
+
+constexpr int kTableThreads = 256;
+
+__device__ __forceinline__ int count_le(const int* sums, int n, int x) {     // how many of n ascending sums are <= x
+  int lo = 0;
+  while (n > 0) {
+    const int half = n >> 1;
+    if (sums[lo + half] <= x) { lo += half + 1; n -= half + 1; } else n = half;
+  }
+  return lo;
+}
+
+}  // namespace
+
+__global__ __launch_bounds__(kTableThreads) void k_block_tables(BlockTableArgs a) {
+  extern __shared__ int sums[];      // three lists of B sums up to and with a sequence: wanted, given back, tokens
+  __shared__ long long wave_sum[3][4];
+  int *want_to = sums, *back_to = sums + a.B, *tok_to = sums + 2 * a.B;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const long long bs = 1ll << a.sh;
+  auto held_of = [&](int b) {
+    const long long x = a.len_old[b], h = x > 0 ? (x + bs - 1) >> a.sh : 0;
+    return h < a.max_blocks ? h : (long long)a.max_blocks;
+  };
+  auto need_of = [&](int b) {
+    const long long x = a.len_new[b];
+    return x > 0 ? (x + bs - 1) >> a.sh : 0ll;
+  };
+  const int per = (a.B + kTableThreads - 1) / kTableThreads, b0 = tid * per, b1 = min(b0 + per, a.B);
+  long long x[3] = {0, 0, 0};
+  auto add = [&](int b) {
+    const long long held = held_of(b), need = need_of(b), more = (long long)max(a.len_new[b], 0) - max(a.len_old[b], 0);
+    x[0] += need > held && need <= a.max_blocks ? need - held : 0;
+    x[1] += held > need ? held - need : 0;
+    x[2] += more > 0 ? more : 0;
+  };
+  for (int b = b0; b < b1; ++b) add(b);
+  long long incl[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    long long s = x[i];
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const long long y = __shfl_up(s, d);
+      if (lane >= d) s += y;
+    }
+    if (lane == 63) wave_sum[i][wave] = s;
+    incl[i] = s;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    long long s = incl[i] - x[i];
+    for (int w = 0; w < wave; ++w) s += wave_sum[i][w];
+    x[i] = s;
+  }
+  const long long top = 0x7fffffffll;
+  for (int b = b0; b < b1; ++b) {
+    add(b);
+    want_to[b] = (int)min(x[0], top);
+    back_to[b] = (int)min(x[1], top);
+    tok_to[b] = (int)min(x[2], top);
+  }
+  long long total[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) total[i] = wave_sum[i][0] + wave_sum[i][1] + wave_sum[i][2] + wave_sum[i][3];
+  long long count = *a.free_in;
+  count = count < 0 ? 0 : count > a.num_blocks ? a.num_blocks : count;
+  const long long back = total[1], there = min(count + back, top - 1);
+  __syncthreads();
+
+  // served: what it wants is there and fits its row of the table
+  auto served = [&](int b) {
+    const long long held = held_of(b), need = need_of(b);
+    return need <= a.max_blocks && (need <= held || want_to[b] <= there);
+  };
+  // blocks taken: the sums of the wanting sequences that are served are the first ones
+  const int reach = count_le(want_to, a.B, (int)there);
+  const long long taken = reach > 0 ? want_to[reach - 1] : 0;
+  auto given = [&](int r) {          // the r-th block given back
+    const int b = count_le(back_to, a.B, r);
+    return a.table[(long long)b * a.max_blocks + need_of(b) + (r - (b > 0 ? back_to[b - 1] : 0))];
+  };
+  auto block_taken = [&](long long i) { return i < back ? given((int)i) : a.free_list[count - 1 - (i - back)]; };
+  const long long first = (long long)blockIdx.x * kTableThreads + tid, step = (long long)gridDim.x * kTableThreads;
+  for (long long i = first; i < taken; i += step) {
+    const int b = count_le(want_to, a.B, (int)i);
+    a.table[(long long)b * a.max_blocks + held_of(b) + (i - (b > 0 ? want_to[b - 1] : 0))] = block_taken(i);
+  }
+  for (long long r = taken + first; r < back; r += step) {
+    const long long at = count + back - 1 - r;
+    if (at < a.num_blocks) a.free_list[at] = given((int)r);
+  }
+  const long long tokens = a.n_tokens < total[2] ? a.n_tokens : total[2];
+  for (long long t = first; t < a.n_tokens; t += step) {
+    if (t >= tokens) {
+      a.slots[t] = -1;
+      continue;
+    }
+    const int b = count_le(tok_to, a.B, (int)t);
+    const long long i = t - (b > 0 ? tok_to[b - 1] : 0), old = max(a.len_old[b], 0), row = old + i, j = row >> a.sh, held = held_of(b);
+    long long slot = -1;
+    if (served(b)) {
+      const long long block = j < held ? a.table[(long long)b * a.max_blocks + j]
+                                       : block_taken((b > 0 ? want_to[b - 1] : 0) + (j - held));
+      slot = (block << a.sh) + (row & (bs - 1));
+    }
+    a.slots[t] = slot;
+    a.pos[t] = (int)((a.seen ? (long long)a.seen[b] : old) + i);
+  }
+  if (blockIdx.x == 0) {
+    for (int b = tid; b < a.B; b += kTableThreads) {
+      a.len_out[b] = served(b) ? max(a.len_new[b], 0) : max(a.len_old[b], 0);
+      a.cu_tokens[b + 1] = tok_to[b];
+    }
+    if (tid == 0) {
+      a.cu_tokens[0] = 0;
+      const long long left = count + back - taken;
+      *a.free_out = (int)(left > a.num_blocks ? a.num_blocks : left);
+    }
+  }
+}
+
+hipError_t launch_block_tables(const BlockTableArgs& a, hipStream_t st) {
+  long long wgs = (a.n_tokens + 511) / 512;
+  const long long moved = (a.num_blocks + 8191) / 8192;
+  if (wgs < moved) wgs = moved;
+  wgs = wgs < 1 ? 1 : wgs > 128 ? 128 : wgs;
+  k_block_tables<<<(unsigned)wgs, kTableThreads, (size_t)a.B * 3 * sizeof(int), st>>>(a);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------------- new rows
+// A workgroup takes a few tokens: their angles go through LDS once (fp64 product and reduction to one turn, fp32 sine and
+// cosine), then every thread turns 8 pairs of channels of a head at a time and stores them.  Values take the same way
+// unturned.  Memory bounds it: every row is read and written once, 16 bytes a lane.
+namespace {
+
+template <typename T> struct Eight;                  // eight channels as they stand in memory
+template <> struct Eight<__bf16> { uint4 w; };
+template <> struct Eight<float> { float4 w[2]; };
+
+__device__ __forceinline__ void widen(const Eight<__bf16>& e, float* x) {
+  const uint32_t w[4] = {e.w.x, e.w.y, e.w.z, e.w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void widen(const Eight<float>& e, float* x) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) { x[4 * i] = e.w[i].x; x[4 * i + 1] = e.w[i].y; x[4 * i + 2] = e.w[i].z; x[4 * i + 3] = e.w[i].w; }
+}
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
+  typedef __bf16 pair __attribute__((ext_vector_type(2)));
+  const pair p = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, p);
+}
+__device__ __forceinline__ Eight<__bf16> narrow(const float* x, __bf16) {
+  return {make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]))};
+}
+__device__ __forceinline__ Eight<float> narrow(const float* x, float) {
+  return {{make_float4(x[0], x[1], x[2], x[3]), make_float4(x[4], x[5], x[6], x[7])}};
+}
+// eight numbers as e4m3 bytes: to nearest even, saturating (a NaN stays one)
+__device__ __forceinline__ uint2 bytes_of(const float* x) {
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = x[i] != x[i] ? x[i] : fminf(fmaxf(x[i], -448.0f), 448.0f);
+  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
+  return make_uint2((uint32_t)lo, (uint32_t)hi);
+}
+
+}  // namespace
+
+template <int D, typename T, bool FP8>
+__global__ __launch_bounds__(256) void k_append(AppendArgs a) {
+  __shared__ float2 turn[kAppendTokens][D / 2];
+  const int tid = threadIdx.x, first = blockIdx.x * a.tokens_per_wg;
+  const int count = min(a.tokens_per_wg, a.n_tokens - first);
+  if (a.inv_freq) {
+    for (int i = tid; i < count * (D / 2); i += 256) {
+      const int t = i / (D / 2), c = i % (D / 2);
+      // whole turns taken out in fp64: what is left keeps 2^-31 of a turn at any position of 32 bits
+      double y = (double)a.pos[first + t] * a.inv_freq[c] * 0.15915494309189533577;
+      y -= rint(y);
+      float si, co;
+      sincospif((float)(2.0 * y), &si, &co);
+      turn[t][c] = make_float2(co, si);
+    }
+    __syncthreads();
+  }
+  constexpr int kPieces = D / 16;                      // of 8 channel pairs in a head
+  const int heads = (a.q ? a.Hq : 0) + 2 * a.Hkv, q_heads = a.q ? a.Hq : 0;
+  for (int t = 0; t < count; ++t) {
+    const int token = first + t;
+    long long blk = 0;
+    int off = 0, b = 0, behind = 0;
+    if (a.slots) {
+      const long long slot = a.slots[token];
+      if (slot < 0 || slot >= (a.num_blocks << a.sh)) continue;
+      blk = slot >> a.sh;
+      off = (int)(slot & ((1 << a.sh) - 1));
+    } else {
+      int lo = 0, hi = a.B;                            // the token's sequence: cu[lo] <= token < cu[hi]
+      if (token < a.cu[0] || token >= a.cu[a.B]) continue;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (a.cu[mid] <= token) lo = mid; else hi = mid;
+      }
+      b = lo;
+      behind = a.cu[lo + 1] - token;
+    }
+    for (int it = blockIdx.y * 256 + tid; it < heads * kPieces; it += gridDim.y * 256) {
+      const int head = it / kPieces, c = it % kPieces;
+      // channels: halves apart or next to each other
+      const bool is_q = head < q_heads, is_v = head >= q_heads + a.Hkv;
+      const int h = is_q ? head : is_v ? head - q_heads - a.Hkv : head - q_heads;
+      const T* src = is_q ? (const T*)a.q + token * a.q_stride : is_v ? (const T*)a.v + token * a.v_stride : (const T*)a.k + token * a.k_stride;
+      const int c0 = a.rope_layout ? c * 16 : c * 8, c1 = a.rope_layout ? c0 + 8 : c0 + D / 2;
+      const Eight<T> e0 = *(const Eight<T>*)(src + h * D + c0), e1 = *(const Eight<T>*)(src + h * D + c1);
+      float x[16], y[16];
+      widen(e0, x);
+      widen(e1, x + 8);
+      if (a.inv_freq && !is_v) {
+        const float2* w = &turn[t][c * 8];
+        if (a.rope_layout) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            y[2 * i] = fmaf(x[2 * i], w[i].x, -x[2 * i + 1] * w[i].y);
+            y[2 * i + 1] = fmaf(x[2 * i], w[i].y, x[2 * i + 1] * w[i].x);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            y[i] = fmaf(x[i], w[i].x, -x[i + 8] * w[i].y);
+            y[i + 8] = fmaf(x[i], w[i].y, x[i + 8] * w[i].x);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y[i] = x[i];
+      }
+      if (is_q) {
+        T* dst = (T*)a.q_out + ((long long)token * a.Hq + h) * D;
+        *(Eight<T>*)(dst + c0) = narrow(y, T());
+        *(Eight<T>*)(dst + c1) = narrow(y + 8, T());
+        continue;
+      }
+      long long row;
+      if (a.slots) {
+        row = ((blk * a.Hkv + h) << a.sh) + off;
+      } else {
+        const long long r = (long long)a.lens[b * a.Hkv + h] - behind;
+        if (r < 0 || r >= a.n_cap) continue;
+        row = ((long long)b * a.Hkv + h) * a.n_cap + r;
+      }
+      if constexpr (FP8) {
+        const float* scale = is_v ? a.v_scale : a.k_scale;
+        if (scale) {
+          const float s = scale[b * a.Hkv + h];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) y[i] /= s;
+        }
+        uint8_t* dst = (uint8_t*)(is_v ? a.v_cache : a.k_cache) + row * D;
+        *(uint2*)(dst + c0) = bytes_of(y);
+        *(uint2*)(dst + c1) = bytes_of(y + 8);
+      } else {
+        T* dst = (T*)(is_v ? a.v_cache : a.k_cache) + row * D;
+        *(Eight<T>*)(dst + c0) = narrow(y, T());
+        *(Eight<T>*)(dst + c1) = narrow(y + 8, T());
+      }
+    }
+  }
+}
+
+hipError_t launch_append(const AppendArgs& given, const Dims& d, hipStream_t st) {
+  AppendArgs a = given;
+  // few tokens: a workgroup for each, and several where the heads give them something to do
+  a.tokens_per_wg = a.n_tokens >= 2048 ? kAppendTokens : 1;
+  const int items = ((a.q ? a.Hq : 0) + 2 * a.Hkv) * (d.D / 16);
+  const dim3 grid((a.n_tokens + a.tokens_per_wg - 1) / a.tokens_per_wg, a.tokens_per_wg == 1 ? (items + 255) / 256 : 1);
+#define EA_CASE(DD)                                                       \
+  if (d.D == DD) {                                                        \
+    if (d.kv_fp8) {                                                       \
+      if constexpr (DD > 64) k_append<DD, __bf16, true><<<grid, 256, 0, st>>>(a);   \
+    } else if (d.dtype == EA_BF16) k_append<DD, __bf16, false><<<grid, 256, 0, st>>>(a); \
+    else k_append<DD, float, false><<<grid, 256, 0, st>>>(a);             \
+  }
+  EA_CASE(64) EA_CASE(128) EA_CASE(256)
+#undef EA_CASE
+  return hipGetLastError();
+}
+
+}  // namespace ea

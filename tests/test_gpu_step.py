@@ -1,0 +1,371 @@
+"""A model's step over its cache on the GPU against its fp64 oracle: block tables, new rows, attention, and a loop of them.
+
+Tolerances, derived before the first run.  A rounding is off by at most half a step: bf16 2^-8, fp16 2^-11, fp32 2^-24, e4m3 2^-4,
+relative.  Rotated rows: angles keep 2^-31 of a turn, sine and cosine and three roundings of the products 2^-22 of the pair's
+length, then the rounding to the stored type.  Attention: see `attend_bounds`."""
+import numpy as np
+import pytest
+
+from ea_inputs import make_block_pools, widen, inv_freq_table, quantize_fp8, bf16_bits_from_f64
+from ea_inputs.torch_io import to_dev, to_host
+from oracle import ea_extensions as X
+from oracle import ea_step as S
+import paper_2510_00636_amd as ea
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+MARK = {"bf16": 0x7FC0, "f32": np.nan}          # what stands where nothing may look: NaN
+
+
+def store(x, dt):
+    return bf16_bits_from_f64(x) if dt == "bf16" else x.astype(np.float32)
+
+
+def kind(dt):
+    return ea.EA_BF16 if dt == "bf16" else ea.EA_F32
+
+
+def i32(x):
+    return to_dev(np.ascontiguousarray(np.asarray(x, dtype=np.int32)))
+
+
+# ----------------------------------------------------------------------------------- block tables
+def run_tables(table, free, count, old, new, bs, n_tokens, seen=None):
+    import torch
+    B, mb = table.shape
+    p = ea.make_params(B, 2, 1, 64, ea.EA_BF16)
+    t, f = i32(table), i32(free)
+    pg = ea.make_paged(t, bs, len(free))
+    out = [torch.full((x,), -7, dtype=torch.int32, device="cuda") for x in (B, 1, B + 1, max(n_tokens, 1))]
+    slots = torch.full((max(n_tokens, 1),), -7, dtype=torch.int64, device="cuda")
+    ea.block_tables(p, pg, i32(old), i32(new), f, i32([count]), out[0], out[1], out[2], n_tokens, slots, out[3],
+                    None if seen is None else i32(seen))
+    torch.cuda.synchronize()
+    return to_host(t), to_host(f), int(out[1]), to_host(out[0]), to_host(out[2]), to_host(slots)[:n_tokens], to_host(out[3])[:n_tokens]
+
+
+def check_tables(got, want, cu_end):
+    for g, w in zip(got[:6], want[:6]):
+        assert np.array_equal(g, w)
+    n = min(cu_end, len(got[6]))
+    assert np.array_equal(got[6][:n], want[6][:n]) and (got[6][n:] == -7).all()
+
+
+@pytest.mark.parametrize("B,bs", [(1, 16), (3, 16), (64, 32), (65, 16), (257, 64), (1000, 16), (4096, 256)])
+@pytest.mark.parametrize("kindof", ["one", "ragged", "cut", "both", "short"])
+def test_block_tables(B, bs, kindof):
+    r = np.random.default_rng(B * 7 + bs)
+    mb = 40
+    old = r.integers(0, mb * bs // 2, B)
+    if kindof == "one":
+        new = old + 1
+    elif kindof == "ragged":
+        new = old + np.where(r.random(B) < 0.2, r.integers(0, 9 * bs, B), r.integers(0, 3, B))
+    elif kindof == "cut":
+        new = (old * r.random(B)).astype(int)
+    else:
+        new = np.where(r.random(B) < 0.5, (old * r.random(B)).astype(int), old + r.integers(0, 2 * bs, B))
+    if kindof == "short" and B > 2:
+        new[1] = mb * bs + 1                                   # one that its row of the table has no room for
+        old[2], new[2] = -5, -9                                # and lengths that make no sense
+    held = [-(-max(int(x), 0) // bs) for x in old]
+    spare = 4 * B if kindof != "short" else max(1, B // 8)     # too few blocks: some are not served
+    nb = sum(held) + spare
+    ids = r.permutation(nb).astype(np.int32)
+    table, at = np.full((B, mb), -1, dtype=np.int32), 0
+    for b in range(B):
+        table[b, :held[b]] = ids[at:at + held[b]]
+        at += held[b]
+    free = np.full(nb, -1, dtype=np.int32)
+    free[:spare] = ids[at:]
+    seen = r.integers(0, 1 << 20, B)
+    total = int(np.maximum(0, np.maximum(new, 0) - np.maximum(old, 0)).sum())
+    for n_tokens in sorted({0, total, total + 300}):
+        for s in (None, seen):
+            want = S.block_tables(table, free, spare, old, new, bs, n_tokens, s)
+            check_tables(run_tables(table, free, spare, old, new, bs, n_tokens, s), want, total)
+    # growing by a step and going back restores the list, the table's held entries and the count
+    if kindof in ("one", "ragged"):
+        t, f, n, lens, *_ = run_tables(table, free, spare, old, new, bs, 0)
+        t2, f2, n2, lens2, *_ = run_tables(t, f, n, lens, old, bs, 0)
+        assert n2 == spare and np.array_equal(f2[:n2], free[:spare]) and np.array_equal(lens2, old) and np.array_equal(t2, t)
+
+
+# --------------------------------------------------------------------------------------- new rows
+def pair_length(x, interleaved):
+    h = x.shape[-1] // 2
+    if interleaved:
+        n = np.hypot(x[..., 0::2], x[..., 1::2])
+        return np.repeat(n, 2, axis=-1)
+    n = np.hypot(x[..., :h], x[..., h:])
+    return np.concatenate([n, n], axis=-1)
+
+
+def check_rotated(got, x, pos, inv, inter, dt):
+    want = S.rotate(x, pos, inv, inter)
+    tol = HALF[dt] * np.abs(want) + 2.0 ** -21 * pair_length(x, inter)
+    assert bool((np.abs(got - want) <= tol).all())
+
+
+@pytest.mark.parametrize("hq,hkv,d,bs,t", [(8, 2, 128, 16, 1), (5, 1, 64, 32, 37), (4, 4, 256, 16, 130), (6, 2, 128, 64, 2049),
+                                          (40, 8, 128, 16, 48)])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("form", ["dense", "strided", "in place", "no queries", "unturned"])
+def test_append_paged(hq, hkv, d, bs, t, inter, form):
+    import torch
+    r = np.random.default_rng(t + d)
+    nb = -(-t // bs) + 5
+    inv = inv_freq_table(d, 5e5)
+    x = store(r.standard_normal((t, hq + 2 * hkv, d)) * 3, "bf16")
+    pos = r.integers(0, 1 << 20, t)
+    pos[0] = 2 ** 31 - 1                                        # the farthest position there is
+    slots = r.permutation(nb * bs)[:t].astype(np.int64)
+    if t > 3:
+        slots[2], slots[3] = -1, nb * bs                        # left out: nothing of them is written
+    pools = [torch.full((nb, hkv, bs, d), 5.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    xd = to_dev(x)
+    parts = [xd[:, :hq], xd[:, hq:hq + hkv], xd[:, hq + hkv:]]
+    if form != "strided":
+        parts = [y.contiguous() for y in parts]
+    q = None if form in ("no queries", "unturned") else parts[0]
+    q_out = None if q is None else q if form == "in place" else torch.full((t, hq, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    p = ea.make_params(1, hq, hkv, d, ea.EA_BF16, rope_layout=int(inter))
+    rows = ea.make_new_rows(q, parts[1], parts[2], i32(pos), None if form == "unturned" else to_dev(inv))
+    table = i32([[0]])
+    ea.append_paged(p, rows, to_dev(slots), pools[0], pools[1], ea.make_paged(table, bs, nb), q_out)
+    torch.cuda.synchronize()
+    stored = (slots >= 0) & (slots < nb * bs)
+    xf = widen(x)
+    got = [widen(to_host(y)).transpose(0, 2, 1, 3).reshape(nb * bs, hkv, d) for y in pools]
+    if form == "unturned":
+        assert np.array_equal(got[0][slots[stored]], xf[stored, hq:hq + hkv])
+    else:
+        check_rotated(got[0][slots[stored]], xf[stored, hq:hq + hkv], pos[stored], inv, inter, "bf16")
+    assert np.array_equal(got[1][slots[stored]], xf[stored, hq + hkv:])
+    rest = np.setdiff1d(np.arange(nb * bs), slots[stored])
+    assert (got[0][rest] == 5.0).all() and (got[1][rest] == 5.0).all()
+    if q is not None:
+        qo = widen(to_host(q_out))
+        check_rotated(qo[stored], xf[stored, :hq], pos[stored], inv, inter, "bf16")
+        assert np.array_equal(qo[~stored], xf[~stored, :hq] if form == "in place" else np.full_like(qo[~stored], 7.0))
+
+
+@pytest.mark.parametrize("dt,d,hq,hkv", [("bf16", 128, 8, 2), ("bf16", 64, 4, 2), ("f32", 64, 4, 2), ("f32", 256, 3, 3), ("fp8", 128, 8, 2), ("fp8", 256, 2, 1)])
+@pytest.mark.parametrize("inter", [False, True])
+def test_append_to_heads_of_different_lengths(dt, d, hq, hkv, inter):
+    import torch
+    r = np.random.default_rng(d + hkv)
+    B, cap = 4, 50
+    m = np.array([1, 7, 0, 30])
+    cu = np.concatenate([[0], np.cumsum(m)])
+    t, room = int(cu[-1]), int(cu[-1]) + 9                      # rows behind the last sequence
+    lens = np.stack([r.integers(mm, cap + 1, hkv) for mm in m])
+    lens[1, 0] = 3                                              # fewer rows than new tokens: the first four have no row
+    lens[3, -1] = cap + 2                                       # and the last two none here
+    st = "f32" if dt == "f32" else "bf16"
+    x = store(r.standard_normal((room, hq + 2 * hkv, d)) * 2, st)
+    pos, inv = r.integers(0, 200000, room), inv_freq_table(d, 1e4)
+    xd = to_dev(x)
+    rows = ea.make_new_rows(xd[:, :hq], xd[:, hq:hq + hkv], xd[:, hq + hkv:], i32(pos), to_dev(inv))
+    q_out = torch.full((room, hq, d), 7.0, dtype=xd.dtype, device="cuda")
+    p = ea.make_params(B, hq, hkv, d, kind(st), rope_layout=int(inter))
+    if dt == "fp8":
+        cache = [torch.full((B, hkv, cap, d), 0x38, dtype=torch.uint8, device="cuda") for _ in range(2)]
+        scale = [(r.random((B, hkv)) * 0.05 + 0.004).astype(np.float32) for _ in range(2)]     # some saturate
+        ea.append_fp8(p, rows, i32(cu), i32(lens), cache[0], cache[1], to_dev(scale[0]), to_dev(scale[1]), cap, q_out)
+        got = [X.fp8_e4m3_decode(to_host(c)) for c in cache]
+        empty = X.fp8_e4m3_decode(np.array([0x38], dtype=np.uint8))[0]
+    else:
+        cache = [torch.full((B, hkv, cap, d), 5.0, dtype=xd.dtype, device="cuda") for _ in range(2)]
+        ea.append(p, rows, i32(cu), i32(lens), cache[0], cache[1], cap, q_out)
+        got, empty = [widen(to_host(c)) for c in cache], 5.0
+    torch.cuda.synchronize()
+    xf = widen(x)
+    want_k, v = S.rotate(xf[:, hq:hq + hkv], pos, inv, inter), xf[:, hq + hkv:]
+    slack = 2.0 ** -21 * pair_length(xf[:, hq:hq + hkv], inter)
+    for b in range(B):
+        for h in range(hkv):
+            written = np.zeros(cap, dtype=bool)
+            for i in range(m[b]):
+                row, tok = lens[b, h] - m[b] + i, cu[b] + i
+                if not 0 <= row < cap:
+                    continue
+                written[row] = True
+                if dt == "fp8":
+                    for c, w, s, more in ((got[0], want_k, scale[0], slack[tok, h]), (got[1], v, scale[1], 0.0)):
+                        y = np.clip(w[tok, h] / float(s[b, h]), -448, 448)
+                        # half a step: 2^-4 of a normal value, half of 2^-9 of those below 2^-6
+                        tol = np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10) + more / float(s[b, h]) + 2.0 ** -22 * np.abs(y)
+                        assert (np.abs(c[b, h, row] - y) <= tol).all()
+                else:
+                    assert (np.abs(got[0][b, h, row] - want_k[tok, h]) <= HALF[dt] * np.abs(want_k[tok, h]) + slack[tok, h]).all()
+                    assert np.array_equal(got[1][b, h, row], v[tok, h])
+            assert (got[0][b, h, ~written] == empty).all() and (got[1][b, h, ~written] == empty).all()
+    qo = widen(to_host(q_out))
+    check_rotated(qo[:t], xf[:t, :hq], pos[:t], inv, inter, st)
+    assert (qo[t:] == 7.0).all()
+
+
+# -------------------------------------------------------------------------------------- attention
+def attend_bounds(want, dt, n, d):
+    """Bounds of |out - exact| and |lse - exact|.
+
+    A logit is a sum of d products in fp32, of which each and each sum rounds once: off by at most delta = (d + 8) 2^-24 max
+    sum |q_c k_c| / sqrt(d), and two more roundings of it on the way to the exponent; a weight exp2f gives is off by 2^-22 more.
+    A weight's relative error e reaches the weighted sum as e * spread (the weighted mean of |v|) and the sum of weights as e, so
+    2 e * spread together.  Weights reach the second product rounded to the stored type: spread * HALF.  fp32 sums of n terms over
+    four wavefronts' lanes and joined pieces: (n / 8 + 64) 2^-24 each.  The result is rounded once."""
+    out, lse, spread, logit = want
+    delta = (d + 8) * 2.0 ** -24 * logit + 2.0 ** -22 * (1 + logit)
+    sums = (n / 8 + 64) * 2.0 ** -24
+    e = 2 * (delta + sums)
+    tol = (e[..., None] + (HALF[dt] if dt == "bf16" else 0.0)) * spread + HALF[dt] * np.abs(out) * 1.01 + 1e-37
+    seen = np.isfinite(lse)
+    return tol, delta + sums + 2.0 ** -22 * np.abs(np.where(seen, lse, 0.0)) + 2.0 ** -22
+
+
+def make_heads(r, lens, d, dt, cap):
+    """K, V [B, H, cap, d] with NaN from each head's length on, as stored and as fp64 lists."""
+    B, H = lens.shape
+    s, mu = np.exp(0.5 * r.standard_normal((H, d))), 1.4 * r.standard_normal((H, d))
+    k = store(r.standard_normal((B, H, cap, d)) * s[None, :, None] + mu[None, :, None], dt)
+    v = store(r.standard_normal((B, H, cap, d)) * np.exp(0.5 * r.standard_normal((B, H, cap, 1))), dt)
+    for b in range(B):
+        for h in range(H):
+            k[b, h, lens[b, h]:] = v[b, h, lens[b, h]:] = MARK[dt]
+    return k, v
+
+
+def attend_inputs(seed, hq, hkv, d, dt, lens, m, room=0, cap=None):
+    r = np.random.default_rng(seed)
+    lens = np.asarray(lens)
+    if lens.ndim == 1:
+        lens = np.repeat(lens[:, None], hkv, axis=1)
+    cap = int(max(lens.max(), 1)) if cap is None else cap
+    k, v = make_heads(r, lens, d, dt, cap)
+    cu = np.concatenate([[0], np.cumsum(m)])
+    q = store(r.standard_normal((int(cu[-1]) + room, hq, d)), dt)
+    return q, cu, k, v, lens
+
+
+def check_attend(got, lse, q, cu, k, v, lens, dt):
+    t, d = int(cu[-1]), q.shape[-1]
+    kf, vf = widen(k) if k.dtype != np.float64 else k, widen(v) if v.dtype != np.float64 else v
+    want = S.attend(widen(q), cu, kf, vf, lens)
+    tol, tol_lse = attend_bounds(want, dt, int(lens.max()), d)
+    out, ref = widen(got)[:t], want[0][:t]
+    assert np.isfinite(out).all()
+    worst = np.abs(out - ref) / tol[:t]
+    assert worst.max() <= 1, worst.max()
+    empty = ~np.isfinite(want[1][:t])
+    assert (out[empty] == 0).all()
+    if lse is not None:
+        assert (lse[:t][empty] == -np.inf).all()
+        assert (np.abs(lse[:t] - want[1][:t])[~empty] <= tol_lse[:t][~empty]).all()
+
+
+def outputs(q, dt):
+    import torch
+    t, hq, d = q.shape
+    out = torch.full((t, hq, d), 7.0, dtype=torch.bfloat16 if dt == "bf16" else torch.float32, device="cuda")
+    return out, torch.full((t, hq), 7.0, dtype=torch.float32, device="cuda")
+
+
+def run_paged(q, cu, k, v, lens, bs, n=None, max_new=None, seed=0, q_stride=0, with_lse=True):
+    import torch
+    B, hkv, cap, d = k.shape
+    p = ea.make_params(B, q.shape[1], hkv, d, ea.EA_BF16)
+    kp, vp, table, nb = make_block_pools(k, v, bs, seed)
+    for b in range(B):                                         # entries behind a sequence's blocks lead nowhere
+        table[b, -(-int(lens[b, 0]) // bs):] = -99
+    t = i32(table)
+    pg = ea.make_paged(t, bs, nb)
+    n = table.shape[1] * bs if n is None else n
+    step = ea.make_step(i32(cu), q.shape[0], int(np.diff(cu).max()) or 1 if max_new is None else max_new, q_stride)
+    cud = i32(cu)
+    step.cu_tokens = cud.data_ptr()
+    out, lse = outputs(q, "bf16")
+    ws = torch.empty(ea.attend_workspace_bytes(p, step, n), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    ea.attend_paged(p, to_dev(q), step, to_dev(kp), to_dev(vp), pg, i32(lens[:, 0]), n, out, lse if with_lse else None, ws)
+    torch.cuda.synchronize()
+    return to_host(out), lse.cpu().numpy()
+
+
+SHAPES = [(8, 2, 128), (5, 1, 128), (16, 1, 128), (14, 2, 64), (4, 2, 256), (24, 1, 128), (64, 1, 64), (40, 2, 256)]
+
+
+@pytest.mark.parametrize("hq,hkv,d", SHAPES)
+@pytest.mark.parametrize("bs", [16, 32, 256])
+def test_single_tokens_over_pools(hq, hkv, d, bs):
+    """Lengths on both sides of a tile's, a group's and a share's end, an empty cache and an absent sequence among them."""
+    lens = [1, 15, 16, 17, 31, 33, 127, 128, 129, 0, 300, 1000, 1025, 40, 2500]
+    m = [1] * len(lens)
+    m[13] = 0
+    q, cu, k, v, L = attend_inputs(hq + d, hq, hkv, d, "bf16", lens, m, room=3)
+    got, lse = run_paged(q, cu, k, v, L, bs)
+    check_attend(got, lse, q, cu, k, v, L, "bf16")
+    assert (widen(got)[cu[-1]:] == 7.0).all() and (lse[cu[-1]:] == 7.0).all()
+
+
+@pytest.mark.parametrize("hq,hkv,d", SHAPES)
+@pytest.mark.parametrize("m", [[2, 3, 1, 4], [33, 1, 0, 70], [64, 64, 5, 200], [9, 40, 300, 2]])
+def test_stretches_over_pools(hq, hkv, d, m):
+    """Stretches of new tokens, with what came before or without, and one with fewer rows than tokens (the first see nothing)."""
+    lens = [max(m[0] - 1, 0), 500 + m[1], 77, 1300]
+    q, cu, k, v, L = attend_inputs(sum(m) + d, hq, hkv, d, "bf16", lens, m, room=2)
+    got, lse = run_paged(q, cu, k, v, L, 16)
+    check_attend(got, lse, q, cu, k, v, L, "bf16")
+    assert (widen(got)[cu[-1]:] == 7.0).all() and (lse[cu[-1]:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dt,hq,hkv,d", [("bf16", 8, 2, 128), ("bf16", 6, 2, 64), ("bf16", 4, 2, 256), ("f32", 4, 2, 64),
+                                        ("f32", 7, 1, 128), ("f32", 3, 3, 256), ("f32", 64, 1, 64)])
+@pytest.mark.parametrize("m", [[1, 1, 1], [3, 0, 1], [40, 1, 130]])
+def test_heads_of_different_lengths(dt, hq, hkv, d, m):
+    import torch
+    r = np.random.default_rng(d + hq)
+    lens = r.integers(0, 900, (3, hkv))
+    lens[0, 0], lens[2, -1], lens[1, 0] = 0, 1500, 1
+    cap = 1501                                                 # rows of 16 do not end with the tensor
+    q, cu, k, v, L = attend_inputs(hq, hq, hkv, d, dt, lens, m, cap=cap)
+    p = ea.make_params(3, hq, hkv, d, kind(dt))
+    cud = i32(cu)
+    for n, lse_too in ((cap, True), (1500, False)):
+        step = ea.make_step(cud, q.shape[0], max(m))
+        out, lse = outputs(q, dt)
+        ws = torch.empty(ea.attend_workspace_bytes(p, step, n), dtype=torch.uint8, device="cuda").fill_(0xFF)
+        ea.attend(p, to_dev(q), step, to_dev(k), to_dev(v), i32(L), n, cap, out, lse if lse_too else None, ws)
+        torch.cuda.synchronize()
+        check_attend(to_host(out), lse.cpu().numpy() if lse_too else None, q, cu, k, v, L, dt)
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (5, 1, 128), (24, 1, 128), (4, 2, 256), (20, 1, 256)])
+@pytest.mark.parametrize("m", [[1, 1], [2, 6], [50, 200]])
+@pytest.mark.parametrize("scaled", [True, False])
+def test_fp8_caches(hq, hkv, d, m, scaled):
+    import torch
+    r = np.random.default_rng(d + hq)
+    lens = r.integers(200, 1300, (2, hkv))
+    lens[0, 0] = 33
+    q, cu, k, v, L = attend_inputs(hq, hq, hkv, d, "f32", lens, m)
+    q = store(q.astype(np.float64), "bf16")
+    k8, ks = quantize_fp8(np.nan_to_num(k.astype(np.float64)))
+    v8, vs = quantize_fp8(np.nan_to_num(v.astype(np.float64)))
+    for b in range(2):
+        for h in range(hkv):
+            k8[b, h, L[b, h]:] = v8[b, h, L[b, h]:] = 0x7F     # NaN
+    if not scaled:
+        ks[:], vs[:] = 1.0, 1.0
+        q = store(widen(q) * 0.05, "bf16")                     # bytes of up to 400: logits of the same size as with scales
+    p = ea.make_params(2, hq, hkv, d, ea.EA_BF16)
+    cud = i32(cu)
+    step = ea.make_step(cud, q.shape[0], max(m))
+    cap = k.shape[2]
+    out, lse = outputs(q, "bf16")
+    ws = torch.empty(ea.attend_workspace_bytes(p, step, cap), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    ea.attend_fp8(p, to_dev(q), step, to_dev(k8), to_dev(v8), to_dev(ks) if scaled else None, to_dev(vs) if scaled else None,
+                  i32(L), cap, cap, out, lse, ws)
+    torch.cuda.synchronize()
+    kf, vf = (X.fp8_e4m3_decode(x) * s.astype(np.float64)[:, :, None, None] for x, s in ((k8, ks), (v8, vs)))
+    check_attend(to_host(out), lse.cpu().numpy(), q, cu, kf, vf, L, "bf16")
