@@ -327,12 +327,26 @@ def compress_layer_fp8(p, q_win, window, q_pos0, inv_freq, t_next, k8, v8, k_sca
                                                 _nbytes(ws), _stream(stream)), "ea_compress_layer_fp8")
 
 
+def _addr(t):
+    """As _ptr, without an object of its own: what ctypes takes for a void*."""
+    return t if t is None or isinstance(t, int) else t.data_ptr()
+
+
+def _now(s):
+    """The stream's handle.  A step's calls are short next to what the host spends on one, so torch's current stream is asked for
+    by the call that its own kernels use (1.5 us less than a Stream object)."""
+    if s is None:
+        import torch
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return s if isinstance(s, int) else s.cuda_stream
+
+
 def block_tables(p, pg, len_old, len_new, free_list, free_in, len_out, free_out, cu_tokens, n_tokens=0, slots=None, pos=None,
                  seen=None, stream=None):
     """Writes the block table that pg points at, too."""
-    _check(load_library().ea_block_tables(ctypes.byref(p), ctypes.byref(pg), _ptr(len_old), _ptr(len_new), _ptr(free_list),
-                                          _ptr(free_in), _ptr(len_out), _ptr(free_out), _ptr(cu_tokens), int(n_tokens),
-                                          _ptr(slots), _ptr(pos), _ptr(seen), _stream(stream)), "ea_block_tables")
+    _check(load_library().ea_block_tables(p, pg, _addr(len_old), _addr(len_new), _addr(free_list), _addr(free_in), _addr(len_out),
+                                          _addr(free_out), _addr(cu_tokens), int(n_tokens), _addr(slots), _addr(pos), _addr(seen),
+                                          _now(stream)), "ea_block_tables")
 
 
 def _token_stride(t):
@@ -353,18 +367,18 @@ def make_new_rows(q, k, v, pos=None, inv_freq=None):
 
 
 def append_paged(p, rows, slots, k_pool, v_pool, pg, q_out=None, stream=None):
-    _check(load_library().ea_append_paged(ctypes.byref(p), ctypes.byref(rows), _ptr(slots), _ptr(k_pool), _ptr(v_pool),
-                                          ctypes.byref(pg), _ptr(q_out), _stream(stream)), "ea_append_paged")
+    _check(load_library().ea_append_paged(p, rows, _addr(slots), _addr(k_pool), _addr(v_pool),
+                                          pg, _addr(q_out), _now(stream)), "ea_append_paged")
 
 
 def append(p, rows, cu_tokens, lengths, k, v, n_cap, q_out=None, stream=None):
-    _check(load_library().ea_append(ctypes.byref(p), ctypes.byref(rows), _ptr(cu_tokens), _ptr(lengths), _ptr(k), _ptr(v),
-                                    int(n_cap), _ptr(q_out), _stream(stream)), "ea_append")
+    _check(load_library().ea_append(p, rows, _addr(cu_tokens), _addr(lengths), _addr(k), _addr(v),
+                                    int(n_cap), _addr(q_out), _now(stream)), "ea_append")
 
 
 def append_fp8(p, rows, cu_tokens, lengths, k8, v8, k_scale, v_scale, n_cap, q_out=None, stream=None):
-    _check(load_library().ea_append_fp8(ctypes.byref(p), ctypes.byref(rows), _ptr(cu_tokens), _ptr(lengths), _ptr(k8), _ptr(v8),
-                                        _ptr(k_scale), _ptr(v_scale), int(n_cap), _ptr(q_out), _stream(stream)), "ea_append_fp8")
+    _check(load_library().ea_append_fp8(p, rows, _addr(cu_tokens), _addr(lengths), _addr(k8), _addr(v8),
+                                        _addr(k_scale), _addr(v_scale), int(n_cap), _addr(q_out), _now(stream)), "ea_append_fp8")
 
 
 def make_step(cu_tokens, n_tokens, max_new, q_stride=0):
@@ -375,24 +389,24 @@ def make_step(cu_tokens, n_tokens, max_new, q_stride=0):
 
 
 def attend_workspace_bytes(p, step, n):
-    return int(load_library().ea_attend_workspace_bytes(ctypes.byref(p), ctypes.byref(step), int(n)))
+    return int(load_library().ea_attend_workspace_bytes(p, step, int(n)))
 
 
 def attend(p, q, step, k, v, lengths, n, n_cap, out, lse, ws, stream=None):
-    _check(load_library().ea_attend(ctypes.byref(p), _ptr(q), ctypes.byref(step), _ptr(k), _ptr(v), _ptr(lengths), int(n),
-                                    int(n_cap), _ptr(out), _ptr(lse), _ptr(ws), _nbytes(ws), _stream(stream)), "ea_attend")
+    _check(load_library().ea_attend(p, _addr(q), step, _addr(k), _addr(v), _addr(lengths), int(n),
+                                    int(n_cap), _addr(out), _addr(lse), _addr(ws), _nbytes(ws), _now(stream)), "ea_attend")
 
 
 def attend_paged(p, q, step, k_pool, v_pool, pg, lengths, n, out, lse, ws, stream=None):
-    _check(load_library().ea_attend_paged(ctypes.byref(p), _ptr(q), ctypes.byref(step), _ptr(k_pool), _ptr(v_pool),
-                                          ctypes.byref(pg), _ptr(lengths), int(n), _ptr(out), _ptr(lse), _ptr(ws), _nbytes(ws),
-                                          _stream(stream)), "ea_attend_paged")
+    _check(load_library().ea_attend_paged(p, _addr(q), step, _addr(k_pool), _addr(v_pool),
+                                          pg, _addr(lengths), int(n), _addr(out), _addr(lse), _addr(ws), _nbytes(ws),
+                                          _now(stream)), "ea_attend_paged")
 
 
 def attend_fp8(p, q, step, k8, v8, k_scale, v_scale, lengths, n, n_cap, out, lse, ws, stream=None):
-    _check(load_library().ea_attend_fp8(ctypes.byref(p), _ptr(q), ctypes.byref(step), _ptr(k8), _ptr(v8), _ptr(k_scale),
-                                        _ptr(v_scale), _ptr(lengths), int(n), int(n_cap), _ptr(out), _ptr(lse), _ptr(ws),
-                                        _nbytes(ws), _stream(stream)), "ea_attend_fp8")
+    _check(load_library().ea_attend_fp8(p, _addr(q), step, _addr(k8), _addr(v8), _addr(k_scale),
+                                        _addr(v_scale), _addr(lengths), int(n), int(n_cap), _addr(out), _addr(lse), _addr(ws),
+                                        _nbytes(ws), _now(stream)), "ea_attend_fp8")
 
 
 N_STAGES = 6

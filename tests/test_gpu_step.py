@@ -369,3 +369,240 @@ def test_fp8_caches(hq, hkv, d, m, scaled):
     torch.cuda.synchronize()
     kf, vf = (X.fp8_e4m3_decode(x) * s.astype(np.float64)[:, :, None, None] for x, s in ((k8, ks), (v8, vs)))
     check_attend(to_host(out), lse.cpu().numpy(), q, cu, kf, vf, L, "bf16")
+
+
+# -------------------------------------------------------------------------------- they run together
+class Loop:
+    """A batch of sequences over block pools: steps of new tokens, and compress passes in between.  The oracle keeps every
+    sequence's rows in numpy; the GPU's state is never corrected from it."""
+
+    def __init__(self, B, hq, hkv, d, bs, max_blocks, num_blocks, seed):
+        import torch
+        self.r, self.B, self.hq, self.hkv, self.d, self.bs = np.random.default_rng(seed), B, hq, hkv, d, bs
+        self.p = ea.make_params(B, hq, hkv, d, ea.EA_BF16)
+        self.table = torch.full((B, max_blocks), -1, dtype=torch.int32, device="cuda")
+        self.pg = ea.make_paged(self.table, bs, num_blocks)
+        self.pools = [torch.full((num_blocks, hkv, bs, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        self.free = to_dev(self.r.permutation(num_blocks).astype(np.int32))
+        self.count, self.lens = [i32([num_blocks]), i32([0])], [i32([0] * B), i32([0] * B)]
+        self.inv = inv_freq_table(d, 5e5)
+        self.invd = to_dev(self.inv)
+        self.seen, self.rows = np.zeros(B, dtype=int), [[np.zeros((0, hkv, d)), np.zeros((0, hkv, d))] for _ in range(B)]
+        self.n = max_blocks * bs
+
+    def step(self, m, room=0):
+        import torch
+        m = np.asarray(m)
+        t = int(m.sum()) + room
+        qkv = store(self.r.standard_normal((t, self.hq + 2 * self.hkv, self.d)) * 1.5, "bf16")
+        new = (self.lens[0].cpu().numpy() + m)
+        cu, slots, pos = (torch.full(s, -5, dtype=x, device="cuda") for s, x in (((self.B + 1,), torch.int32), ((t,), torch.int64), ((t,), torch.int32)))
+        pos.fill_(0)
+        ea.block_tables(self.p, self.pg, self.lens[0], i32(new), self.free, self.count[0], self.lens[1], self.count[1], cu, t, slots, pos,
+                        i32(self.seen))
+        x = to_dev(qkv)
+        rows = ea.make_new_rows(x[:, :self.hq], x[:, self.hq:self.hq + self.hkv], x[:, self.hq + self.hkv:], pos, self.invd)
+        q = torch.zeros(t, self.hq, self.d, dtype=torch.bfloat16, device="cuda")
+        ea.append_paged(self.p, rows, slots, self.pools[0], self.pools[1], self.pg, q)
+        st = ea.make_step(cu, t, int(m.max()))
+        out, lse = outputs(q, "bf16")
+        ws = torch.empty(ea.attend_workspace_bytes(self.p, st, self.n), dtype=torch.uint8, device="cuda")
+        ea.attend_paged(self.p, q, st, self.pools[0], self.pools[1], self.pg, self.lens[1], self.n, out, lse, ws)
+        torch.cuda.synchronize()
+        self.lens.reverse(), self.count.reverse()
+        # the oracle: what stands in the cache is what the call stored, to within its own rounding
+        xf, at = widen(qkv), np.concatenate([[0], np.cumsum(m)])
+        assert np.array_equal(cu.cpu().numpy(), at) and np.array_equal(self.lens[0].cpu().numpy(), new)
+        kp, vp, tab = (widen(to_host(y)) if y.dtype == torch.bfloat16 else to_host(y) for y in (*self.pools, self.table))
+        used = []
+        for b in range(self.B):
+            s = slice(at[b], at[b + 1])
+            k = S.rotate(xf[s, self.hq:self.hq + self.hkv], self.seen[b] + np.arange(m[b]), self.inv, False)
+            blocks = tab[b, :-(-int(new[b]) // self.bs)]
+            used += blocks.tolist()
+            have = [X.paged_rows(z, blocks[None], int(new[b]))[0].transpose(1, 0, 2) if new[b] else np.zeros((0, self.hkv, self.d)) for z in (kp, vp)]
+            old = len(self.rows[b][0])
+            assert np.array_equal(have[0][:old], self.rows[b][0]) and np.array_equal(have[1][:old], self.rows[b][1])
+            if m[b]:
+                check_rotated(have[0][old:], xf[s, self.hq:self.hq + self.hkv], self.seen[b] + np.arange(m[b]), self.inv, False, "bf16")
+                assert np.array_equal(have[1][old:], xf[s, self.hq + self.hkv:])
+            self.rows[b] = have
+        assert len(set(used)) == len(used) and len(used) + int(self.count[0]) == len(self.free)
+        assert sorted(used + self.free[:int(self.count[0])].tolist()) == list(range(len(self.free)))
+        self.seen += m
+        L = np.repeat(new[:, None], self.hkv, axis=1)
+        lists = [[[self.rows[b][i][:, h] for h in range(self.hkv)] for b in range(self.B)] for i in range(2)]
+        want = S.attend(widen(to_host(q)), at, lists[0], lists[1], L)
+        tol, tol_lse = attend_bounds(want, "bf16", int(new.max()), self.d)
+        n = int(at[-1])
+        assert bool((np.abs(widen(to_host(out)) - want[0])[:n] <= tol[:n]).all())
+        assert bool((np.abs(lse.cpu().numpy() - want[1])[:n] <= tol_lse[:n]).all())
+        return out
+
+    def compress(self, n_keep):
+        """All sequences hold as many rows as each other: a pass over the pools, then the blocks behind go back."""
+        import torch
+        n = int(self.lens[0][0])
+        w = 16
+        win = to_dev(store(self.r.standard_normal((self.B, self.hq, w, self.d)), "bf16"))
+        ws = torch.empty(ea.workspace_bytes(self.p, n, w), dtype=torch.uint8, device="cuda")
+        idx = torch.zeros(self.B, self.hkv, n_keep, dtype=torch.int32, device="cuda")
+        ea.compress_layer_paged(self.p, win, w, int(self.seen[0]) - w, self.invd, int(self.seen[0]), self.pools[0], self.pools[1], self.pg, n, n_keep,
+                                0, None, idx, None, ws)
+        cu = torch.zeros(self.B + 1, dtype=torch.int32, device="cuda")
+        ea.block_tables(self.p, self.pg, self.lens[0], i32([n_keep] * self.B), self.free, self.count[0], self.lens[1], self.count[1], cu)
+        torch.cuda.synchronize()
+        self.lens.reverse(), self.count.reverse()
+        assert (self.lens[0] == n_keep).all() and (cu == 0).all()
+        kept = idx.cpu().numpy()
+        for b in range(self.B):
+            self.rows[b] = [np.stack([z[kept[b, h], h] for h in range(self.hkv)], axis=1) for z in self.rows[b]]
+
+
+@pytest.mark.parametrize("B,hq,hkv,d,bs", [(3, 8, 2, 128, 16), (2, 5, 1, 64, 32), (2, 4, 2, 256, 16)])
+def test_a_loop_of_steps_and_compress_passes(B, hq, hkv, d, bs):
+    s = Loop(B, hq, hkv, d, bs, max_blocks=40, num_blocks=B * 30 + 2, seed=d)
+    s.step([200] * B)                          # the prompts
+    for _ in range(3):
+        s.step([1] * B, room=5)                # single tokens, with room behind them
+    s.compress(90)                             # rows are no positions from here on
+    s.step([3] * B)
+    s.step([0] + [7] * (B - 1))                # one sequence waits
+    s.step([41] + [34] * (B - 1))
+    s.compress(64)
+    s.step([1] * B)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp8"])
+def test_generation_over_an_adaptive_cache(dt):
+    """compress_layer_adaptive leaves heads of different lengths; steps go on from there."""
+    import torch
+    r = np.random.default_rng(5)
+    B, hq, hkv, d, n, cap, w = 2, 8, 4, 128, 600, 700, 16
+    inv = inv_freq_table(d, 5e5)
+    p = ea.make_params(B, hq, hkv, d, ea.EA_BF16)
+    if dt == "bf16":
+        k, v = (to_dev(store(r.standard_normal((B, hkv, cap, d)), "bf16")) for _ in range(2))
+        win = to_dev(store(r.standard_normal((B, hq, w, d)), "bf16"))
+        ws = torch.empty(ea.workspace_bytes(p, n, w), dtype=torch.uint8, device="cuda")
+        idx, lens = torch.zeros(B, hkv, n, dtype=torch.int32, device="cuda"), torch.zeros(B, hkv, dtype=torch.int32, device="cuda")
+        ea.compress_layer_adaptive(p, win, w, n - w, to_dev(inv), n, k, v, n, cap, 200, 20, None, idx, lens, ws)
+        assert len(set(lens.flatten().tolist())) > 1
+        scale = [None, None]
+    else:
+        k, v = (to_dev(r.integers(0, 0x77, (B, hkv, cap, d)).astype(np.uint8)) for _ in range(2))
+        lens = i32(r.integers(100, 600, (B, hkv)))
+        scale = [to_dev((r.random((B, hkv)) * 0.02 + 0.01).astype(np.float32)) for _ in range(2)]
+    seen = n
+    for m in ([1, 1], [5, 2], [1, 0], [40, 30]):
+        t = sum(m)
+        cu = i32(np.concatenate([[0], np.cumsum(m)]))
+        lens = lens + i32(m)[:, None]
+        x = to_dev(store(r.standard_normal((t, hq + 2 * hkv, d)), "bf16"))
+        pos = i32(np.concatenate([seen + np.arange(a) for a in m]))
+        q = torch.zeros(t, hq, d, dtype=torch.bfloat16, device="cuda")
+        rows = ea.make_new_rows(x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], pos, to_dev(inv))
+        st = ea.make_step(cu, t, max(m))
+        out, lse = outputs(q, "bf16")
+        ws = torch.empty(ea.attend_workspace_bytes(p, st, cap), dtype=torch.uint8, device="cuda")
+        if dt == "bf16":
+            ea.append(p, rows, cu, lens, k, v, cap, q)
+            ea.attend(p, q, st, k, v, lens, cap, cap, out, lse, ws)
+        else:
+            ea.append_fp8(p, rows, cu, lens, k, v, scale[0], scale[1], cap, q)
+            ea.attend_fp8(p, q, st, k, v, scale[0], scale[1], lens, cap, cap, out, lse, ws)
+        torch.cuda.synchronize()
+        if dt == "bf16":
+            kf, vf = widen(to_host(k)), widen(to_host(v))
+        else:
+            kf, vf = (X.fp8_e4m3_decode(to_host(z)) * to_host(s).astype(np.float64)[:, :, None, None] for z, s in ((k, scale[0]), (v, scale[1])))
+        check_attend(to_host(out), lse.cpu().numpy(), to_host(q), cu.cpu().numpy(), kf, vf, lens.cpu().numpy(), "bf16")
+        seen += max(m)
+
+
+def test_a_step_in_a_graph_follows_the_lengths():
+    """One captured step, replayed over lengths that grow on the device, against eager calls; eager work on the same workspace and
+    other tensors in between."""
+    import torch
+    r = np.random.default_rng(11)
+    B, hq, hkv, d, bs, mb = 5, 8, 2, 128, 16, 40
+    nb = B * mb + 3
+    p = ea.make_params(B, hq, hkv, d, ea.EA_BF16)
+    inv = to_dev(inv_freq_table(d, 5e5))
+    state = {}
+    for name in ("graph", "eager"):
+        g = np.random.default_rng(3)
+        table = torch.full((B, mb), -1, dtype=torch.int32, device="cuda")
+        state[name] = dict(table=table, pg=ea.make_paged(table, bs, nb), pools=[torch.zeros(nb, hkv, bs, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)],
+                           free=to_dev(g.permutation(nb).astype(np.int32)), count=i32([nb]), lens=i32([0, 3, 100, 15, 400]) * 0, seen=i32([0] * B),
+                           more=i32([1] * B), len_out=i32([0] * B), count_out=i32([0]), cu=i32([0] * (B + 1)), slots=torch.zeros(60, dtype=torch.int64, device="cuda"),
+                           pos=torch.zeros(60, dtype=torch.int32, device="cuda"), x=torch.zeros(60, hq + 2 * hkv, d, dtype=torch.bfloat16, device="cuda"),
+                           q=torch.zeros(60, hq, d, dtype=torch.bfloat16, device="cuda"), out=torch.zeros(60, hq, d, dtype=torch.bfloat16, device="cuda"),
+                           lse=torch.zeros(60, hq, device="cuda"), want=i32([0] * B))
+
+    def prepare(s, ws_of):
+        st = ea.make_step(s["cu"], 60, 60)
+        s["st"], s["ws"] = st, ws_of if ws_of is not None else torch.empty(ea.attend_workspace_bytes(p, st, mb * bs), dtype=torch.uint8, device="cuda")
+
+    def go(s):
+        torch.add(s["lens"], s["more"], out=s["want"])
+        ea.block_tables(p, s["pg"], s["lens"], s["want"], s["free"], s["count"], s["len_out"], s["count_out"], s["cu"], 60, s["slots"], s["pos"], s["seen"])
+        rows = ea.make_new_rows(s["x"][:, :hq], s["x"][:, hq:hq + hkv], s["x"][:, hq + hkv:], s["pos"], inv)
+        ea.append_paged(p, rows, s["slots"], s["pools"][0], s["pools"][1], s["pg"], s["q"])
+        ea.attend_paged(p, s["q"], s["st"], s["pools"][0], s["pools"][1], s["pg"], s["len_out"], mb * bs, s["out"], s["lse"], s["ws"])
+        s["lens"].copy_(s["len_out"])
+        s["count"].copy_(s["count_out"])
+        s["seen"].add_(s["more"])
+
+    prepare(state["graph"], None)
+    prepare(state["eager"], state["graph"]["ws"])              # both use one workspace, one after the other
+    side = torch.cuda.Stream()
+    s = state["graph"]
+    graph = torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        go(s)
+    torch.cuda.synchronize()
+    for more in ([20, 3, 0, 30, 1], [1] * 5, [1] * 5, [0, 1, 50, 1, 1], [1] * 5, [2, 2, 2, 2, 2], [1] * 5):
+        x = to_dev(store(r.standard_normal((60, hq + 2 * hkv, d)), "bf16"))
+        for z in state.values():
+            z["x"].copy_(x)
+            z["more"].copy_(i32(more))
+        state["graph"]["ws"].fill_(0xA5)                       # undefined between calls
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        go(state["eager"])
+        torch.cuda.synchronize()
+        n = sum(more)
+        for key in ("table", "free", "count", "lens", "cu", "slots", "seen"):
+            assert torch.equal(state["graph"][key], state["eager"][key]), key
+        for key in ("q", "out", "lse"):
+            assert torch.equal(state["graph"][key][:n], state["eager"][key][:n]), key
+
+
+def test_calls_on_side_streams():
+    """Two calls at once, each with a workspace of its own, give what they give alone."""
+    import torch
+    jobs = []
+    for seed, m in ((1, [1, 1, 1]), (2, [30, 1, 64])):
+        q, cu, k, v, L = attend_inputs(seed, 8, 2, 128, "bf16", [700, 1300, 90], m)
+        jobs.append((run_paged(q, cu, k, v, L, 16, seed=seed), (q, cu, k, v, L)))
+    p = ea.make_params(3, 8, 2, 128, ea.EA_BF16)
+    streams, keep = [torch.cuda.Stream() for _ in range(2)], []
+    for (_, (q, cu, k, v, L)), seed in zip(jobs, (1, 2)):
+        kp, vp, table, nb = make_block_pools(k, v, 16, seed)
+        t, cud, ld = i32(table), i32(cu), i32(L[:, 0])
+        pg, st = ea.make_paged(t, 16, nb), ea.make_step(cud, q.shape[0], int(np.diff(cu).max()))
+        out, lse = outputs(q, "bf16")
+        n = table.shape[1] * 16
+        ws = torch.empty(ea.attend_workspace_bytes(p, st, n), dtype=torch.uint8, device="cuda")
+        keep.append((to_dev(q), st, to_dev(kp), to_dev(vp), pg, ld, n, out, lse, ws, t))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, (q, st, kp, vp, pg, ld, n, out, lse, ws, _t) in zip(streams, keep):
+            ea.attend_paged(p, q, st, kp, vp, pg, ld, n, out, lse, ws, stream=s)
+    torch.cuda.synchronize()
+    for ((want, want_lse), _), k in zip(jobs, keep):
+        assert np.array_equal(to_host(k[7]), want) and np.array_equal(k[8].cpu().numpy(), want_lse)
