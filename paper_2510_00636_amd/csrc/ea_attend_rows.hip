@@ -2,8 +2,10 @@
 //
 // The cache is read once and that bounds it (4 G d operations for 4 d bytes of a pair), so the whole chip reads all the time:
 // the call's heads are laid end to end in groups of 128 rows and every workgroup takes an equal, contiguous share of them,
-// from the lengths that stand on the device.  A head that falls into several shares leaves partial results (maximum, sum,
-// weighted values) that a second launch joins in the order of the shares.
+// from the lengths that stand on the device.  A head that falls into several shares leaves a partial result (maximum, sum,
+// weighted values) of each, which a second launch joins in the order of the shares.
+// (One launch, with the workgroup that arrives last joining, was slower: it waits for its stores, for a counter across the dies
+// and, alone, for all the pieces: 40 query heads over 4097 rows 20.6 us against 9.3 and 4.2.)
 //
 // S^T = K Q^T and O^T = V^T P^T by v_mfma_f32_16x16x32_bf16, 32 keys at a time and wavefront.  A lane of group g (of four) then
 // holds of its query row the keys 4 g + r of either half of the tile, which is a set of eight keys that the second product
@@ -59,15 +61,32 @@ __device__ __forceinline__ void widen_piece(const VPiece<D, FP8>& p, uint32_t* o
   }
 }
 
+// four channels of a finished row
+template <int D>
+__device__ __forceinline__ void write_row(const AttendArgs& a, int t0, int h, int unit, int row, int c4, float top, float sum, float4 acc) {
+  const int tok = row / a.G, hd = row - tok * a.G;
+  const long long at = (long long)(t0 + tok) * a.Hq + h * a.G + hd;
+  const bool any = sum > 0.0f || sum != sum;
+  const float f = (a.vscale ? a.vscale[unit] : 1.0f) / sum;
+  *(uint2*)((__bf16*)a.out + at * D + c4) =
+      any ? make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f)) : make_uint2(0u, 0u);
+  if (a.lse && c4 == 0) a.lse[at] = natural_lse(top, sum);
+}
+
 }  // namespace
+
+// A head's (or its part's) results of one wavefront: [wavefront][row][channel], rows four floats apart from a whole number of
+// 64 banks; behind them maxima and sums.
+template <int D, int MT> constexpr int rows_lds_floats() { return 4 * 16 * MT * (D + 4) + 4 * 16 * MT * 2; }
 
 template <int D, bool FP8, int MT>
 __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(AttendArgs a) {
   using S = RowShape<D, FP8>;
-  constexpr int kM = 16 * MT;
-  __shared__ float pass_o[2][MT * S::kTiles * 4][64];
-  __shared__ float pass_ml[4][2][kM];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int kM = 16 * MT, kPitch = D + 4;
+  extern __shared__ float lds[];
+  float* pass_o = lds;
+  float2* pass_ml = (float2*)(lds + 4 * kM * kPitch);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n16 = lane & 15, g = lane >> 4;
   const int supers = a.per_head ? a.B * a.Hkv : a.B, mult = a.per_head ? 1 : a.Hkv;
 
@@ -78,55 +97,143 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
   for (int base = 64; base < supers; base += 64)
     total += last_lane(wave_prefix(base + lane < supers ? groups_of(a, base + lane) : 0));
   const long long all = (long long)total * mult;
-  const long long per = (all + gridDim.x - 1) / gridDim.x;
-  const long long x0 = per * blockIdx.x, x1 = x0 + per < all ? x0 + per : all;
+  const int per = (int)((all + gridDim.x - 1) / gridDim.x);
+  const long long x0 = (long long)per * blockIdx.x, x1 = x0 + per < all ? x0 + per : all;
   if (x0 >= x1) return;
-  int su = 0, have = 0;     // `have`: groups in front of super-unit su
+
+  // ---- a part of a head that falls into the share
+  struct Part {
+    int su, have, grp;        // super-unit, groups in front of it, its groups
+    int b, h, off, take;      // sequence, KV head, first group of the part and how many
+    int t0, m, len;
+  };
+  long long x = x0;
+  auto fill = [&](Part& c) {
+    const int rel = (int)(x - (long long)c.have * mult), hh = rel / c.grp;
+    c.off = rel - hh * c.grp;
+    c.take = (int)(x1 - x < c.grp - c.off ? x1 - x : c.grp - c.off);
+    c.b = a.per_head ? c.su / a.Hkv : c.su;
+    c.h = a.per_head ? c.su - c.b * a.Hkv : hh;
+    c.t0 = __builtin_amdgcn_readfirstlane(first_token(a, c.b));
+    c.m = __builtin_amdgcn_readfirstlane(first_token(a, c.b + 1)) - c.t0;
+    c.len = __builtin_amdgcn_readfirstlane(rows_of(a, c.b, c.h));
+  };
+  Part cur;
+  cur.su = -1;
+  cur.have = 0;
   for (int base = 0; base < supers; base += 64) {
     if (base > 0) pre = wave_prefix(mine = base + lane < supers ? groups_of(a, base + lane) : 0);
-    const uint64_t in = __ballot((long long)(have + pre) * mult > x0);
+    const uint64_t in = __ballot((long long)(cur.have + pre) * mult > x0);
     if (in) {
       const int l = __builtin_ctzll(in);
-      su = base + l;
-      have += __builtin_amdgcn_readlane(pre, l) - __builtin_amdgcn_readlane(mine, l);
+      cur.su = base + l;
+      cur.grp = __builtin_amdgcn_readlane(mine, l);
+      cur.have += __builtin_amdgcn_readlane(pre, l) - cur.grp;
       break;
     }
-    have += last_lane(pre);
+    cur.have += last_lane(pre);
   }
-  int grp = groups_of(a, su);
-  grp = __builtin_amdgcn_readfirstlane(grp);
-  if (grp == 0) return;
+  if (cur.su < 0) return;
+  fill(cur);
 
-  long long x = x0;
-  while (x < x1) {
-    const int rel = (int)(x - (long long)have * mult);
-    const int hh = rel / grp, off = rel - hh * grp;
-    const int take = (int)(x1 - x < grp - off ? x1 - x : grp - off);
-    const int b = a.per_head ? su / a.Hkv : su, h = a.per_head ? su - b * a.Hkv : hh;
-    const int t0 = __builtin_amdgcn_readfirstlane(first_token(a, b));
-    const int m = __builtin_amdgcn_readfirstlane(first_token(a, b + 1)) - t0;
-    const int len = __builtin_amdgcn_readfirstlane(rows_of(a, b, h));
-    const int rows = m * a.G;
+  // ---- what is in flight: a tile of K and of V, and the next part's queries
+  int entries = 0, window = 0;
+  auto entries_of = [&](const Part& c, int from) {      // of the wavefront's 32 tiles from row `from` on, two per tile, one in each lane
+    const int r = from + (lane >> 1) * kGroup + (lane & 1) * 16;
+    return table_entry(a, c.b, r < c.len ? r : c.len > 0 ? c.len - 1 : 0);
+  };
+  u32x4 kraw[2][FP8 ? S::kSteps / 2 : S::kSteps];
+  VPiece<D, FP8> vraw[8][S::kLoads];
+  long long base[2];
+  int lim[2];
+  auto place = [&](const Part& c, int at) {             // the two halves of the tile at row `at`: where they start, and their last row
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int r = at + t * 16 < c.len ? at + t * 16 : at;
+      const int e = __builtin_amdgcn_readlane(entries, (at - window) / kGroup * 2 + (r != at ? 1 : 0));
+      base[t] = row_base(a, c.b, c.h, r, e) * S::kBytes;
+      lim[t] = c.len - 1 - r < 15 ? c.len - 1 - r : 15;
+    }
+  };
+  auto load_k = [&]() {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const char* p = (const char*)a.k + base[t];
+      const int at = (n16 < lim[t] ? n16 : lim[t]) * S::kBytes + g * 16;
+#pragma unroll
+      for (int s = 0; s < (FP8 ? S::kSteps / 2 : S::kSteps); ++s) kraw[t][s] = *(const u32x4*)(p + at + s * 64);
+    }
+  };
+  auto load_v = [&]() {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const char* p = (const char*)a.v + base[j >> 2];
+      const int r = 4 * g + (j & 3), last = lim[j >> 2];
+      const int at = (r < last ? r : last) * S::kBytes + n16 * (S::kCpl * (FP8 ? 1 : 2));
+#pragma unroll
+      for (int u = 0; u < S::kLoads; ++u)
+        vraw[j][u] = *(const VPiece<D, FP8>*)(p + at + u * (16 * S::kCpl * (FP8 ? 1 : 2)));
+    }
+  };
+  // the query operand: row n16 (+ 16) of the head's rows (token, head of the group), channels as the keys' operand has them
+  u32x4 q[MT][S::kSteps];
+  auto load_q = [&](const Part& c) {
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      const int row = t * 16 + n16, in = row < c.m * a.G ? row : 0, tok = in / a.G, hd = in - tok * a.G;
+      const __bf16* src = (const __bf16*)a.q + (long long)(c.t0 + tok) * a.q_stride + (c.h * a.G + hd) * D;
+#pragma unroll
+      for (int s = 0; s < S::kSteps; ++s)
+        q[t][s] = *(const u32x4*)(src + (FP8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8));
+    }
+  };
+  // the first loads of a part, in the order of what waits for them
+  auto begin = [&](const Part& c) {
+    const int row = c.off * kGroup + wave * 32;
+    window = row;
+    if (row < c.len) {
+      place(c, row);
+      load_k();
+      load_v();
+    }
+    load_q(c);
+  };
+  entries = entries_of(cur, cur.off * kGroup + wave * 32);
+  begin(cur);
 
-    // the query operand: row n16 (+ 16) of the head's rows (token, head of the group), channels as the keys' operand has them
-    bf16x8 q[MT][S::kSteps];
+  for (;;) {
+    x += cur.take;
+    // ---- the part behind this one, and the entries of its blocks
+    Part next = cur;
+    int next_entries = 0;
+    bool go_on = x < x1;
+    if (go_on) {
+      if (x >= (long long)(cur.have + cur.grp) * mult) {
+        next.have += cur.grp;
+        do {
+          if (++next.su >= supers) break;
+          next.grp = __builtin_amdgcn_readfirstlane(groups_of(a, next.su));
+        } while (next.grp == 0);
+        go_on = next.su < supers;
+      }
+      if (go_on) {
+        fill(next);
+        next_entries = entries_of(next, next.off * kGroup + wave * 32);
+      }
+    }
+    const int rows = cur.m * a.G, unit = cur.b * a.Hkv + cur.h, len = cur.len;
+    const bool whole = cur.take == cur.grp;
+    if (cur.off == 0 && tid == 0) {     // the workgroups that the head falls to, from this one on, for the joining launch
+      const int left = (int)(x1 - x), rest = cur.grp - cur.take;
+      ((int2*)(a.ws + a.plan.info))[unit] = make_int2((int)blockIdx.x, left > 0 ? 1 : 1 + (rest + per - 1) / per);
+    }
+    const float qk = a.scale * (FP8 && a.kscale ? a.kscale[unit] : 1.0f);
     int vis[MT];            // keys that the row sees
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-      const int row = t * 16 + n16, tok = row / a.G, hd = row - tok * a.G;
-      const bool in = row < rows;
-      vis[t] = in ? len - (m - 1 - tok) : len;
-      const __bf16* src = (const __bf16*)a.q + (long long)(t0 + (in ? tok : 0)) * a.q_stride + (h * a.G + (in ? hd : 0)) * D;
-#pragma unroll
-      for (int s = 0; s < S::kSteps; ++s) {
-        const int c = FP8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8;
-        bf16x8 w = *(const bf16x8*)(src + c);
-        if (!in) w = (bf16x8)(__bf16)0.0f;
-        q[t][s] = w;
-      }
+      const int row = t * 16 + n16, tok = row / a.G;
+      vis[t] = row < rows ? len - (cur.m - 1 - tok) : len;
     }
-    const float qk = a.scale * (FP8 && a.kscale ? a.kscale[b * a.Hkv + h] : 1.0f);
-
     f32x4 o[MT][S::kTiles];
     float mx[MT], l[MT];
 #pragma unroll
@@ -136,57 +243,10 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
 #pragma unroll
       for (int c = 0; c < S::kTiles; ++c) o[t][c] = (f32x4)0.0f;
     }
-
-    const int row_lo = off * kGroup, row_hi = min((off + take) * kGroup, len);
-    int row = row_lo + wave * 32;
-    // table entries of the wavefront's next 32 tiles, two per tile, one in each lane
-    int entries = 0, window = row;
-    auto load_window = [&](int from) {
-      const int r = from + (lane >> 1) * kGroup + (lane & 1) * 16;
-      entries = table_entry(a, b, r < len ? r : len - 1);
-      window = from;
-    };
-    uint4 kraw[2][FP8 ? S::kSteps / 2 : S::kSteps];
-    VPiece<D, FP8> vraw[8][S::kLoads];
-    long long base[2];
-    int lim[2];
-    auto place = [&](int at) {      // the two halves of the tile at row `at`: where they start, and their last row
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int r = at + t * 16 < len ? at + t * 16 : at;
-        const int e = __builtin_amdgcn_readlane(entries, (at - window) / kGroup * 2 + (r != at ? 1 : 0));
-        base[t] = row_base(a, b, h, r, e) * S::kBytes;
-        lim[t] = len - 1 - r < 15 ? len - 1 - r : 15;
-      }
-    };
-    auto load_k = [&]() {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const char* p = (const char*)a.k + base[t];
-        const int at = (n16 < lim[t] ? n16 : lim[t]) * S::kBytes + g * 16;
-#pragma unroll
-        for (int s = 0; s < (FP8 ? S::kSteps / 2 : S::kSteps); ++s) kraw[t][s] = *(const uint4*)(p + at + s * 64);
-      }
-    };
-    auto load_v = [&]() {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const char* p = (const char*)a.v + base[j >> 2];
-        const int r = 4 * g + (j & 3), last = lim[j >> 2];
-        const int at = (r < last ? r : last) * S::kBytes + n16 * (S::kCpl * (FP8 ? 1 : 2));
-#pragma unroll
-        for (int u = 0; u < S::kLoads; ++u)
-          vraw[j][u] = *(const VPiece<D, FP8>*)(p + at + u * (16 * S::kCpl * (FP8 ? 1 : 2)));
-      }
-    };
-    if (row < row_hi) {
-      load_window(row);
-      place(row);
-      load_k();
-      load_v();
-    }
+    const int row_hi = min((cur.off + cur.take) * kGroup, len);
+    int row = cur.off * kGroup + wave * 32;
     while (row < row_hi) {
-      const int next = row + kGroup;
+      const int following = row + kGroup;
       // ---- S^T: 32 keys x 16 rows
       f32x4 s[MT][2];
 #pragma unroll
@@ -195,28 +255,33 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
       for (int c = 0; c < S::kSteps; ++c)
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          uint4 w;
+          bf16x8 w;
           if constexpr (FP8) {
-            const uint4 p = kraw[t][c >> 1];
-            w = c & 1 ? widen_fp8(make_uint2(p.z, p.w)) : widen_fp8(make_uint2(p.x, p.y));
+            const u32x4 p = kraw[t][c >> 1];
+            w = __builtin_bit_cast(bf16x8, c & 1 ? widen_fp8(make_uint2(p[2], p[3])) : widen_fp8(make_uint2(p[0], p[1])));
           } else {
-            w = kraw[t][c];
+            w = __builtin_bit_cast(bf16x8, kraw[t][c]);
           }
 #pragma unroll
           for (int i = 0; i < MT; ++i)
-            s[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), q[i][c], s[i][t], 0, 0, 0);
+            s[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, q[i][c]), s[i][t], 0, 0, 0);
         }
-      const bool more = next < row_hi;
+      const bool more = following < row_hi;
       if (more) {
-        if (next - window >= 32 * kGroup) load_window(next);
-        place(next);
+        if (following - window >= 32 * kGroup) {
+          entries = entries_of(cur, following);
+          window = following;
+        }
+        place(cur, following);
         load_k();
       }
       __builtin_amdgcn_sched_barrier(0);
       // ---- weights.  The maximum that they are taken against moves only when a row's passes it by more than 2^8: their sum and
       // the weighted values stay far from either end of fp32 then, and the division at the end takes the factor out again.
-      const bool ragged = row + 32 > len - (m - 1);
-      uint32_t p[MT][4];
+      // A weight reaches the second product as two bf16 numbers, which together are as good as fp32 next to the values' eight
+      // bits: the matrix cores have time for it here.
+      const bool ragged = row + 32 > len - (cur.m - 1);
+      uint32_t p[MT][4], plo[MT][4];
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
         s[t][0] *= qk;
@@ -241,6 +306,7 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
           const float lo = pow2(s[t][i >> 1][(i & 1) * 2] - from), hi = pow2(s[t][i >> 1][(i & 1) * 2 + 1] - from);
           l[t] += lo + hi;
           p[t][i] = pack_bf16(lo, hi);
+          plo[t][i] = pack_bf16(lo - __uint_as_float(p[t][i] << 16), hi - __uint_as_float(p[t][i] & 0xffff0000u));
         }
       }
       // ---- O^T
@@ -261,194 +327,146 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
           const uint4 v = make_uint4(__builtin_amdgcn_perm(w[1][c >> 1], w[0][c >> 1], sel), __builtin_amdgcn_perm(w[3][c >> 1], w[2][c >> 1], sel),
                                      __builtin_amdgcn_perm(w[5][c >> 1], w[4][c >> 1], sel), __builtin_amdgcn_perm(w[7][c >> 1], w[6][c >> 1], sel));
 #pragma unroll
-          for (int t = 0; t < MT; ++t)
-            o[t][u * S::kCpl + c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, make_uint4(p[t][0], p[t][1], p[t][2], p[t][3])),
-                o[t][u * S::kCpl + c], 0, 0, 0);
+          for (int t = 0; t < MT; ++t) {
+            f32x4& acc = o[t][u * S::kCpl + c];
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, make_uint4(plo[t][0], plo[t][1], plo[t][2], plo[t][3])), acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, make_uint4(p[t][0], p[t][1], p[t][2], p[t][3])), acc, 0, 0, 0);
+          }
         }
       }
       if (more) load_v();
       __builtin_amdgcn_sched_barrier(0);
-      row = next;
+      row = following;
     }
+    // the next part's first tile is on its way while this one's results are put together
+    if (go_on) {
+      entries = next_entries;
+      begin(next);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 
-    // ---- the four wavefronts' results: one maximum per row, then sums over wavefronts 2 + 0 and 3 + 1, then the two
+    // ---- the four wavefronts' results through LDS, once; then every thread makes four channels of a row of them
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       l[t] = sum_xor16(sum_halves(l[t]));
-      if (g == 0) {
-        pass_ml[wave][0][t * 16 + n16] = mx[t];
-        pass_ml[wave][1][t * 16 + n16] = l[t];
-      }
-    }
-    __syncthreads();
-    float top[MT], sum[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
       const int r = t * 16 + n16;
-      top[t] = fmaxf(fmaxf(pass_ml[0][0][r], pass_ml[1][0][r]), fmaxf(pass_ml[2][0][r], pass_ml[3][0][r]));
-      const float from = top[t] == -__builtin_inff() ? 0.0f : top[t];
-      sum[t] = 0.0f;
+      if (r < rows) {
+        if (g == 0) pass_ml[wave * kM + r] = make_float2(mx[t], l[t]);
+        float* dst = pass_o + (wave * kM + r) * kPitch;
+        // channel u 16 cpl + (4 g + r) cpl + c is o[u cpl + c][r]
 #pragma unroll
-      for (int w = 0; w < 4; ++w) sum[t] += pass_ml[w][1][r] * pow2(pass_ml[w][0][r] - from);
-      const float f = pow2(mx[t] - from);
+        for (int u = 0; u < S::kLoads; ++u)
 #pragma unroll
-      for (int c = 0; c < S::kTiles; ++c) o[t][c] *= f;
-    }
-    if (wave >= 2)
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int c = 0; c < S::kTiles; ++c)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) pass_o[wave - 2][(t * S::kTiles + c) * 4 + r][lane] = o[t][c][r];
-    __syncthreads();
-    if (wave < 2)
-#pragma unroll
-      for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int c = 0; c < S::kTiles; ++c)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            o[t][c][r] += pass_o[wave][(t * S::kTiles + c) * 4 + r][lane];
-            if (wave == 1) pass_o[1][(t * S::kTiles + c) * 4 + r][lane] = o[t][c][r];
-          }
-    __syncthreads();
-    if (wave == 0) {
-#pragma unroll
-      for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int c = 0; c < S::kTiles; ++c)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) o[t][c][r] += pass_o[1][(t * S::kTiles + c) * 4 + r][lane];
-      const int unit = b * a.Hkv + h;
-      const bool whole = take == grp;
-      if (off == 0 && lane == 0) {      // the pieces of this head: the workgroups from this one on, for the joining launch
-        const long long end = x + grp - 1;
-        ((int2*)(a.ws + a.plan.info))[unit] = make_int2((int)blockIdx.x, (int)(end / per - blockIdx.x) + 1);
+            for (int c = 0; c < S::kCpl; c += 4) {
+              const f32x4* w = &o[t][u * S::kCpl + c];
+              *(float4*)(dst + u * 16 * S::kCpl + (4 * g + i) * S::kCpl + c) = make_float4(w[0][i], w[1][i], w[2][i], w[3][i]);
+            }
       }
-      // channel u 16 cpl + (4 g + r) cpl + c of row n16 is o[u cpl + c][r]
+    }
+    __syncthreads();
+    // slot 0 of a workgroup: a head that began in front of it; slot 1: one that goes on behind it
+    const long long slot = ((long long)blockIdx.x * 2 + (cur.off == 0 ? 1 : 0)) * kM;
+    float* part_o = (float*)(a.ws + a.plan.part_o) + slot * D;
+    float2* part_ml = (float2*)(a.ws + a.plan.part_ml) + slot;
+    constexpr int kLanes = D / 4;
+    const int c4 = tid % kLanes * 4;
+    for (int r = tid / kLanes; r < rows; r += 256 / kLanes) {
+      float2 ml[4];
+#pragma unroll
+      for (int w = 0; w < 4; ++w) ml[w] = pass_ml[w * kM + r];
+      const float top = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x)), from = top == -__builtin_inff() ? 0.0f : top;
+      float4 acc = make_float4(0, 0, 0, 0);
+      float sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = pow2(ml[w].x - from);
+        const float4 y = *(const float4*)(pass_o + (w * kM + r) * kPitch + c4);
+        sum += ml[w].y * f;
+        acc.x += y.x * f; acc.y += y.y * f; acc.z += y.z * f; acc.w += y.w * f;
+      }
       if (whole) {
-        const float vs = FP8 && a.vscale ? a.vscale[unit] : 1.0f;
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          const int rw = t * 16 + n16, tok = rw / a.G, hd = rw - tok * a.G;
-          if (rw < rows) {
-            const long long at = (long long)(t0 + tok) * a.Hq + h * a.G + hd;
-            const float f = vs / sum[t];
-            __bf16* dst = (__bf16*)a.out + at * D;
-#pragma unroll
-            for (int u = 0; u < S::kLoads; ++u)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const int c0 = u * 16 * S::kCpl + (4 * g + r) * S::kCpl;
-#pragma unroll
-                for (int c = 0; c < S::kCpl; c += 4) {
-                  const f32x4* w = &o[t][u * S::kCpl + c];
-                  *(uint2*)(dst + c0 + c) = sum[t] > 0.0f || sum[t] != sum[t]
-                      ? make_uint2(pack_bf16(w[0][r] * f, w[1][r] * f), pack_bf16(w[2][r] * f, w[3][r] * f)) : make_uint2(0u, 0u);
-                }
-              }
-            if (a.lse && g == 0) a.lse[at] = natural_lse(top[t], sum[t]);
-          }
-        }
+        write_row<D>(a, cur.t0, cur.h, unit, r, c4, top, sum, acc);
       } else {
-        // slot 0 of a workgroup: a head that began in front of it; slot 1: one that goes on behind it
-        const long long slot = ((long long)blockIdx.x * 2 + (off == 0 ? 1 : 0)) * kM;
-        float* po = (float*)(a.ws + a.plan.part_o) + slot * D;
-        float2* ml = (float2*)(a.ws + a.plan.part_ml) + slot;
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          const int rw = t * 16 + n16;
-          if (rw < rows) {
-#pragma unroll
-            for (int u = 0; u < S::kLoads; ++u)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const int c0 = u * 16 * S::kCpl + (4 * g + r) * S::kCpl;
-#pragma unroll
-                for (int c = 0; c < S::kCpl; c += 4) {
-                  const f32x4* w = &o[t][u * S::kCpl + c];
-                  *(float4*)(po + (long long)rw * D + c0 + c) = make_float4(w[0][r], w[1][r], w[2][r], w[3][r]);
-                }
-              }
-            if (g == 0) ml[rw] = make_float2(top[t], sum[t]);
-          }
-        }
+        *(float4*)(part_o + (long long)r * D + c4) = acc;
+        if (c4 == 0) part_ml[r] = make_float2(top, sum);
       }
     }
-    x += take;
-    if (x < x1) {
-      __syncthreads();      // the next head's results go through the same LDS
-      if (x >= (long long)(have + grp) * mult) {
-        have += grp;
-        do {
-          if (++su >= supers) return;
-          grp = __builtin_amdgcn_readfirstlane(groups_of(a, su));
-        } while (grp == 0);
-      }
-    }
+    if (!go_on) return;
+    __syncthreads();      // the next part's results go through the same LDS
+    cur = next;
   }
 }
 
-// The heads that fell into several shares: one workgroup per (head, row), four pieces at a time.
+// The heads that fell into several shares: a workgroup per (head, row), 256 / (D / 4) pieces at a time and eight rounds of them
+// requested together, so that what takes the time is one round trip for where the pieces are and one for them.
 template <int D>
 __global__ __launch_bounds__(256) void k_attend_rows_join(AttendArgs a) {
-  constexpr int kLanes = D / 4, kWays = 256 / kLanes;
+  constexpr int kLanes = D / 4, kWays = 256 / kLanes, kRounds = 8;
   __shared__ float4 pass[kWays][kLanes];
-  __shared__ float pass_l[kWays];
+  __shared__ float2 pass_ml[kWays];
   const int unit = blockIdx.x / a.short_rows, row = blockIdx.x - unit * a.short_rows;
   const int b = unit / a.Hkv, h = unit - b * a.Hkv;
+  const int2 info = ((const int2*)(a.ws + a.plan.info))[unit];
   const int t0 = first_token(a, b), m = first_token(a, b + 1) - t0;
   if (m < 1 || m * a.G > a.short_rows || row >= m * a.G) return;
-  const int2 info = ((const int2*)(a.ws + a.plan.info))[unit];
   const int pieces = info.y;
   if (pieces <= 1) return;
-  const int way = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
-  const float* po = (const float*)(a.ws + a.plan.part_o);
-  const float2* ml = (const float2*)(a.ws + a.plan.part_ml);
-  auto slot = [&](int i) { return ((long long)(info.x + i) * 2 + (i == 0 ? 1 : 0)) * a.plan.piece_rows + row; };
-  float top = -__builtin_inff();
-  for (int i = threadIdx.x & 63; i < pieces; i += 64) top = fmaxf(top, ml[slot(i)].x);
-#pragma unroll
-  for (int i = 1; i < 64; i *= 2) top = fmaxf(top, __shfl_xor(top, i));
-  const float from = top == -__builtin_inff() ? 0.0f : top;
+  const int way = threadIdx.x / kLanes, c4 = threadIdx.x % kLanes * 4;
+  const float* po = (const float*)(a.ws + a.plan.part_o) + c4;
+  const float2* part_ml = (const float2*)(a.ws + a.plan.part_ml);
+  float top = -__builtin_inff(), sum = 0.0f;
   float4 acc = make_float4(0, 0, 0, 0);
-  float sum = 0.0f;
-  for (int i = way; i < pieces; i += kWays) {
-    const long long s = slot(i);
-    const float2 w = ml[s];
-    const float4 x = *(const float4*)(po + s * D + c * 4);
-    const float f = pow2(w.x - from);
-    sum += w.y * f;
-    acc.x += x.x * f; acc.y += x.y * f; acc.z += x.z * f; acc.w += x.w * f;
+  auto take = [&](float2 ml, float4 y) {
+    const float t = fmaxf(top, ml.x), from = t == -__builtin_inff() ? 0.0f : t;
+    const float f = pow2(top - from), n = pow2(ml.x - from);
+    top = t;
+    sum = sum * f + ml.y * n;
+    acc.x = acc.x * f + y.x * n; acc.y = acc.y * f + y.y * n; acc.z = acc.z * f + y.z * n; acc.w = acc.w * f + y.w * n;
+  };
+  for (int i0 = way; i0 < pieces; i0 += kWays * kRounds) {
+    float2 ml[kRounds];
+    float4 y[kRounds];
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+      const int i = i0 + k * kWays < pieces ? i0 + k * kWays : i0;
+      const long long slot = ((long long)(info.x + i) * 2 + (i == 0 ? 1 : 0)) * a.plan.piece_rows + row;
+      ml[k] = part_ml[slot];
+      y[k] = *(const float4*)(po + slot * D);
+    }
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k)
+      if (i0 + k * kWays < pieces) take(ml[k], y[k]);
   }
-  pass[way][c] = acc;
-  if (c == 0) pass_l[way] = sum;
+  if (c4 == 0) pass_ml[way] = make_float2(top, sum);
+  pass[way][c4 / 4] = acc;
   __syncthreads();
   if (way != 0) return;
-  for (int w = 1; w < kWays; ++w) {
-    const float4 x = pass[w][c];
-    acc.x += x.x; acc.y += x.y; acc.z += x.z; acc.w += x.w;
-    sum += pass_l[w];
-  }
-  const int tok = row / a.G, hd = row - tok * a.G;
-  const long long at = (long long)(t0 + tok) * a.Hq + h * a.G + hd;
-  const float f = (a.vscale ? a.vscale[unit] : 1.0f) / sum;
-  const bool any = sum > 0.0f || sum != sum;
-  *(uint2*)((__bf16*)a.out + at * D + c * 4) =
-      any ? make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f)) : make_uint2(0u, 0u);
-  if (a.lse && c == 0) a.lse[at] = natural_lse(top, sum);
+#pragma unroll
+  for (int w = 1; w < kWays; ++w) take(pass_ml[w], pass[w][c4 / 4]);
+  write_row<D>(a, t0, h, unit, row, c4, top, sum, acc);
 }
 
-template <int D, bool FP8>
-static hipError_t rows_of_type(const AttendArgs& a, hipStream_t st) {
-  if (D == 256 || a.plan.mt == 1) k_attend_rows<D, FP8, 1><<<a.plan.shares, 256, 0, st>>>(a);
-  else if constexpr (D < 256) k_attend_rows<D, FP8, 2><<<a.plan.shares, 256, 0, st>>>(a);
-  hipError_t e = hipGetLastError();
+template <int D, bool FP8, int MT>
+static hipError_t rows_of_height(const AttendArgs& a, hipStream_t st) {
+  static LdsOptIn opt;
+  const size_t bytes = rows_lds_floats<D, MT>() * sizeof(float);
+  const hipError_t e = opt.ensure((const void*)k_attend_rows<D, FP8, MT>, bytes);
   if (e != hipSuccess) return e;
+  k_attend_rows<D, FP8, MT><<<a.plan.shares, 256, bytes, st>>>(a);
+  const hipError_t e2 = hipGetLastError();
+  if (e2 != hipSuccess) return e2;
   k_attend_rows_join<D><<<a.B * a.Hkv * a.short_rows, 256, 0, st>>>(a);
   return hipGetLastError();
+}
+template <int D, bool FP8>
+static hipError_t rows_of_type(const AttendArgs& a, hipStream_t st) {
+  if constexpr (D < 256)
+    if (a.plan.mt == 2) return rows_of_height<D, FP8, 2>(a, st);
+  return rows_of_height<D, FP8, 1>(a, st);
 }
 
 hipError_t launch_attend_rows(const AttendArgs& a, const Dims& d, hipStream_t st) {
