@@ -10,25 +10,64 @@ namespace ea {
 
 namespace {
 
-constexpr int kM = kAttendTileRows;
 using s16x4 = short __attribute__((ext_vector_type(4)));
 
-// LDS rows: K's start four banks apart (16-byte reads of eight rows at a time), V's sixteen (transposing reads of four rows,
-// 64 bytes of each)
-template <int D> constexpr int k_pitch() { return D * 2 + 16; }
-template <int D> constexpr int v_pitch() { return D * 2 + 64; }
+// A tile in LDS.  bf16 rows come straight from memory, 1 KiB per wavefront and load, so they stand without gaps; what would make
+// rows meet in the banks is taken out by their order in 16-byte pieces: piece c of a row stands at c ^ (row & 7) in K (16-byte reads
+// of eight rows at a time) and at c ^ 4 (row & 3) in V (transposing reads of 64 bytes of four rows; d = 64: two rows to all banks).
+// 8-bit rows pass through registers and are widened there; their K rows are four banks apart, V's sixteen.
+template <int D, bool FP8> constexpr int k_pitch() { return D * 2 + (FP8 ? 16 : 0); }
+template <int D, bool FP8> constexpr int v_pitch() { return D * 2 + (FP8 ? 64 : 0); }
 template <int D> constexpr int tile_keys() { return D == 256 ? 32 : 64; }
-template <int D> constexpr int buffer_bytes() { return tile_keys<D>() * (k_pitch<D>() + v_pitch<D>()); }
+template <int D, bool FP8> constexpr int buffer_bytes() { return tile_keys<D>() * (k_pitch<D, FP8>() + v_pitch<D, FP8>()); }
+template <int D> __device__ __forceinline__ int k_piece(int row) { return row & 7; }
+template <int D> __device__ __forceinline__ int v_piece(int row) { return D == 64 ? (row >> 1 & 1) * 4 : (row & 3) * 4; }
+
+// 16 bytes per lane from base + at to LDS address `to` and on, lanes in order.  Nothing waits for it but the s_waitcnt in front of
+// the barrier behind which the tile is read; the compiler, told of such a load, would wait at the next read of any LDS.  (m0 is
+// nobody else's here: LDS instructions of this chip do not read it.)
+__device__ __forceinline__ void to_lds(uint32_t to, const void* base, uint32_t at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(to), "v"(at), "s"(base) : "memory");
+}
+
+// The order in which a block's instructions are issued: operands from LDS a few products ahead (left to itself the compiler
+// reads one, waits for it, multiplies), and the next weights between the products.
+template <int PRODUCTS, int kAhead>
+__device__ __forceinline__ void order_products() {
+  __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+  for (int i = 0; i < PRODUCTS - kAhead; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+  __builtin_amdgcn_sched_barrier(0);
+}
+// 16 keys: their products, each with two reads for the next 16 keys and a share of the next weights behind it
+template <int TILES>
+__device__ __forceinline__ void order_weighted() {
+#pragma unroll
+  for (int i = 0; i < TILES; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, (16 + TILES - 1) / TILES, 0);
+    __builtin_amdgcn_sched_group_barrier(0x400, (8 + TILES - 1) / TILES, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
 
 }  // namespace
 
-template <int D, bool FP8>
-__global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_tile(AttendArgs a) {
+template <int D, bool FP8, int NW>
+__global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_attend_tile(AttendArgs a) {
+  constexpr int kM = NW * 32;
   constexpr int kN = tile_keys<D>(), kKt = kN / 32, kSteps = D / 16, kCt = D / 32;
   constexpr int kRowBytes = D * (FP8 ? 1 : 2);
   constexpr int kPer = 1024 / kRowBytes;                 // rows that a wavefront's load covers
-  constexpr int kPasses = kN / (4 * kPer);               // of the workgroup's loads over a tile
+  constexpr int kPasses = kN / (NW * kPer);               // of the workgroup's loads over a tile
   constexpr int kChunks = kRowBytes / 16;
+  constexpr int kKPitch = k_pitch<D, FP8>(), kVPitch = v_pitch<D, FP8>(), kBuffer = buffer_bytes<D, FP8>();
+  constexpr bool kOrdered = D < 256;                     // at d = 256 the registers are all taken without an order
   extern __shared__ char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n32 = lane & 31, hi = lane >> 5;
@@ -76,45 +115,58 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_tile(AttendA
   }
   const float qk = a.scale * (FP8 && a.kscale ? a.kscale[unit] : 1.0f);
 
-  // ---- loads of a tile: pass i of wavefront w covers rows (4 i + w) kPer ..
+  // ---- loads of a tile: pass i of wavefront w covers rows (NW i + w) kPer ..
   int entries = 0, window = key_lo;
   auto load_window = [&](int from) {
     const int r = from + lane * 16;
     entries = table_entry(a, b, r < len ? r : len > 0 ? len - 1 : 0);
     window = from;
   };
-  u32x4 kraw[kPasses], vraw[kPasses];
-  auto request = [&](int at) {
+  u32x4 kraw[FP8 ? kPasses : 1], vraw[FP8 ? kPasses : 1];
+  const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const int my_row = wave * kPer + lane / kChunks, my_piece = lane % kChunks;      // of the tile, in pass 0; the others are whole eights behind
+  const int k_off = (FP8 ? my_piece : my_piece ^ k_piece<D>(my_row)) * 16, v_off = (FP8 ? my_piece : my_piece ^ v_piece<D>(my_row)) * 16;
+  auto request = [&](int at, int buf) {
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
-      const int r0 = at + (4 * i + wave) * kPer, sub = r0 & ~15;
+      const int r0 = at + (NW * i + wave) * kPer, sub = r0 & ~15;
       const int from = sub < len ? sub : (len - 1) & ~15;
       const int e = __builtin_amdgcn_readlane(entries, (from - window) >> 4);
-      int r = r0 - sub + lane / kChunks;
-      r = min(r, len - 1 - from);
+      const int r = min(r0 - sub + lane / kChunks, len - 1 - from);
       const long long at_byte = row_base(a, b, h, from, e) * kRowBytes;
-      const int off = r * kRowBytes + lane % kChunks * 16;
-      kraw[i] = *(const u32x4*)((const char*)a.k + at_byte + off);
-      vraw[i] = *(const u32x4*)((const char*)a.v + at_byte + off);
+      if constexpr (FP8) {
+        kraw[i] = *(const u32x4*)((const char*)a.k + at_byte + (r * kRowBytes + k_off));
+        vraw[i] = *(const u32x4*)((const char*)a.v + at_byte + (r * kRowBytes + v_off));
+      } else {
+        const uint32_t to = lds_at + buf * kBuffer + (NW * i + wave) * 1024;
+        to_lds(to, (const char*)a.k + at_byte, r * kRowBytes + k_off);
+        to_lds(to + kN * kKPitch, (const char*)a.v + at_byte, r * kRowBytes + v_off);
+      }
     }
   };
-  auto stage = [&](int at, char* buf) {
+  // 8-bit rows: from registers to LDS, those behind the last one as zeros, which weigh nothing whatever stood there
+  auto stage = [&](int at, int buf) {
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-      const int r = (4 * i + wave) * kPer + lane / kChunks, c = lane % kChunks;
-      const uint32_t keep = at + r >= key_hi ? 0u : ~0u;       // rows behind the last one weigh nothing, whatever they hold
+    for (int i = 0; i < (FP8 ? kPasses : 0); ++i) {
+      const int r = (NW * i) * kPer + my_row;
+      const uint32_t keep = at + r >= key_hi ? 0u : ~0u;
       const u32x4 v = vraw[i] & keep;
-      char* kd = buf + r * k_pitch<D>() + c * (FP8 ? 32 : 16);
-      char* vd = buf + kN * k_pitch<D>() + r * v_pitch<D>() + c * (FP8 ? 32 : 16);
-      if constexpr (FP8) {
-        *(uint4*)kd = widen_fp8(make_uint2(kraw[i].x, kraw[i].y));
-        *(uint4*)(kd + 16) = widen_fp8(make_uint2(kraw[i].z, kraw[i].w));
-        *(uint4*)vd = widen_fp8(make_uint2(v.x, v.y));
-        *(uint4*)(vd + 16) = widen_fp8(make_uint2(v.z, v.w));
-      } else {
-        *(u32x4*)kd = kraw[i];
-        *(u32x4*)vd = v;
-      }
+      char* kd = lds + buf * kBuffer + r * kKPitch + my_piece * 32;
+      char* vd = lds + buf * kBuffer + kN * kKPitch + r * kVPitch + my_piece * 32;
+      *(uint4*)kd = widen_fp8(make_uint2(kraw[i].x, kraw[i].y));
+      *(uint4*)(kd + 16) = widen_fp8(make_uint2(kraw[i].z, kraw[i].w));
+      *(uint4*)vd = widen_fp8(make_uint2(v.x, v.y));
+      *(uint4*)(vd + 16) = widen_fp8(make_uint2(v.z, v.w));
+    }
+  };
+  // bf16 rows: all of the tile has arrived; the values behind the last row become zeros
+  auto arrived = [&](int at, int buf) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (at + kN > key_hi) {
+      u32x4* v = (u32x4*)(lds + buf * kBuffer + kN * kKPitch);
+      for (int i = (key_hi - at) * (D / 8) + (int)threadIdx.x; i < kN * (D / 8); i += NW * 64) v[i] = (u32x4)0u;
+      __syncthreads();
     }
   };
 
@@ -124,25 +176,58 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_tile(AttendA
   float mx = -__builtin_inff(), l = 0.0f;
   if (key_lo < key_hi) {
     load_window(key_lo);
-    request(key_lo);
-    stage(key_lo, lds);
-    if (key_lo + kN < key_hi) request(key_lo + kN);
-    __syncthreads();
+    request(key_lo, 0);
+    if constexpr (FP8) {
+      stage(key_lo, 0);
+      if (key_lo + kN < key_hi) request(key_lo + kN, 1);
+      __syncthreads();
+    } else {
+      arrived(key_lo, 0);
+    }
   }
+  // where the lane's operands stand: K's row n32, pieces 2 c + hi; V's rows 4 hi + .., 64-byte stretches c
+  const int v_row = 4 * hi + ((lane & 15) >> 2);
+  constexpr int kKWays = FP8 ? 1 : 4, kVWays = FP8 ? 1 : D == 64 ? 2 : 4;
+  uint32_t k_at[kKWays], v_at[kVWays];
+#pragma unroll
+  for (int c = 0; c < kKWays; ++c) k_at[c] = n32 * kKPitch + ((2 * c + hi) ^ (FP8 ? 0 : k_piece<D>(n32))) * 16;
+#pragma unroll
+  for (int c = 0; c < kVWays; ++c)
+    v_at[c] = kN * kKPitch + v_row * kVPitch + ((c * 4) ^ (FP8 ? 0 : v_piece<D>(v_row))) * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
   int buf = 0;
   for (int key = key_lo; key < key_hi; key += kN, buf ^= 1) {
-    const char* kt = lds + buf * buffer_bytes<D>();
-    const char* vt = kt + kN * k_pitch<D>();
+    const char* kt = lds + buf * kBuffer;
+    const int next = key + kN;
+    if constexpr (!FP8)
+      if (next < key_hi) {
+        if (next - window >= 1024) load_window(next);
+        request(next, buf ^ 1);
+      }
     f32x16 s[kKt];
 #pragma unroll
     for (int t = 0; t < kKt; ++t) {
       s[t] = (f32x16)0.0f;
 #pragma unroll
       for (int c = 0; c < kSteps; ++c) {
-        const bf16x8 w = *(const bf16x8*)(kt + (t * 32 + n32) * k_pitch<D>() + c * 32 + hi * 16);
+        const bf16x8 w = *(const bf16x8*)(kt + k_at[c % kKWays] + t * 32 * kKPitch + c / kKWays * kKWays * 32);
         s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[c], s[t], 0, 0, 0);
       }
     }
+    if constexpr (kOrdered) order_products<kKt * kSteps, 6>();
+    // V^T's operands, kRing of them ahead of the products.  Lanes 16 j .. of a group of 16 read four rows of 16 channels, and get one
+    // channel of the four rows each
+    constexpr int kRing = D == 256 ? 1 : 4, kOperands = kKt * 2 * kCt;
+    bf16x8 vf[kRing];
+    auto read_v = [&](int f) {
+      const int c = f % kCt;
+      const char* at = kt + v_at[c % kVWays] + (f / kCt) * 16 * kVPitch + c / kVWays * kVWays * 64;
+      using lds_s16x4 = __attribute__((address_space(3))) s16x4;
+      const s16x4 w0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+      const s16x4 w1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * kVPitch));
+      vf[f % kRing] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(w0, w1, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+#pragma unroll
+    for (int f = 0; f < kRing; ++f) read_v(f);
     // key of s[t][r]: t 32 + (r / 4) 8 + hi 4 + r % 4
     if constexpr (FP8)
 #pragma unroll
@@ -169,40 +254,42 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_tile(AttendA
       for (int c = 0; c < kCt; ++c) o[c] *= f;
     }
     const float from = mx == -__builtin_inff() ? 0.0f : mx;
-    uint32_t p[kKt][8];
+    // weights of 16 keys at a time, one block ahead of the products that take them
+    uint32_t p[kKt * 2][4];
+    auto weigh = [&](int kb) {
 #pragma unroll
-    for (int t = 0; t < kKt; ++t)
-#pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const float x = FP8 ? pow2(s[t][2 * r] - from) : pow2(fmaf(s[t][2 * r], qk, -from));
-        const float y = FP8 ? pow2(s[t][2 * r + 1] - from) : pow2(fmaf(s[t][2 * r + 1], qk, -from));
+      for (int r = 0; r < 4; ++r) {
+        const float s0 = s[kb >> 1][(kb & 1) * 8 + 2 * r], s1 = s[kb >> 1][(kb & 1) * 8 + 2 * r + 1];
+        const float x = FP8 ? pow2(s0 - from) : pow2(fmaf(s0, qk, -from)), y = FP8 ? pow2(s1 - from) : pow2(fmaf(s1, qk, -from));
         l += x + y;
-        p[t][r] = pack_bf16(x, y);
+        p[kb][r] = pack_bf16(x, y);
       }
+    };
+    weigh(0);
+    if constexpr (kOrdered) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int kb = 0; kb < kKt * 2; ++kb) {
-      const uint32_t* pw = &p[kb >> 1][(kb & 1) * 4];
-      const bf16x8 pv = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+      const bf16x8 pv = __builtin_bit_cast(bf16x8, make_uint4(p[kb][0], p[kb][1], p[kb][2], p[kb][3]));
 #pragma unroll
       for (int c = 0; c < kCt; ++c) {
-        // lanes 16 j .. of a group of 16 read four rows of 16 channels, and get one channel of the four rows each
-        const int i = lane & 15, half = (lane >> 4) & 1;
-        const char* at = vt + (kb * 16 + 4 * hi + (i >> 2)) * v_pitch<D>() + (c * 32 + half * 16 + (i & 3) * 4) * 2;
-        using lds_s16x4 = __attribute__((address_space(3))) s16x4;
-        const s16x4 w0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at));
-        const s16x4 w1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * v_pitch<D>()));
-        const uint2 u0 = __builtin_bit_cast(uint2, w0), u1 = __builtin_bit_cast(uint2, w1);
-        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(u0.x, u0.y, u1.x, u1.y)), pv, o[c], 0, 0, 0);
+        const int f = kb * kCt + c;
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f % kRing], pv, o[c], 0, 0, 0);
+        if (f + kRing < kOperands) read_v(f + kRing);
       }
+      if (kb + 1 < kKt * 2) weigh(kb + 1);
+      if constexpr (kOrdered) order_weighted<kCt>();
     }
-    const int next = key + kN;
     if (next < key_hi) {
-      stage(next, lds + (buf ^ 1) * buffer_bytes<D>());
-      if (next + kN < key_hi) {
-        if (next + kN - window >= 1024) load_window(next + kN);
-        request(next + kN);
+      if constexpr (FP8) {
+        stage(next, buf ^ 1);
+        if (next + kN < key_hi) {
+          if (next + kN - window >= 1024) load_window(next + kN);
+          request(next + kN, buf);
+        }
+        __syncthreads();
+      } else {
+        arrived(next, buf ^ 1);
       }
-      __syncthreads();
     }
   }
 
@@ -286,15 +373,19 @@ hipError_t launch_attend_join(const AttendArgs& a, bool f32, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int D, bool FP8>
-static hipError_t tile_of_type(const AttendArgs& a, hipStream_t st) {
+template <int D, bool FP8, int NW>
+static hipError_t tile_of_width(const AttendArgs& a, hipStream_t st) {
   static LdsOptIn opt;
-  hipError_t e = opt.ensure((const void*)k_attend_tile<D, FP8>, 2 * buffer_bytes<D>());
+  hipError_t e = opt.ensure((const void*)k_attend_tile<D, FP8, NW>, 2 * buffer_bytes<D, FP8>());
   if (e != hipSuccess) return e;
-  k_attend_tile<D, FP8><<<(unsigned)(a.plan.tiles * a.plan.nsplit * a.Hkv), 256, 2 * buffer_bytes<D>(), st>>>(a);
+  k_attend_tile<D, FP8, NW><<<(unsigned)(a.plan.tiles * a.plan.nsplit * a.Hkv), NW * 64, 2 * buffer_bytes<D, FP8>(), st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess || a.plan.nsplit == 1) return e;
   return launch_attend_join(a, false, st);
+}
+template <int D, bool FP8>
+static hipError_t tile_of_type(const AttendArgs& a, hipStream_t st) {
+  return a.plan.tile_rows == 256 ? tile_of_width<D, FP8, 8>(a, st) : tile_of_width<D, FP8, 4>(a, st);
 }
 
 hipError_t launch_attend_tile(const AttendArgs& a, const Dims& d, hipStream_t st) {

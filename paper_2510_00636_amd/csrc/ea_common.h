@@ -56,7 +56,6 @@ struct PageMap {
 
 // Attention of a step's tokens: how a call is cut, and where its workspace holds what.
 constexpr int kAttendGroup = 128;       // keys of a group of the row kernel, whose workgroups take whole ones
-constexpr int kAttendTileRows = 128;    // (token, head) rows of a workgroup of the tile kernel
 constexpr int kAttendF32Rows = 16;      // and of the fp32 kernel
 constexpr int kAttendShares = 512;      // most workgroups of the row kernel
 constexpr int64_t kAttendMaxTokens = (int64_t)1 << 24;
@@ -66,6 +65,7 @@ struct AttendPlan {
   int short_rows;     // most (token, head) rows of a sequence that is the row kernel's
   int shares;         // its workgroups
   int piece_rows;     // rows reserved for a partial result
+  int tile_rows;      // (token, head) rows of a workgroup of the tile kernel
   int tiles;          // of the tile kernel, per KV head
   int nsplit, chunk;  // stretches of keys that workgroups of their own take there, and keys of each
   size_t info, part_o, part_ml, split_o, split_ml, total;

@@ -1,6 +1,7 @@
 // Host-only part of libea: argument validation, tiling plans, workspace layout, and the two
 // host helpers of the ABI.  Nothing here touches the GPU, so it is testable without one.
 #include <math.h>
+#include <stdlib.h>
 
 #include "ea_common.h"
 
@@ -343,7 +344,8 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   a.tile = f32 || most > a.piece_rows;
   a.shares = 2 * num_cu < kAttendShares ? 2 * num_cu : kAttendShares;
   a.nsplit = 1;
-  const int64_t unit_rows = f32 ? kAttendF32Rows : kAttendTileRows;
+  a.tile_rows = f32 ? kAttendF32Rows : most >= 256 && !getenv("EA_T4") ? 256 : 128;
+  const int64_t unit_rows = a.tile_rows;
   // sequence b's tiles start at floor(first token G / unit_rows) + b
   a.tiles = (int)(n_tokens * d.G / unit_rows + d.B);
   // enough workgroups for two per CU: keys in stretches where the tiles are few
