@@ -82,6 +82,12 @@ __device__ __forceinline__ int wave_prefix(int x) {
   x = dpp_add_int<0x142, 0xa>(x);   // the last lane of rows 0 and 2 to rows 1 and 3
   return dpp_add_int<0x143, 0xc>(x);
 }
+// largest x of the wavefront, of either sign, in every lane
+__device__ __forceinline__ float wave_max_any(float x) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
+  return x;
+}
 __device__ __forceinline__ int last_lane(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
 __device__ __forceinline__ float max_xor32(float x) {
@@ -91,6 +97,98 @@ __device__ __forceinline__ float max_xor32(float x) {
 __device__ __forceinline__ float max_xor16(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// ---- Stretches: which piece a workgroup takes.
+// A sequence's (token, head) rows come in tiles of ROWS; tiles of few, long sequences are cut along the keys as well, so that the
+// pieces fill the chip's slots evenly.  How finely follows from the lengths on the device: every lane looks at one way to cut the
+// longest (and with it the others, into pieces of at most as many keys), the rounds of pieces that it takes times what a piece takes,
+// and the cheapest is taken.  A piece costs kPieceSteps steps of 64 keys besides its own (its queries, its first tile, its results),
+// cutting at all kJoinSteps (the launch that joins).  All workgroups come to the same result, and the first of a sequence writes
+// down for the joining launch how it was cut.
+constexpr int kPieceSteps = 3, kJoinSteps = 4, kLeastSteps = 4;
+struct Piece {
+  int b, h, tile, split;        // tile < 0: none
+  int tiles, nsplit, chunk;     // of the sequence, and keys of a stretch
+  int t0, m;
+  bool first;
+};
+__device__ __forceinline__ int ceil_div(int x, int by) {      // x < 2^24, both sides exact in fp32
+  int k = (int)((float)(x + by - 1) * __builtin_amdgcn_rcpf((float)by));
+  if (k * by > x + by - 1) --k;
+  if ((k + 1) * by <= x + by - 1) ++k;
+  return k;
+}
+template <int ROWS>
+__device__ __forceinline__ Piece find_piece(const AttendArgs& a, int index) {
+  const int lane = threadIdx.x & 63;
+  auto look = [&](int b, int& tiles, int& steps) {
+    tiles = steps = 0;
+    if (b >= a.B) return;
+    const int rows = (first_token(a, b + 1) - first_token(a, b)) * a.G;
+    if (rows < 1 || (a.only_long && rows <= a.short_rows)) return;
+    tiles = (rows + ROWS - 1) / ROWS;
+    int len = rows_of(a, b, 0);
+    if (a.per_head)
+      for (int h = 1; h < a.Hkv; ++h) len = max(len, rows_of(a, b, h));
+    steps = len > 0 ? (len + 63) >> 6 : 1;
+  };
+  int tiles, steps;
+  look(lane, tiles, steps);
+  const int tiles0 = tiles, steps0 = steps;
+  int q = 1 << 24;              // most steps of a piece
+  if (a.plan.most_pieces > 0) {
+    int most = (int)wave_max((float)steps);
+    for (int base = 64; base < a.B; base += 64) {
+      look(base + lane, tiles, steps);
+      most = max(most, (int)wave_max((float)steps));
+    }
+    q = max(ceil_div(most, lane + 1), min(kLeastSteps, most));
+    float pieces = 0.0f;
+    for (int base = 0; base < a.B; base += 64) {
+      if (base > 0) look(base + lane, tiles, steps); else tiles = tiles0, steps = steps0;
+      for (uint64_t left = __ballot(tiles > 0); left; left &= left - 1) {
+        const int l = __builtin_ctzll(left);
+        pieces += (float)(__builtin_amdgcn_readlane(tiles, l) * ceil_div(__builtin_amdgcn_readlane(steps, l), q));
+      }
+    }
+    pieces *= (float)a.Hkv;
+    float cost = ceilf(pieces * a.plan.per_slot) * (float)(q + kPieceSteps);
+    if (q < most) cost = pieces > (float)a.plan.most_pieces ? 3e38f : cost + kJoinSteps;
+    const float least = -wave_max_any(-cost);
+    q = __builtin_amdgcn_readlane(q, __builtin_ctzll(__ballot(cost == least)));
+  }
+  Piece p;
+  p.tile = -1;
+  int have = 0;
+  for (int base = 0; base < a.B; base += 64) {
+    if (base > 0) look(base + lane, tiles, steps); else tiles = tiles0, steps = steps0;
+    const int cuts = ceil_div(steps, q), mine = tiles * cuts * a.Hkv, pre = wave_prefix(mine);
+    const uint64_t in = __ballot(have + pre > index);
+    if (in) {
+      const int l = __builtin_ctzll(in);
+      p.b = base + l;
+      p.tiles = __builtin_amdgcn_readlane(tiles, l);
+      p.nsplit = __builtin_amdgcn_readlane(cuts, l);
+      p.chunk = ceil_div(__builtin_amdgcn_readlane(steps, l), p.nsplit) * 64;
+      const int at = index - have - (__builtin_amdgcn_readlane(pre, l) - __builtin_amdgcn_readlane(mine, l));
+      // heads next to each other (they run on different dies), the last tiles, which see most keys, first
+      p.h = at % a.Hkv;
+      const int rest = at / a.Hkv;
+      p.split = rest % p.nsplit;
+      p.tile = p.tiles - 1 - rest / p.nsplit;
+      p.first = at == 0;
+      p.t0 = __builtin_amdgcn_readfirstlane(first_token(a, p.b));
+      p.m = __builtin_amdgcn_readfirstlane(first_token(a, p.b + 1)) - p.t0;
+      return p;
+    }
+    have += last_lane(pre);
+  }
+  return p;
+}
+// where the rows of a piece's partial result stand, and what the joining launch needs to find them
+__device__ __forceinline__ void note_cuts(const AttendArgs& a, const Piece& p, int index) {
+  if (a.plan.most_pieces > 0 && p.first && threadIdx.x == 0) ((int4*)(a.ws + a.plan.cuts))[p.b] = make_int4(index, p.nsplit, p.chunk, p.tiles);
 }
 
 // base-2 logarithm of a row's sum and maximum -> natural log-sum-exp; -inf for a row that saw nothing

@@ -14,26 +14,17 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_f32(AttendAr
   __shared__ float pass_ml[4][2][kM];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, g = lane >> 4;
-  const int h = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
-  const int split = rest % a.plan.nsplit, item = a.plan.tiles - 1 - rest / a.plan.nsplit;
-  int b = -1;
-  for (int base = 0; base < a.B; base += 64) {
-    const int i = base + lane;
-    const uint64_t le = __ballot(i < a.B && first_token(a, i < a.B ? i : 0) * a.G / kM + i <= item);
-    b += __builtin_popcountll(le);
-    if (~le) break;
-  }
-  if (b < 0) return;
-  const int t0 = first_token(a, b), m = first_token(a, b + 1) - t0;
-  const int rows = m * a.G, row0 = (item - (t0 * a.G / kM + b)) * kM;
-  if (row0 >= rows) return;
+  const Piece piece = find_piece<kM>(a, blockIdx.x);
+  if (piece.tile < 0) return;
+  note_cuts(a, piece, blockIdx.x);
+  const int b = piece.b, h = piece.h, t0 = piece.t0, m = piece.m, rows = m * a.G, row0 = piece.tile * kM;
   const int len = rows_of(a, b, h);
   int key_hi = len - (m - 1 - (min(row0 + kM, rows) - 1) / a.G);
   key_hi = key_hi < 0 ? 0 : key_hi;
-  const int key_lo = split * a.plan.chunk;
-  if (a.plan.nsplit > 1) {
-    if (key_lo >= key_hi && split > 0) return;
-    key_hi = min(key_hi, key_lo + a.plan.chunk);
+  const int key_lo = piece.split * piece.chunk;
+  if (piece.nsplit > 1) {
+    if (key_lo >= key_hi) return;
+    key_hi = min(key_hi, key_lo + piece.chunk);
   }
   const int row = row0 + n16, tok = row / a.G, hd = row - tok * a.G;
   const bool in = row < rows;
@@ -141,8 +132,8 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_f32(AttendAr
   __syncthreads();
   if (wave != 0 || !in) return;
   const long long at = (long long)(t0 + tok) * a.Hq + h * a.G + hd;
-  const long long slot = (long long)split * a.n_tokens * a.Hq + at;
-  const bool whole = a.plan.nsplit == 1, any = sum > 0.0f || sum != sum;
+  const long long slot = (long long)blockIdx.x * kM + n16;
+  const bool whole = piece.nsplit == 1, any = sum > 0.0f || sum != sum;
   float* dst = whole ? (float*)a.out + at * D : (float*)(a.ws + a.plan.split_o) + slot * D;
   const float by = !whole ? 1.0f : 1.0f / sum;
   // channel u 64 + (4 g + r) 4 + j of row n16 is o[u 4 + j][r]
@@ -164,12 +155,12 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_f32(AttendAr
 }
 
 hipError_t launch_attend_f32(const AttendArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)(a.plan.tiles * a.plan.nsplit * a.Hkv);
+  const unsigned grid = (unsigned)a.plan.grid;
   if (a.D == 64) k_attend_f32<64><<<grid, 256, 0, st>>>(a);
   else if (a.D == 128) k_attend_f32<128><<<grid, 256, 0, st>>>(a);
   else k_attend_f32<256><<<grid, 256, 0, st>>>(a);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess || a.plan.nsplit == 1 ? e : launch_attend_join(a, true, st);
+  return e != hipSuccess || a.plan.most_pieces == 0 ? e : launch_attend_join(a, true, st);
 }
 
 }  // namespace ea

@@ -72,30 +72,18 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n32 = lane & 31, hi = lane >> 5;
 
-  // ---- which tile: heads next to each other (they run on different dies), the last tiles, which see most keys, first
-  const int h = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
-  const int split = rest % a.plan.nsplit, item = a.plan.tiles - 1 - rest / a.plan.nsplit;
-  // sequence b's tiles start at floor(cu[b] G / 128) + b: as many as it can have up to there
-  int b = -1;
-  for (int base = 0; base < a.B; base += 64) {
-    const int i = base + lane;
-    const uint64_t le = __ballot(i < a.B && first_token(a, i < a.B ? i : 0) * a.G / kM + i <= item);
-    b += __builtin_popcountll(le);
-    if (~le) break;
-  }
-  if (b < 0) return;
-  const int t0 = __builtin_amdgcn_readfirstlane(first_token(a, b));
-  const int m = __builtin_amdgcn_readfirstlane(first_token(a, b + 1)) - t0;
-  const int rows = m * a.G, row0 = (item - (t0 * a.G / kM + b)) * kM;
-  if (row0 >= rows || (a.only_long && rows <= a.short_rows)) return;
+  const Piece piece = find_piece<kM>(a, blockIdx.x);
+  if (piece.tile < 0) return;
+  note_cuts(a, piece, blockIdx.x);
+  const int b = piece.b, h = piece.h, t0 = piece.t0, m = piece.m, rows = m * a.G, row0 = piece.tile * kM;
   const int len = __builtin_amdgcn_readfirstlane(rows_of(a, b, h));
   const int last_row = min(row0 + kM, rows) - 1;
   int key_hi = len - (m - 1 - last_row / a.G);           // keys that the tile's last token sees
   key_hi = key_hi < 0 ? 0 : key_hi;
-  const int key_lo = split * a.plan.chunk;
-  if (a.plan.nsplit > 1) {
-    if (key_lo >= key_hi && split > 0) return;
-    key_hi = min(key_hi, key_lo + a.plan.chunk);
+  const int key_lo = piece.split * piece.chunk;
+  if (piece.nsplit > 1) {
+    if (key_lo >= key_hi) return;                        // (the joining launch does not ask for it)
+    key_hi = min(key_hi, key_lo + piece.chunk);
   }
   const int unit = b * a.Hkv + h;
 
@@ -103,6 +91,8 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   const bool in = row < rows;
   const int vis = in ? len - (m - 1 - tok) : len;
   const int vis_min = len - (m - 1 - (row0 + wave * 32) / a.G);      // of the wavefront's rows
+  // (a scale's sign goes to the queries, so that logits order like their products, and a scale of zero leaves masked ones -inf)
+  const float scale = FP8 && a.kscale ? a.kscale[unit] : 1.0f, qk = a.scale * fmaxf(fabsf(scale), 1e-30f);
   bf16x8 q[kSteps];
   {
     const __bf16* src = (const __bf16*)a.q + (long long)(t0 + (in ? tok : 0)) * a.q_stride + (h * a.G + (in ? hd : 0)) * D;
@@ -110,10 +100,10 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
     for (int s = 0; s < kSteps; ++s) {
       bf16x8 w = *(const bf16x8*)(src + s * 16 + hi * 8);
       if (!in) w = (bf16x8)(__bf16)0.0f;
+      if (FP8 && scale < 0.0f) w = -w;
       q[s] = w;
     }
   }
-  const float qk = a.scale * (FP8 && a.kscale ? a.kscale[unit] : 1.0f);
 
   // ---- loads of a tile: pass i of wavefront w covers rows (NW i + w) kPer ..
   int entries = 0, window = key_lo;
@@ -229,9 +219,6 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
 #pragma unroll
     for (int f = 0; f < kRing; ++f) read_v(f);
     // key of s[t][r]: t 32 + (r / 4) 8 + hi 4 + r % 4
-    if constexpr (FP8)
-#pragma unroll
-      for (int t = 0; t < kKt; ++t) s[t] *= qk;
     if (key + kN > vis_min)
 #pragma unroll
       for (int t = 0; t < kKt; ++t)
@@ -243,7 +230,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
     for (int t = 0; t < kKt; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
-    if constexpr (!FP8) top *= qk;
+    top *= qk;
     // the maximum that weights are taken against moves only when a row's passes it by more than 2^8
     if (__any(top > mx + 8.0f)) {
       top = fmaxf(max_xor32(top), mx);
@@ -260,7 +247,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float s0 = s[kb >> 1][(kb & 1) * 8 + 2 * r], s1 = s[kb >> 1][(kb & 1) * 8 + 2 * r + 1];
-        const float x = FP8 ? pow2(s0 - from) : pow2(fmaf(s0, qk, -from)), y = FP8 ? pow2(s1 - from) : pow2(fmaf(s1, qk, -from));
+        const float x = pow2(fmaf(s0, qk, -from)), y = pow2(fmaf(s1, qk, -from));
         l += x + y;
         p[kb][r] = pack_bf16(x, y);
       }
@@ -297,7 +284,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   if (!in) return;
   const long long at = (long long)(t0 + tok) * a.Hq + h * a.G + hd;
   // channel c 32 + (r / 4) 8 + hi 4 + r % 4 is o[c][r]
-  if (a.plan.nsplit == 1) {
+  if (piece.nsplit == 1) {
     const bool any = l > 0.0f || l != l;
     const float f = (FP8 && a.vscale ? a.vscale[unit] : 1.0f) / l;
     __bf16* dst = (__bf16*)a.out + at * D;
@@ -309,7 +296,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
                                                        : make_uint2(0u, 0u);
     if (a.lse && hi == 0) a.lse[at] = natural_lse(mx, l);
   } else {
-    const long long slot = (long long)split * a.n_tokens * a.Hq + at;
+    const long long slot = (long long)blockIdx.x * kM + (row - row0);
     float* po = (float*)(a.ws + a.plan.split_o) + slot * D;
 #pragma unroll
     for (int c = 0; c < kCt; ++c)
@@ -320,47 +307,61 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   }
 }
 
-// The splits of every (token, head) row together: D / 4 threads each.
+// The pieces of every (token, head) row together: D / 4 threads each, eight pieces requested at a time.
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
-  constexpr int kLanes = D / 4;
+  constexpr int kLanes = D / 4, kRounds = 8;
   const long long at = (long long)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
-  const int c = threadIdx.x % kLanes;
+  const int c4 = threadIdx.x % kLanes * 4;
   const int token = (int)(at / a.Hq), head = (int)(at - (long long)token * a.Hq), h = head / a.G;
   // the token's sequence: tokens behind the last one are nobody's
-  int lo = 0, hi = a.B;
+  int b = 0, behind = a.B;
   if (token >= first_token(a, a.B) || token < first_token(a, 0)) return;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first_token(a, mid) <= token) lo = mid; else hi = mid;
+  while (behind - b > 1) {
+    const int mid = (b + behind) >> 1;
+    if (first_token(a, mid) <= token) b = mid; else behind = mid;
   }
-  const int t0 = first_token(a, lo), m = first_token(a, lo + 1) - t0;
+  const int t0 = first_token(a, b), m = first_token(a, b + 1) - t0;
   if (token >= t0 + m || (a.only_long && m * a.G <= a.short_rows)) return;
-  const int vis = rows_of(a, lo, h) - (m - 1 - (token - t0));
-  int n = (vis + a.plan.chunk - 1) / a.plan.chunk;
-  n = n < 1 ? 0 : n > a.plan.nsplit ? a.plan.nsplit : n;
-  const float* po = (const float*)(a.ws + a.plan.split_o);
-  const float2* ml = (const float2*)(a.ws + a.plan.split_ml);
-  const long long step = (long long)a.n_tokens * a.Hq;
+  const int4 cut = ((const int4*)(a.ws + a.plan.cuts))[b];      // its first piece, cuts, keys of a stretch, tiles
+  if (cut.y <= 1) return;
+  const int row = (token - t0) * a.G + head % a.G, tile = row / a.plan.tile_rows;
+  const int vis = rows_of(a, b, h) - (m - 1 - (token - t0));
+  int n = (vis + cut.z - 1) / cut.z;
+  n = n < 1 ? 0 : n > cut.y ? cut.y : n;
+  const int first = cut.x + (cut.w - 1 - tile) * cut.y * a.Hkv + h;
+  const float* po = (const float*)(a.ws + a.plan.split_o) + c4;
+  const float2* part_ml = (const float2*)(a.ws + a.plan.split_ml);
   float top = -__builtin_inff(), sum = 0.0f;
-  for (int i = 0; i < n; ++i) top = fmaxf(top, ml[i * step + at].x);
-  const float from = top == -__builtin_inff() ? 0.0f : top;
   float4 acc = make_float4(0, 0, 0, 0);
-  for (int i = 0; i < n; ++i) {
-    const float2 w = ml[i * step + at];
-    const float4 x = *(const float4*)(po + (i * step + at) * D + c * 4);
-    const float f = pow2(w.x - from);
-    sum += w.y * f;
-    acc.x += x.x * f; acc.y += x.y * f; acc.z += x.z * f; acc.w += x.w * f;
+  for (int i0 = 0; i0 < n; i0 += kRounds) {
+    float2 ml[kRounds];
+    float4 y[kRounds];
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k) {
+      const int i = i0 + k < n ? i0 + k : i0;
+      const long long slot = (long long)(first + i * a.Hkv) * a.plan.tile_rows + (row - tile * a.plan.tile_rows);
+      ml[k] = part_ml[slot];
+      y[k] = *(const float4*)(po + slot * D);
+    }
+#pragma unroll
+    for (int k = 0; k < kRounds; ++k)
+      if (i0 + k < n) {
+        const float t = fmaxf(top, ml[k].x), from = t == -__builtin_inff() ? 0.0f : t;
+        const float f = pow2(top - from), w = pow2(ml[k].x - from);
+        top = t;
+        sum = sum * f + ml[k].y * w;
+        acc.x = acc.x * f + y[k].x * w; acc.y = acc.y * f + y[k].y * w; acc.z = acc.z * f + y[k].z * w; acc.w = acc.w * f + y[k].w * w;
+      }
   }
   const bool any = sum > 0.0f || sum != sum;
-  const float f = any ? (a.vscale ? a.vscale[lo * a.Hkv + h] : 1.0f) / sum : 0.0f;
+  const float f = (a.vscale ? a.vscale[b * a.Hkv + h] : 1.0f) / sum;
   if (F32)
-    *(float4*)((float*)a.out + at * D + c * 4) = any ? make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f) : make_float4(0, 0, 0, 0);
+    *(float4*)((float*)a.out + at * D + c4) = any ? make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f) : make_float4(0, 0, 0, 0);
   else
-    *(uint2*)((__bf16*)a.out + at * D + c * 4) =
+    *(uint2*)((__bf16*)a.out + at * D + c4) =
         any ? make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f)) : make_uint2(0u, 0u);
-  if (a.lse && c == 0) a.lse[at] = natural_lse(top, sum);
+  if (a.lse && c4 == 0) a.lse[at] = natural_lse(top, sum);
 }
 
 hipError_t launch_attend_join(const AttendArgs& a, bool f32, hipStream_t st) {
@@ -378,9 +379,9 @@ static hipError_t tile_of_width(const AttendArgs& a, hipStream_t st) {
   static LdsOptIn opt;
   hipError_t e = opt.ensure((const void*)k_attend_tile<D, FP8, NW>, 2 * buffer_bytes<D, FP8>());
   if (e != hipSuccess) return e;
-  k_attend_tile<D, FP8, NW><<<(unsigned)(a.plan.tiles * a.plan.nsplit * a.Hkv), NW * 64, 2 * buffer_bytes<D, FP8>(), st>>>(a);
+  k_attend_tile<D, FP8, NW><<<(unsigned)a.plan.grid, NW * 64, 2 * buffer_bytes<D, FP8>(), st>>>(a);
   e = hipGetLastError();
-  if (e != hipSuccess || a.plan.nsplit == 1) return e;
+  if (e != hipSuccess || a.plan.most_pieces == 0) return e;
   return launch_attend_join(a, false, st);
 }
 template <int D, bool FP8>

@@ -66,9 +66,10 @@ struct AttendPlan {
   int shares;         // its workgroups
   int piece_rows;     // rows reserved for a partial result
   int tile_rows;      // (token, head) rows of a workgroup of the tile kernel
-  int tiles;          // of the tile kernel, per KV head
-  int nsplit, chunk;  // stretches of keys that workgroups of their own take there, and keys of each
-  size_t info, part_o, part_ml, split_o, split_ml, total;
+  int64_t grid;       // its workgroups: as many as there may be pieces
+  int most_pieces;    // most pieces where tiles are cut along the keys, 0: none is
+  float per_slot;     // 1 / workgroups that run at once
+  size_t info, part_o, part_ml, cuts, split_o, split_ml, total;
 };
 
 struct WsLayout {

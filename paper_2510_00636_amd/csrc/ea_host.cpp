@@ -1,7 +1,6 @@
 // Host-only part of libea: argument validation, tiling plans, workspace layout, and the two
 // host helpers of the ABI.  Nothing here touches the GPU, so it is testable without one.
 #include <math.h>
-#include <stdlib.h>
 
 #include "ea_common.h"
 
@@ -343,22 +342,16 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   a.rows = !f32 && a.short_rows >= d.G && (most <= a.piece_rows || d.B > 1);
   a.tile = f32 || most > a.piece_rows;
   a.shares = 2 * num_cu < kAttendShares ? 2 * num_cu : kAttendShares;
-  a.nsplit = 1;
-  a.tile_rows = f32 ? kAttendF32Rows : most >= 256 && !getenv("EA_T4") ? 256 : 128;
-  const int64_t unit_rows = a.tile_rows;
-  // sequence b's tiles start at floor(first token G / unit_rows) + b
-  a.tiles = (int)(n_tokens * d.G / unit_rows + d.B);
-  // enough workgroups for two per CU: keys in stretches where the tiles are few
-  const int64_t step = 64, busy = (n_tokens * d.G + unit_rows - 1) / unit_rows * d.Hkv, slots = 2 * (int64_t)num_cu;
-  int64_t cut = busy > 0 ? slots / busy : 1;
-  const int64_t most_cuts = (n + 511) / 512;
-  if (cut > most_cuts) cut = most_cuts;
-  if (cut < 1) cut = 1;
-  int64_t chunk = ((n + cut - 1) / cut + step - 1) / step * step;
-  if (chunk < step) chunk = step;
-  a.chunk = (int)chunk;
-  a.nsplit = (int)((n + chunk - 1) / chunk);
-  if (a.nsplit < 1) a.nsplit = 1;
+  a.tile_rows = f32 ? kAttendF32Rows : most > 128 ? 256 : 128;
+  // a sequence's last tile may be short: one more for each
+  const int64_t tiles = n_tokens * d.G / a.tile_rows + d.B, slots = a.tile_rows == 256 ? num_cu : 2 * (int64_t)num_cu;
+  a.grid = tiles * d.Hkv;
+  a.per_slot = 1.0f / (float)slots;
+  // more rounds of whole tiles than this share out the chip well enough
+  if (n_tokens * d.G / a.tile_rows * d.Hkv < 4 * slots && n > 64) {
+    a.most_pieces = (int)(2 * slots);
+    if (a.grid < a.most_pieces) a.grid = a.most_pieces;
+  }
   size_t o = 0;
   auto take = [&](size_t bytes) {
     const size_t at = o;
@@ -370,8 +363,9 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
     a.part_o = take((size_t)a.shares * 2 * a.piece_rows * d.D * sizeof(float));
     a.part_ml = take((size_t)a.shares * 2 * a.piece_rows * 2 * sizeof(float));
   }
-  if (a.tile && a.nsplit > 1) {
-    const size_t rows = (size_t)a.nsplit * (size_t)n_tokens * d.Hq;
+  if (a.tile && a.most_pieces > 0) {
+    const size_t rows = (size_t)a.most_pieces * a.tile_rows;
+    a.cuts = take((size_t)d.B * 4 * sizeof(int32_t));
     a.split_o = take(rows * d.D * sizeof(float));
     a.split_ml = take(rows * 2 * sizeof(float));
   }

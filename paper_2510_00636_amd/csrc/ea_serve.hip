@@ -36,9 +36,9 @@ static ea_status attend(const Dims& d, const void* q, const ea_step* step, const
   if (overlap(out, out_bytes, k, cache) || overlap(out, out_bytes, v, cache)) return EA_ERR_INVALID_ARG;
   a.plan = make_attend_plan(d, n, step->n_tokens, step->max_new, kPlanCus);
   if (ws_bytes < a.plan.total) return EA_ERR_WORKSPACE;
-  // (workgroups of 256 threads, 2^32 threads to a launch)
-  const int64_t most = (int64_t)1 << 23;
-  if ((int64_t)a.plan.tiles * a.plan.nsplit * d.Hkv > most || (int64_t)d.units() * a.plan.short_rows > most) return EA_ERR_UNSUPPORTED;
+  // (workgroups of up to 512 threads, 2^32 threads to a launch)
+  const int64_t most = (int64_t)1 << 22;
+  if (a.plan.grid > most || (int64_t)d.units() * a.plan.short_rows > most) return EA_ERR_UNSUPPORTED;
   if (step->n_tokens == 0) return EA_OK;
   a.q = q; a.k = k; a.v = v; a.cu = step->cu_tokens; a.lens = lengths; a.kscale = kscale; a.vscale = vscale;
   a.out = out; a.lse = lse; a.ws = (char*)ws;
