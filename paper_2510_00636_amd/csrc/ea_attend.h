@@ -102,11 +102,11 @@ __device__ __forceinline__ float max_xor16(float x) {
 // ---- Stretches: which piece a workgroup takes.
 // A sequence's (token, head) rows come in tiles of ROWS; tiles of few, long sequences are cut along the keys as well, so that the
 // pieces fill the chip's slots evenly.  How finely follows from the lengths on the device: every lane looks at one way to cut the
-// longest (and with it the others, into pieces of at most as many keys), the rounds of pieces that it takes times what a piece takes,
-// and the cheapest is taken.  A piece costs kPieceSteps steps of 64 keys besides its own (its queries, its first tile, its results),
-// cutting at all kJoinSteps (the launch that joins).  All workgroups come to the same result, and the first of a sequence writes
-// down for the joining launch how it was cut.
-constexpr int kPieceSteps = 3, kJoinSteps = 4, kLeastSteps = 4;
+// longest (and with it the others, into pieces of at most as many keys), and the one that is done first is taken.  All workgroups
+// come to the same result, and the first of a sequence writes down for the joining launch how it was cut.  In steps of 64 keys:
+// a piece costs kPieceSteps besides its own (its queries, its first tile, its results), a cut one kCutSteps more of a slot
+// (its partial result written and read again, 5 TB/s for all), cutting at all kJoinSteps (the launch that joins).
+constexpr int kPieceSteps = 3, kCutSteps = 6, kJoinSteps = 4, kLeastSteps = 4, kLongSteps = 64;
 struct Piece {
   int b, h, tile, split;        // tile < 0: none
   int tiles, nsplit, chunk;     // of the sequence, and keys of a stretch
@@ -144,26 +144,40 @@ __device__ __forceinline__ Piece find_piece(const AttendArgs& a, int index) {
       most = max(most, (int)wave_max((float)steps));
     }
     q = max(ceil_div(most, lane + 1), min(kLeastSteps, most));
-    float pieces = 0.0f;
+    float pieces = 0.0f, cut = 0.0f, work = 0.0f;
     for (int base = 0; base < a.B; base += 64) {
       if (base > 0) look(base + lane, tiles, steps); else tiles = tiles0, steps = steps0;
       for (uint64_t left = __ballot(tiles > 0); left; left &= left - 1) {
-        const int l = __builtin_ctzll(left);
-        pieces += (float)(__builtin_amdgcn_readlane(tiles, l) * ceil_div(__builtin_amdgcn_readlane(steps, l), q));
+        const int l = __builtin_ctzll(left), n = __builtin_amdgcn_readlane(tiles, l) * a.Hkv, each = __builtin_amdgcn_readlane(steps, l);
+        const int k = ceil_div(each, q);
+        pieces += (float)(n * k);
+        cut += k > 1 ? (float)(n * k) : 0.0f;
+        work += (float)n * (float)each;
       }
     }
-    pieces *= (float)a.Hkv;
-    float cost = ceilf(pieces * a.plan.per_slot) * (float)(q + kPieceSteps);
-    if (q < most) cost = pieces > (float)a.plan.most_pieces ? 3e38f : cost + kJoinSteps;
+    // one round: its longest piece.  More: the work shared out, with a quarter of a piece at the end, but whole rounds where all
+    // pieces are alike
+    const float longest = (float)(q + kPieceSteps), per_slot = a.plan.per_slot;
+    float cost = longest;
+    if (pieces * per_slot > 1.0f) {
+      cost = (work + pieces * kPieceSteps) * per_slot + 0.25f * longest;
+      if (work > 0.9f * pieces * (float)q) cost = fmaxf(cost, ceilf(pieces * per_slot) * longest);
+    }
+    if (cut > 0.0f) cost = pieces > (float)a.plan.most_pieces ? 3e38f : cost + kJoinSteps + cut * per_slot * kCutSteps;
     const float least = -wave_max_any(-cost);
     q = __builtin_amdgcn_readlane(q, __builtin_ctzll(__ballot(cost == least)));
   }
   Piece p;
   p.tile = -1;
   int have = 0;
-  for (int base = 0; base < a.B; base += 64) {
-    if (base > 0) look(base + lane, tiles, steps); else tiles = tiles0, steps = steps0;
-    const int cuts = ceil_div(steps, q), mine = tiles * cuts * a.Hkv, pre = wave_prefix(mine);
+  // sequences of long pieces first, so that short ones fill up the end
+  const int blocks = (a.B + 63) >> 6;
+  for (int turn = 0; turn < 2 * blocks; ++turn) {
+    const int base = (turn >= blocks ? turn - blocks : turn) * 64;
+    if (blocks > 1) look(base + lane, tiles, steps); else tiles = tiles0, steps = steps0;
+    const int cuts = ceil_div(steps, q);
+    if ((2 * ceil_div(steps, max(cuts, 1)) >= min(q, kLongSteps)) != (turn < blocks)) tiles = 0;
+    const int mine = tiles * cuts * a.Hkv, pre = wave_prefix(mine);
     const uint64_t in = __ballot(have + pre > index);
     if (in) {
       const int l = __builtin_ctzll(in);

@@ -19,6 +19,8 @@ using s16x4 = short __attribute__((ext_vector_type(4)));
 template <int D, bool FP8> constexpr int k_pitch() { return D * 2 + (FP8 ? 16 : 0); }
 template <int D, bool FP8> constexpr int v_pitch() { return D * 2 + (FP8 ? 64 : 0); }
 template <int D> constexpr int tile_keys() { return D == 256 ? 32 : 64; }
+// Tiles in LDS at once: one worked on, the others on their way.  As many as fit the workgroups of a CU.
+template <int D, bool FP8, int NW> constexpr int stages() { return FP8 ? 2 : D == 128 && NW == 4 ? 2 : 4; }
 template <int D, bool FP8> constexpr int buffer_bytes() { return tile_keys<D>() * (k_pitch<D, FP8>() + v_pitch<D, FP8>()); }
 template <int D> __device__ __forceinline__ int k_piece(int row) { return row & 7; }
 template <int D> __device__ __forceinline__ int v_piece(int row) { return D == 64 ? (row >> 1 & 1) * 4 : (row & 3) * 4; }
@@ -67,6 +69,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   constexpr int kPasses = kN / (NW * kPer);               // of the workgroup's loads over a tile
   constexpr int kChunks = kRowBytes / 16;
   constexpr int kKPitch = k_pitch<D, FP8>(), kVPitch = v_pitch<D, FP8>(), kBuffer = buffer_bytes<D, FP8>();
+  constexpr int kStages = stages<D, FP8, NW>();
   constexpr bool kOrdered = D < 256;                     // at d = 256 the registers are all taken without an order
   extern __shared__ char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -105,12 +108,19 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
     }
   }
 
-  // ---- loads of a tile: pass i of wavefront w covers rows (NW i + w) kPer ..
-  int entries = 0, window = key_lo;
-  auto load_window = [&](int from) {
-    const int r = from + lane * 16;
-    entries = table_entry(a, b, r < len ? r : len > 0 ? len - 1 : 0);
-    window = from;
+  // ---- loads of a tile: pass i of wavefront w covers rows (NW i + w) kPer .., which lie in one block; its table entry is looked up
+  // a tile ahead (by scalar loads: a vector load's wait would be one for all the rows on their way)
+  int entry[kPasses];
+  auto first_row = [&](int at, int i) {                  // of the 16 rows that the pass's lie in, or of the last ones there are
+    const int sub = (at + (NW * i + wave) * kPer) & ~15;
+    return sub < len ? sub : (len - 1) & ~15;
+  };
+  auto look_up = [&](int at) {
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      const long long blk = (long long)b * a.pm.max_blocks + (first_row(at, i) >> a.pm.sh);
+      entry[i] = a.pm.table ? ((const __attribute__((address_space(4))) int32_t*)a.pm.table)[blk] : 0;
+    }
   };
   u32x4 kraw[FP8 ? kPasses : 1], vraw[FP8 ? kPasses : 1];
   const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
@@ -119,11 +129,9 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   auto request = [&](int at, int buf) {
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
-      const int r0 = at + (NW * i + wave) * kPer, sub = r0 & ~15;
-      const int from = sub < len ? sub : (len - 1) & ~15;
-      const int e = __builtin_amdgcn_readlane(entries, (from - window) >> 4);
-      const int r = min(r0 - sub + lane / kChunks, len - 1 - from);
-      const long long at_byte = row_base(a, b, h, from, e) * kRowBytes;
+      const int from = first_row(at, i), r0 = at + (NW * i + wave) * kPer;
+      const int r = min(r0 - (r0 & ~15) + lane / kChunks, len - 1 - from);
+      const long long at_byte = row_base(a, b, h, from, entry[i]) * kRowBytes;
       if constexpr (FP8) {
         kraw[i] = *(const u32x4*)((const char*)a.k + at_byte + (r * kRowBytes + k_off));
         vraw[i] = *(const u32x4*)((const char*)a.v + at_byte + (r * kRowBytes + v_off));
@@ -149,9 +157,11 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
       *(uint4*)(vd + 16) = widen_fp8(make_uint2(v.z, v.w));
     }
   };
-  // bf16 rows: all of the tile has arrived; the values behind the last row become zeros
-  auto arrived = [&](int at, int buf) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  // bf16 rows: the tile at `at` has arrived (its loads and all in front of them; `behind`: as many tiles as the ring takes have been
+  // requested behind it); the values behind the last row become zeros
+  auto arrived = [&](int at, int buf, bool behind) {
+    if (behind) asm volatile("s_waitcnt vmcnt(%0)" :: "n"((kStages - 2) * 2 * kPasses) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (at + kN > key_hi) {
       u32x4* v = (u32x4*)(lds + buf * kBuffer + kN * kKPitch);
@@ -165,14 +175,24 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   for (int c = 0; c < kCt; ++c) o[c] = (f32x16)0.0f;
   float mx = -__builtin_inff(), l = 0.0f;
   if (key_lo < key_hi) {
-    load_window(key_lo);
-    request(key_lo, 0);
+    look_up(key_lo);
     if constexpr (FP8) {
+      request(key_lo, 0);
+      look_up(key_lo + kN);
       stage(key_lo, 0);
-      if (key_lo + kN < key_hi) request(key_lo + kN, 1);
+      if (key_lo + kN < key_hi) {
+        request(key_lo + kN, 1);
+        look_up(key_lo + 2 * kN);
+      }
       __syncthreads();
     } else {
-      arrived(key_lo, 0);
+#pragma unroll
+      for (int t = 0; t < kStages - 1; ++t)
+        if (key_lo + t * kN < key_hi) {
+          request(key_lo + t * kN, t);
+          look_up(key_lo + (t + 1) * kN);
+        }
+      arrived(key_lo, 0, key_lo + (kStages - 2) * kN < key_hi);
     }
   }
   // where the lane's operands stand: K's row n32, pieces 2 c + hi; V's rows 4 hi + .., 64-byte stretches c
@@ -185,13 +205,14 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   for (int c = 0; c < kVWays; ++c)
     v_at[c] = kN * kKPitch + v_row * kVPitch + ((c * 4) ^ (FP8 ? 0 : v_piece<D>(v_row))) * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
   int buf = 0;
-  for (int key = key_lo; key < key_hi; key += kN, buf ^= 1) {
+  for (int key = key_lo; key < key_hi; key += kN, buf = buf + 1 < kStages ? buf + 1 : 0) {
     const char* kt = lds + buf * kBuffer;
     const int next = key + kN;
+    const int next_buf = buf + 1 < kStages ? buf + 1 : 0, far = key + (kStages - 1) * kN;
     if constexpr (!FP8)
-      if (next < key_hi) {
-        if (next - window >= 1024) load_window(next);
-        request(next, buf ^ 1);
+      if (far < key_hi) {
+        request(far, buf > 0 ? buf - 1 : kStages - 1);
+        look_up(far + kN);
       }
     f32x16 s[kKt];
 #pragma unroll
@@ -268,14 +289,14 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
     }
     if (next < key_hi) {
       if constexpr (FP8) {
-        stage(next, buf ^ 1);
+        stage(next, next_buf);
         if (next + kN < key_hi) {
-          if (next + kN - window >= 1024) load_window(next + kN);
           request(next + kN, buf);
+          look_up(next + 2 * kN);
         }
         __syncthreads();
       } else {
-        arrived(next, buf ^ 1);
+        arrived(next, next_buf, next + (kStages - 2) * kN < key_hi);
       }
     }
   }
@@ -377,9 +398,9 @@ hipError_t launch_attend_join(const AttendArgs& a, bool f32, hipStream_t st) {
 template <int D, bool FP8, int NW>
 static hipError_t tile_of_width(const AttendArgs& a, hipStream_t st) {
   static LdsOptIn opt;
-  hipError_t e = opt.ensure((const void*)k_attend_tile<D, FP8, NW>, 2 * buffer_bytes<D, FP8>());
+  hipError_t e = opt.ensure((const void*)k_attend_tile<D, FP8, NW>, stages<D, FP8, NW>() * buffer_bytes<D, FP8>());
   if (e != hipSuccess) return e;
-  k_attend_tile<D, FP8, NW><<<(unsigned)a.plan.grid, NW * 64, 2 * buffer_bytes<D, FP8>(), st>>>(a);
+  k_attend_tile<D, FP8, NW><<<(unsigned)a.plan.grid, NW * 64, stages<D, FP8, NW>() * buffer_bytes<D, FP8>(), st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess || a.plan.most_pieces == 0) return e;
   return launch_attend_join(a, false, st);
