@@ -12,18 +12,25 @@ namespace {
 
 using s16x4 = short __attribute__((ext_vector_type(4)));
 
-// A tile in LDS.  bf16 rows come straight from memory, 1 KiB per wavefront and load, so they stand without gaps; what would make
-// rows meet in the banks is taken out by their order in 16-byte pieces: piece c of a row stands at c ^ (row & 7) in K (16-byte reads
-// of eight rows at a time) and at c ^ 4 (row & 3) in V (transposing reads of 64 bytes of four rows; d = 64: two rows to all banks).
-// 8-bit rows pass through registers and are widened there; their K rows are four banks apart, V's sixteen.
+// A tile in LDS.  bf16 rows come straight from memory, 1 KiB per wavefront and load, lanes in order, so what would make rows meet in
+// the 64 banks has to be taken out by gaps between such loads and by the order of the 16-byte pieces in a row.  K is read sixteen rows
+// at a time, 16 bytes of each: 64 bytes of gap behind every KiB, and piece c stands at c ^ k_piece(row).  V is read (transposing) four
+// rows at a time, 64 bytes of each: no gaps, piece c at c ^ v_piece(row).  8-bit rows pass through registers, are widened there, and
+// have rows four banks apart for K, sixteen for V.
 template <int D, bool FP8> constexpr int k_pitch() { return D * 2 + (FP8 ? 16 : 0); }
 template <int D, bool FP8> constexpr int v_pitch() { return D * 2 + (FP8 ? 64 : 0); }
 template <int D> constexpr int tile_keys() { return D == 256 ? 32 : 64; }
+template <int D, bool FP8> constexpr int k_bytes() { return FP8 ? tile_keys<D>() * k_pitch<D, true>() : tile_keys<D>() * D * 2 / 1024 * 1088; }
 // Tiles in LDS at once: one worked on, the others on their way.  As many as fit the workgroups of a CU.
 template <int D, bool FP8, int NW> constexpr int stages() { return FP8 ? 2 : D == 128 && NW == 4 ? 2 : 4; }
-template <int D, bool FP8> constexpr int buffer_bytes() { return tile_keys<D>() * (k_pitch<D, FP8>() + v_pitch<D, FP8>()); }
-template <int D> __device__ __forceinline__ int k_piece(int row) { return row & 7; }
+template <int D, bool FP8> constexpr int buffer_bytes() { return k_bytes<D, FP8>() + tile_keys<D>() * v_pitch<D, FP8>(); }
+// (the row's bits that its place in its KiB and the gap in front of that leave over)
+template <int D> __device__ __forceinline__ int k_piece(int row) { return D == 64 ? row >> 1 & 3 : D == 128 ? row & 3 : (row & 1) | (row >> 2 & 2); }
 template <int D> __device__ __forceinline__ int v_piece(int row) { return D == 64 ? (row >> 1 & 1) * 4 : (row & 3) * 4; }
+// where row `row` of K begins
+template <int D, bool FP8> __host__ __device__ constexpr int k_row(int row) {
+  return FP8 ? row * k_pitch<D, true>() : row / (512 / D) * 1088 + row % (512 / D) * D * 2;
+}
 
 // 16 bytes per lane from base + at to LDS address `to` and on, lanes in order.  Nothing waits for it but the s_waitcnt in front of
 // the barrier behind which the tile is read; the compiler, told of such a load, would wait at the next read of any LDS.  (m0 is
@@ -68,7 +75,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   constexpr int kPer = 1024 / kRowBytes;                 // rows that a wavefront's load covers
   constexpr int kPasses = kN / (NW * kPer);               // of the workgroup's loads over a tile
   constexpr int kChunks = kRowBytes / 16;
-  constexpr int kKPitch = k_pitch<D, FP8>(), kVPitch = v_pitch<D, FP8>(), kBuffer = buffer_bytes<D, FP8>();
+  constexpr int kKPitch = k_pitch<D, FP8>(), kKBytes = k_bytes<D, FP8>(), kVPitch = v_pitch<D, FP8>(), kBuffer = buffer_bytes<D, FP8>();
   constexpr int kStages = stages<D, FP8, NW>();
   constexpr bool kOrdered = D < 256;                     // at d = 256 the registers are all taken without an order
   extern __shared__ char lds[];
@@ -124,21 +131,22 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   };
   u32x4 kraw[FP8 ? kPasses : 1], vraw[FP8 ? kPasses : 1];
   const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  const int my_row = wave * kPer + lane / kChunks, my_piece = lane % kChunks;      // of the tile, in pass 0; the others are whole eights behind
-  const int k_off = (FP8 ? my_piece : my_piece ^ k_piece<D>(my_row)) * 16, v_off = (FP8 ? my_piece : my_piece ^ v_piece<D>(my_row)) * 16;
+  const int my_row = wave * kPer + lane / kChunks, my_piece = lane % kChunks;      // of the tile, in pass 0
   auto request = [&](int at, int buf) {
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
       const int from = first_row(at, i), r0 = at + (NW * i + wave) * kPer;
       const int r = min(r0 - (r0 & ~15) + lane / kChunks, len - 1 - from);
       const long long at_byte = row_base(a, b, h, from, entry[i]) * kRowBytes;
+      const int in_tile = NW * i * kPer + my_row;
+      const int k_off = (FP8 ? my_piece : my_piece ^ k_piece<D>(in_tile)) * 16, v_off = (FP8 ? my_piece : my_piece ^ v_piece<D>(in_tile)) * 16;
       if constexpr (FP8) {
         kraw[i] = *(const u32x4*)((const char*)a.k + at_byte + (r * kRowBytes + k_off));
         vraw[i] = *(const u32x4*)((const char*)a.v + at_byte + (r * kRowBytes + v_off));
       } else {
-        const uint32_t to = lds_at + buf * kBuffer + (NW * i + wave) * 1024;
-        to_lds(to, (const char*)a.k + at_byte, r * kRowBytes + k_off);
-        to_lds(to + kN * kKPitch, (const char*)a.v + at_byte, r * kRowBytes + v_off);
+        const uint32_t to = lds_at + buf * kBuffer;
+        to_lds(to + (NW * i + wave) * 1088, (const char*)a.k + at_byte, r * kRowBytes + k_off);
+        to_lds(to + kKBytes + (NW * i + wave) * 1024, (const char*)a.v + at_byte, r * kRowBytes + v_off);
       }
     }
   };
@@ -150,7 +158,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
       const uint32_t keep = at + r >= key_hi ? 0u : ~0u;
       const u32x4 v = vraw[i] & keep;
       char* kd = lds + buf * kBuffer + r * kKPitch + my_piece * 32;
-      char* vd = lds + buf * kBuffer + kN * kKPitch + r * kVPitch + my_piece * 32;
+      char* vd = lds + buf * kBuffer + kKBytes + r * kVPitch + my_piece * 32;
       *(uint4*)kd = widen_fp8(make_uint2(kraw[i].x, kraw[i].y));
       *(uint4*)(kd + 16) = widen_fp8(make_uint2(kraw[i].z, kraw[i].w));
       *(uint4*)vd = widen_fp8(make_uint2(v.x, v.y));
@@ -164,7 +172,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     if (at + kN > key_hi) {
-      u32x4* v = (u32x4*)(lds + buf * kBuffer + kN * kKPitch);
+      u32x4* v = (u32x4*)(lds + buf * kBuffer + kKBytes);
       for (int i = (key_hi - at) * (D / 8) + (int)threadIdx.x; i < kN * (D / 8); i += NW * 64) v[i] = (u32x4)0u;
       __syncthreads();
     }
@@ -197,13 +205,13 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   }
   // where the lane's operands stand: K's row n32, pieces 2 c + hi; V's rows 4 hi + .., 64-byte stretches c
   const int v_row = 4 * hi + ((lane & 15) >> 2);
-  constexpr int kKWays = FP8 ? 1 : 4, kVWays = FP8 ? 1 : D == 64 ? 2 : 4;
+  constexpr int kKWays = FP8 ? 1 : 2, kVWays = FP8 ? 1 : D == 64 ? 2 : 4;
   uint32_t k_at[kKWays], v_at[kVWays];
 #pragma unroll
-  for (int c = 0; c < kKWays; ++c) k_at[c] = n32 * kKPitch + ((2 * c + hi) ^ (FP8 ? 0 : k_piece<D>(n32))) * 16;
+  for (int c = 0; c < kKWays; ++c) k_at[c] = k_row<D, FP8>(n32) + ((2 * c + hi) ^ (FP8 ? 0 : k_piece<D>(n32))) * 16;
 #pragma unroll
   for (int c = 0; c < kVWays; ++c)
-    v_at[c] = kN * kKPitch + v_row * kVPitch + ((c * 4) ^ (FP8 ? 0 : v_piece<D>(v_row))) * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    v_at[c] = kKBytes + v_row * kVPitch + ((c * 4) ^ (FP8 ? 0 : v_piece<D>(v_row))) * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
   int buf = 0;
   for (int key = key_lo; key < key_hi; key += kN, buf = buf + 1 < kStages ? buf + 1 : 0) {
     const char* kt = lds + buf * kBuffer;
@@ -214,17 +222,19 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
         request(far, buf > 0 ? buf - 1 : kStages - 1);
         look_up(far + kN);
       }
+    __builtin_amdgcn_s_setprio(1);
     f32x16 s[kKt];
 #pragma unroll
     for (int t = 0; t < kKt; ++t) {
       s[t] = (f32x16)0.0f;
 #pragma unroll
       for (int c = 0; c < kSteps; ++c) {
-        const bf16x8 w = *(const bf16x8*)(kt + k_at[c % kKWays] + t * 32 * kKPitch + c / kKWays * kKWays * 32);
+        const bf16x8 w = *(const bf16x8*)(kt + k_at[c % kKWays] + t * k_row<D, FP8>(32) + c / kKWays * kKWays * 32);
         s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[c], s[t], 0, 0, 0);
       }
     }
     if constexpr (kOrdered) order_products<kKt * kSteps, 6>();
+    __builtin_amdgcn_s_setprio(0);
     // V^T's operands, kRing of them ahead of the products.  Lanes 16 j .. of a group of 16 read four rows of 16 channels, and get one
     // channel of the four rows each
     constexpr int kRing = D == 256 ? 1 : 4, kOperands = kKt * 2 * kCt;
@@ -274,6 +284,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
       }
     };
     weigh(0);
+    __builtin_amdgcn_s_setprio(1);
     if constexpr (kOrdered) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int kb = 0; kb < kKt * 2; ++kb) {
@@ -287,6 +298,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
       if (kb + 1 < kKt * 2) weigh(kb + 1);
       if constexpr (kOrdered) order_weighted<kCt>();
     }
+    __builtin_amdgcn_s_setprio(0);
     if (next < key_hi) {
       if constexpr (FP8) {
         stage(next, next_buf);
