@@ -67,7 +67,7 @@ __device__ __forceinline__ void order_weighted() {
 
 }  // namespace
 
-template <int D, bool FP8, int NW>
+template <int D, bool FP8, bool PAGED, int NW>
 __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_attend_tile(AttendArgs a) {
   constexpr int kM = NW * 32;
   constexpr int kN = tile_keys<D>(), kKt = kN / 32, kSteps = D / 16, kCt = D / 32;
@@ -115,38 +115,56 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
     }
   }
 
-  // ---- loads of a tile: pass i of wavefront w covers rows (NW i + w) kPer .., which lie in one block; its table entry is looked up
-  // a tile ahead (by scalar loads: a vector load's wait would be one for all the rows on their way)
-  int entry[kPasses];
-  auto first_row = [&](int at, int i) {                  // of the 16 rows that the pass's lie in, or of the last ones there are
+  // ---- loads of a tile: pass i of wavefront w covers rows (NW i + w) kPer .., which lie in one block.  Rows behind the last one are
+  // asked for as the last one.  A tile's places are made while the tile in front of it is worked on, and their blocks looked up one
+  // tile before that (by scalar loads: a vector load's wait would be one for all the rows on their way).
+  const char* kp = (const char*)a.k + (PAGED ? ((long long)h << a.pm.sh) : ((long long)b * a.Hkv + h) * a.n_cap) * kRowBytes;
+  const char* vp = (const char*)a.v + (kp - (const char*)a.k);
+  const int32_t* table = PAGED ? a.pm.table + (long long)b * a.pm.max_blocks : nullptr;
+  const uint32_t block_bytes = PAGED ? ((uint32_t)a.Hkv << a.pm.sh) * (uint32_t)kRowBytes : 0;     // (less than 2^32: the host sees to it)
+  const int in_block = PAGED ? (1 << a.pm.sh) - 1 : ~0, last_block = (int)(a.pm.num_blocks - 1), last_sub = (len - 1) & ~15;
+  const int my_row = wave * kPer + lane / kChunks, my_piece = lane % kChunks;      // of the tile, in pass 0
+  const int last_tile = key_lo + (key_hi - 1 - key_lo) / kN * kN;
+  int entry[kPasses];                // of the tile behind the one whose places stand in `place`
+  long long place[kPasses];
+  uint32_t k_off[kPasses], v_off[kPasses];
+  auto first_row = [&](int at, int i) {                  // of the 16 rows that the pass's lie in
     const int sub = (at + (NW * i + wave) * kPer) & ~15;
-    return sub < len ? sub : (len - 1) & ~15;
+    return sub < last_sub ? sub : last_sub;
   };
   auto look_up = [&](int at) {
+    at = at < last_tile ? at : last_tile;
+#pragma unroll
+    for (int i = 0; i < (PAGED ? kPasses : 0); ++i)
+      entry[i] = ((const __attribute__((address_space(4))) int32_t*)table)[first_row(at, i) >> a.pm.sh];
+  };
+  auto make_places = [&](int at) {
+    at = at < last_tile ? at : last_tile;
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
-      const long long blk = (long long)b * a.pm.max_blocks + (first_row(at, i) >> a.pm.sh);
-      entry[i] = a.pm.table ? ((const __attribute__((address_space(4))) int32_t*)a.pm.table)[blk] : 0;
+      const int from = first_row(at, i), r0 = at + (NW * i + wave) * kPer, in_tile = NW * i * kPer + my_row;
+      const int r = min(r0 - (r0 & ~15) + lane / kChunks, len - 1 - from);
+      k_off[i] = r * kRowBytes + (FP8 ? my_piece : my_piece ^ k_piece<D>(in_tile)) * 16;
+      v_off[i] = r * kRowBytes + (FP8 ? my_piece : my_piece ^ v_piece<D>(in_tile)) * 16;
+      place[i] = (long long)(from & in_block) * kRowBytes;
+      if (PAGED) {
+        const int blk = entry[i] < 0 ? 0 : entry[i] < last_block ? entry[i] : last_block;      // a bad entry leads into the pool
+        place[i] += (long long)((uint64_t)(uint32_t)blk * block_bytes);
+      }
     }
   };
   u32x4 kraw[FP8 ? kPasses : 1], vraw[FP8 ? kPasses : 1];
   const uint32_t lds_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  const int my_row = wave * kPer + lane / kChunks, my_piece = lane % kChunks;      // of the tile, in pass 0
-  auto request = [&](int at, int buf) {
+  auto request = [&](int buf) {      // the tile at `place`
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
-      const int from = first_row(at, i), r0 = at + (NW * i + wave) * kPer;
-      const int r = min(r0 - (r0 & ~15) + lane / kChunks, len - 1 - from);
-      const long long at_byte = row_base(a, b, h, from, entry[i]) * kRowBytes;
-      const int in_tile = NW * i * kPer + my_row;
-      const int k_off = (FP8 ? my_piece : my_piece ^ k_piece<D>(in_tile)) * 16, v_off = (FP8 ? my_piece : my_piece ^ v_piece<D>(in_tile)) * 16;
       if constexpr (FP8) {
-        kraw[i] = *(const u32x4*)((const char*)a.k + at_byte + (r * kRowBytes + k_off));
-        vraw[i] = *(const u32x4*)((const char*)a.v + at_byte + (r * kRowBytes + v_off));
+        kraw[i] = *(const u32x4*)(kp + place[i] + k_off[i]);
+        vraw[i] = *(const u32x4*)(vp + place[i] + v_off[i]);
       } else {
         const uint32_t to = lds_at + buf * kBuffer;
-        to_lds(to + (NW * i + wave) * 1088, (const char*)a.k + at_byte, r * kRowBytes + k_off);
-        to_lds(to + kKBytes + (NW * i + wave) * 1024, (const char*)a.v + at_byte, r * kRowBytes + v_off);
+        to_lds(to + (NW * i + wave) * 1088, kp + place[i], k_off[i]);
+        to_lds(to + kKBytes + (NW * i + wave) * 1024, vp + place[i], v_off[i]);
       }
     }
   };
@@ -165,11 +183,10 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
       *(uint4*)(vd + 16) = widen_fp8(make_uint2(v.z, v.w));
     }
   };
-  // bf16 rows: the tile at `at` has arrived (its loads and all in front of them; `behind`: as many tiles as the ring takes have been
-  // requested behind it); the values behind the last row become zeros
-  auto arrived = [&](int at, int buf, bool behind) {
-    if (behind) asm volatile("s_waitcnt vmcnt(%0)" :: "n"((kStages - 2) * 2 * kPasses) : "memory");
-    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  // bf16 rows: a tile has arrived, kStages - 2 others are on their way behind it.  (Behind the last one the last one is asked for
+  // again, so that their number is always the same.)  Values behind the last row become zeros.
+  auto arrived = [&](int at, int buf) {
+    asm volatile("s_waitcnt vmcnt(%0)" :: "n"((kStages - 2) * 2 * kPasses) : "memory");
     __syncthreads();
     if (at + kN > key_hi) {
       u32x4* v = (u32x4*)(lds + buf * kBuffer + kKBytes);
@@ -182,25 +199,25 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
 #pragma unroll
   for (int c = 0; c < kCt; ++c) o[c] = (f32x16)0.0f;
   float mx = -__builtin_inff(), l = 0.0f;
+  constexpr int kFirst = FP8 ? 1 : kStages - 1;      // tiles asked for in front of the loop
   if (key_lo < key_hi) {
     look_up(key_lo);
+#pragma unroll
+    for (int t = 0; t < kFirst; ++t) {
+      make_places(key_lo + t * kN);
+      look_up(key_lo + (t + 1) * kN);
+      request(t);
+    }
+    make_places(key_lo + kFirst * kN);
+    look_up(key_lo + (kFirst + 1) * kN);
     if constexpr (FP8) {
-      request(key_lo, 0);
-      look_up(key_lo + kN);
       stage(key_lo, 0);
-      if (key_lo + kN < key_hi) {
-        request(key_lo + kN, 1);
-        look_up(key_lo + 2 * kN);
-      }
+      request(1);
+      make_places(key_lo + 2 * kN);
+      look_up(key_lo + 3 * kN);
       __syncthreads();
     } else {
-#pragma unroll
-      for (int t = 0; t < kStages - 1; ++t)
-        if (key_lo + t * kN < key_hi) {
-          request(key_lo + t * kN, t);
-          look_up(key_lo + (t + 1) * kN);
-        }
-      arrived(key_lo, 0, key_lo + (kStages - 2) * kN < key_hi);
+      arrived(key_lo, 0);
     }
   }
   // where the lane's operands stand: K's row n32, pieces 2 c + hi; V's rows 4 hi + .., 64-byte stretches c
@@ -216,12 +233,8 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   for (int key = key_lo; key < key_hi; key += kN, buf = buf + 1 < kStages ? buf + 1 : 0) {
     const char* kt = lds + buf * kBuffer;
     const int next = key + kN;
-    const int next_buf = buf + 1 < kStages ? buf + 1 : 0, far = key + (kStages - 1) * kN;
-    if constexpr (!FP8)
-      if (far < key_hi) {
-        request(far, buf > 0 ? buf - 1 : kStages - 1);
-        look_up(far + kN);
-      }
+    const int next_buf = buf + 1 < kStages ? buf + 1 : 0;
+    if constexpr (!FP8) request(buf > 0 ? buf - 1 : kStages - 1);      // in place of the tile in front of this one
     __builtin_amdgcn_s_setprio(1);
     f32x16 s[kKt];
 #pragma unroll
@@ -296,22 +309,23 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
         if (f + kRing < kOperands) read_v(f + kRing);
       }
       if (kb + 1 < kKt * 2) weigh(kb + 1);
+      if (!FP8 && kb == 0) make_places(key + kStages * kN);
+      if (!FP8 && kb == 1) look_up(key + (kStages + 1) * kN);
       if constexpr (kOrdered) order_weighted<kCt>();
     }
     __builtin_amdgcn_s_setprio(0);
     if (next < key_hi) {
       if constexpr (FP8) {
         stage(next, next_buf);
-        if (next + kN < key_hi) {
-          request(next + kN, buf);
-          look_up(next + 2 * kN);
-        }
+        request(0);
+        make_places(next + 2 * kN);
         __syncthreads();
       } else {
-        arrived(next, next_buf, next + (kStages - 2) * kN < key_hi);
+        arrived(next, next_buf);
       }
     }
   }
+  if constexpr (!FP8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing writes to LDS behind the workgroup's end
 
   l = sum_halves(l);
   if (!in) return;
@@ -407,24 +421,29 @@ hipError_t launch_attend_join(const AttendArgs& a, bool f32, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int D, bool FP8, int NW>
+template <int D, bool FP8, bool PAGED, int NW>
 static hipError_t tile_of_width(const AttendArgs& a, hipStream_t st) {
   static LdsOptIn opt;
-  hipError_t e = opt.ensure((const void*)k_attend_tile<D, FP8, NW>, stages<D, FP8, NW>() * buffer_bytes<D, FP8>());
+  const size_t lds = stages<D, FP8, NW>() * buffer_bytes<D, FP8>();
+  hipError_t e = opt.ensure((const void*)k_attend_tile<D, FP8, PAGED, NW>, lds);
   if (e != hipSuccess) return e;
-  k_attend_tile<D, FP8, NW><<<(unsigned)a.plan.grid, NW * 64, stages<D, FP8, NW>() * buffer_bytes<D, FP8>(), st>>>(a);
+  k_attend_tile<D, FP8, PAGED, NW><<<(unsigned)a.plan.grid, NW * 64, lds, st>>>(a);
   e = hipGetLastError();
   if (e != hipSuccess || a.plan.most_pieces == 0) return e;
   return launch_attend_join(a, false, st);
 }
-template <int D, bool FP8>
+template <int D, bool FP8, bool PAGED>
 static hipError_t tile_of_type(const AttendArgs& a, hipStream_t st) {
-  return a.plan.tile_rows == 256 ? tile_of_width<D, FP8, 8>(a, st) : tile_of_width<D, FP8, 4>(a, st);
+  return a.plan.tile_rows == 256 ? tile_of_width<D, FP8, PAGED, 8>(a, st) : tile_of_width<D, FP8, PAGED, 4>(a, st);
 }
 
 hipError_t launch_attend_tile(const AttendArgs& a, const Dims& d, hipStream_t st) {
-  if (d.kv_fp8) return d.D == 128 ? tile_of_type<128, true>(a, st) : tile_of_type<256, true>(a, st);
-  return d.D == 64 ? tile_of_type<64, false>(a, st) : d.D == 128 ? tile_of_type<128, false>(a, st) : tile_of_type<256, false>(a, st);
+  if (d.kv_fp8) return d.D == 128 ? tile_of_type<128, true, false>(a, st) : tile_of_type<256, true, false>(a, st);
+#define EA_CASE(DD) if (d.D == DD) return a.pm.table ? tile_of_type<DD, false, true>(a, st) : tile_of_type<DD, false, false>(a, st)
+  EA_CASE(64);
+  EA_CASE(128);
+#undef EA_CASE
+  return a.pm.table ? tile_of_type<256, false, true>(a, st) : tile_of_type<256, false, false>(a, st);
 }
 
 }  // namespace ea

@@ -39,6 +39,8 @@ static ea_status attend(const Dims& d, const void* q, const ea_step* step, const
   // (workgroups of up to 512 threads, 2^32 threads to a launch)
   const int64_t most = (int64_t)1 << 22;
   if (a.plan.grid > most || (int64_t)d.units() * a.plan.short_rows > most) return EA_ERR_UNSUPPORTED;
+  // (the kernels step over a block by a 32-bit number of bytes)
+  if (pm && (((uint64_t)d.Hkv << pm->sh) * d.D * d.esize()) >> 32) return EA_ERR_UNSUPPORTED;
   if (step->n_tokens == 0) return EA_OK;
   a.q = q; a.k = k; a.v = v; a.cu = step->cu_tokens; a.lens = lengths; a.kscale = kscale; a.vscale = vscale;
   a.out = out; a.lse = lse; a.ws = (char*)ws;
