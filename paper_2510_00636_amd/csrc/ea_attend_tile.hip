@@ -19,11 +19,15 @@ using s16x4 = short __attribute__((ext_vector_type(4)));
 // have rows four banks apart for K, sixteen for V.
 template <int D, bool FP8> constexpr int k_pitch() { return D * 2 + (FP8 ? 16 : 0); }
 template <int D, bool FP8> constexpr int v_pitch() { return D * 2 + (FP8 ? 64 : 0); }
-template <int D> constexpr int tile_keys() { return D == 256 ? 32 : 64; }
-template <int D, bool FP8> constexpr int k_bytes() { return FP8 ? tile_keys<D>() * k_pitch<D, true>() : tile_keys<D>() * D * 2 / 1024 * 1088; }
-// Tiles in LDS at once: one worked on, the others on their way.  As many as fit the workgroups of a CU.
-template <int D, bool FP8, int NW> constexpr int stages() { return FP8 ? 2 : D == 128 && NW == 4 ? 2 : 4; }
-template <int D, bool FP8> constexpr int buffer_bytes() { return k_bytes<D, FP8>() + tile_keys<D>() * v_pitch<D, FP8>(); }
+template <int D, bool FP8, int NW> constexpr int tile_keys() { return D == 256 || (D == 128 && NW == 4 && !FP8) ? 32 : 64; }
+template <int D, bool FP8, int NW> constexpr int k_bytes() {
+  return FP8 ? tile_keys<D, FP8, NW>() * k_pitch<D, true>() : tile_keys<D, FP8, NW>() * D * 2 / 1024 * 1088;
+}
+// Tiles in LDS at once.  bf16: two that are worked on and two on their way, and a barrier for every two: of the two wavefronts on a
+// SIMD one is always ahead (it gets the matrix cores first, and the vector unit while the other has those), and where they meet it
+// waits for the other.  8-bit rows: one of each.
+template <bool FP8> constexpr int stages() { return FP8 ? 2 : 4; }
+template <int D, bool FP8, int NW> constexpr int buffer_bytes() { return k_bytes<D, FP8, NW>() + tile_keys<D, FP8, NW>() * v_pitch<D, FP8>(); }
 // (the row's bits that its place in its KiB and the gap in front of that leave over)
 template <int D> __device__ __forceinline__ int k_piece(int row) { return D == 64 ? row >> 1 & 3 : D == 128 ? row & 3 : (row & 1) | (row >> 2 & 2); }
 template <int D> __device__ __forceinline__ int v_piece(int row) { return D == 64 ? (row >> 1 & 1) * 4 : (row & 3) * 4; }
@@ -70,13 +74,13 @@ __device__ __forceinline__ void order_weighted() {
 template <int D, bool FP8, bool PAGED, int NW>
 __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_attend_tile(AttendArgs a) {
   constexpr int kM = NW * 32;
-  constexpr int kN = tile_keys<D>(), kKt = kN / 32, kSteps = D / 16, kCt = D / 32;
+  constexpr int kN = tile_keys<D, FP8, NW>(), kKt = kN / 32, kSteps = D / 16, kCt = D / 32;
   constexpr int kRowBytes = D * (FP8 ? 1 : 2);
   constexpr int kPer = 1024 / kRowBytes;                 // rows that a wavefront's load covers
   constexpr int kPasses = kN / (NW * kPer);               // of the workgroup's loads over a tile
   constexpr int kChunks = kRowBytes / 16;
-  constexpr int kKPitch = k_pitch<D, FP8>(), kKBytes = k_bytes<D, FP8>(), kVPitch = v_pitch<D, FP8>(), kBuffer = buffer_bytes<D, FP8>();
-  constexpr int kStages = stages<D, FP8, NW>();
+  constexpr int kKPitch = k_pitch<D, FP8>(), kKBytes = k_bytes<D, FP8, NW>(), kVPitch = v_pitch<D, FP8>(), kBuffer = buffer_bytes<D, FP8, NW>();
+  constexpr int kStages = stages<FP8>();
   constexpr bool kOrdered = D < 256;                     // at d = 256 the registers are all taken without an order
   extern __shared__ char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -183,14 +187,14 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
       *(uint4*)(vd + 16) = widen_fp8(make_uint2(v.z, v.w));
     }
   };
-  // bf16 rows: a tile has arrived, kStages - 2 others are on their way behind it.  (Behind the last one the last one is asked for
-  // again, so that their number is always the same.)  Values behind the last row become zeros.
+  // bf16 rows: the tiles at `at` and behind it, buffers `buf` and buf + 1, have arrived.  Values behind the last row become zeros.
   auto arrived = [&](int at, int buf) {
-    asm volatile("s_waitcnt vmcnt(%0)" :: "n"((kStages - 2) * 2 * kPasses) : "memory");
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (at + kN > key_hi) {
-      u32x4* v = (u32x4*)(lds + buf * kBuffer + kKBytes);
-      for (int i = (key_hi - at) * (D / 8) + (int)threadIdx.x; i < kN * (D / 8); i += NW * 64) v[i] = (u32x4)0u;
+    if (at + 2 * kN > key_hi) {
+      const int nth = at + kN < key_hi ? 1 : 0;
+      u32x4* v = (u32x4*)(lds + (buf + nth) * kBuffer + kKBytes);
+      for (int i = (key_hi - at - nth * kN) * (D / 8) + (int)threadIdx.x; i < kN * (D / 8); i += NW * 64) v[i] = (u32x4)0u;
       __syncthreads();
     }
   };
@@ -199,7 +203,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
 #pragma unroll
   for (int c = 0; c < kCt; ++c) o[c] = (f32x16)0.0f;
   float mx = -__builtin_inff(), l = 0.0f;
-  constexpr int kFirst = FP8 ? 1 : kStages - 1;      // tiles asked for in front of the loop
+  constexpr int kFirst = FP8 ? 1 : 2;      // tiles asked for in front of the loop
   if (key_lo < key_hi) {
     look_up(key_lo);
 #pragma unroll
@@ -234,7 +238,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
     const char* kt = lds + buf * kBuffer;
     const int next = key + kN;
     const int next_buf = buf + 1 < kStages ? buf + 1 : 0;
-    if constexpr (!FP8) request(buf > 0 ? buf - 1 : kStages - 1);      // in place of the tile in front of this one
+    if constexpr (!FP8) request(buf ^ 2);                  // the tile behind the next one
     __builtin_amdgcn_s_setprio(1);
     f32x16 s[kKt];
 #pragma unroll
@@ -309,8 +313,8 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
         if (f + kRing < kOperands) read_v(f + kRing);
       }
       if (kb + 1 < kKt * 2) weigh(kb + 1);
-      if (!FP8 && kb == 0) make_places(key + kStages * kN);
-      if (!FP8 && kb == 1) look_up(key + (kStages + 1) * kN);
+      if (!FP8 && kb == 0) make_places(key + 3 * kN);
+      if (!FP8 && kb == 1) look_up(key + 4 * kN);
       if constexpr (kOrdered) order_weighted<kCt>();
     }
     __builtin_amdgcn_s_setprio(0);
@@ -320,7 +324,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
         request(0);
         make_places(next + 2 * kN);
         __syncthreads();
-      } else {
+      } else if (buf & 1) {
         arrived(next, next_buf);
       }
     }
@@ -424,7 +428,7 @@ hipError_t launch_attend_join(const AttendArgs& a, bool f32, hipStream_t st) {
 template <int D, bool FP8, bool PAGED, int NW>
 static hipError_t tile_of_width(const AttendArgs& a, hipStream_t st) {
   static LdsOptIn opt;
-  const size_t lds = stages<D, FP8, NW>() * buffer_bytes<D, FP8>();
+  const size_t lds = stages<FP8>() * buffer_bytes<D, FP8, NW>();
   hipError_t e = opt.ensure((const void*)k_attend_tile<D, FP8, PAGED, NW>, lds);
   if (e != hipSuccess) return e;
   k_attend_tile<D, FP8, PAGED, NW><<<(unsigned)a.plan.grid, NW * 64, lds, st>>>(a);
