@@ -69,19 +69,6 @@ __device__ __forceinline__ int table_entry(const AttendArgs& a, int b, int row) 
   return a.pm.table ? a.pm.table[(size_t)b * a.pm.max_blocks + (row >> a.pm.sh)] : 0;
 }
 
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp_add_int(int x) {
-  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, true);
-}
-// sums of x over the lanes up to and with this one
-__device__ __forceinline__ int wave_prefix(int x) {
-  x = dpp_add_int<0x111, 0xf>(x);
-  x = dpp_add_int<0x112, 0xf>(x);
-  x = dpp_add_int<0x114, 0xf>(x);
-  x = dpp_add_int<0x118, 0xf>(x);
-  x = dpp_add_int<0x142, 0xa>(x);   // the last lane of rows 0 and 2 to rows 1 and 3
-  return dpp_add_int<0x143, 0xc>(x);
-}
 // largest x of the wavefront, of either sign, in every lane
 __device__ __forceinline__ float wave_max_any(float x) {
 #pragma unroll

@@ -21,14 +21,20 @@ namespace {
 
 constexpr int kGroup = kAttendGroup;    // rows of a group: 32 for each wavefront
 
-// the groups of super-unit su (a sequence where heads share a length, else a head): none if it is not this kernel's
-__device__ __forceinline__ int groups_of(const AttendArgs& a, int su) {
+// Super-unit su (a sequence where heads share a length, else a head): its first token, tokens, cached rows and groups (none if it
+// is not this kernel's).
+struct Super { int t0, m, len, grp; };
+__device__ __forceinline__ Super super_unit(const AttendArgs& a, int su, int supers) {
+  Super s = {0, 0, 0, 0};
+  if (su >= supers) return s;
   const int b = a.per_head ? su / a.Hkv : su;
-  const int m = first_token(a, b + 1) - first_token(a, b);
-  if (m < 1 || m * a.G > a.short_rows) return 0;
-  const int len = rows_of(a, b, a.per_head ? su - b * a.Hkv : 0);
-  return len < 1 ? 1 : (len + kGroup - 1) / kGroup;
+  s.len = rows_of(a, b, a.per_head ? su - b * a.Hkv : 0);
+  s.t0 = first_token(a, b);
+  s.m = first_token(a, b + 1) - s.t0;
+  if (s.m >= 1 && s.m * a.G <= a.short_rows) s.grp = s.len < 1 ? 1 : (s.len + kGroup - 1) / kGroup;
+  return s;
 }
+__device__ __forceinline__ int from_lane(int x, int l) { return __builtin_amdgcn_readlane(x, l); }
 
 template <int D, bool FP8>
 struct RowShape {
@@ -90,50 +96,55 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
   const int n16 = lane & 15, g = lane >> 4;
   const int supers = a.per_head ? a.B * a.Hkv : a.B, mult = a.per_head ? 1 : a.Hkv;
 
-  // ---- the share: total of all groups, then the super-unit in which this workgroup's begins
-  int mine = lane < supers ? groups_of(a, lane) : 0;
-  int pre = wave_prefix(mine);
-  int total = last_lane(pre);
-  for (int base = 64; base < supers; base += 64)
-    total += last_lane(wave_prefix(base + lane < supers ? groups_of(a, base + lane) : 0));
-  const long long all = (long long)total * mult;
-  const int per = (int)((all + gridDim.x - 1) / gridDim.x);
-  const long long x0 = (long long)per * blockIdx.x, x1 = x0 + per < all ? x0 + per : all;
-  if (x0 >= x1) return;
+  // ---- the share: total of all groups, then the super-unit in which this workgroup's begins.  A lane holds one of 64 of them.
+  Super mine = super_unit(a, lane, supers);
+  int pre = wave_prefix(mine.grp), total = last_lane(pre), block = 0;
+  for (int base = 64; base < supers; base += 64) total += last_lane(wave_prefix(super_unit(a, base + lane, supers).grp));
+  const long long all = (long long)total * mult, wgs = all < gridDim.x ? all : gridDim.x;
+  if (blockIdx.x >= wgs) return;      // (a head's pieces are those of neighbours: no share in between is empty)
+  // all w / wgs without a 64-bit division where there is none to do
+  const bool small = all < (1ll << 31);
+  const long long each = small ? (long long)((uint32_t)all / (uint32_t)wgs) : all / wgs;
+  const uint32_t extra = (uint32_t)(all - each * wgs);
+  auto share_at = [&](uint32_t w) { return each * w + extra * w / (uint32_t)wgs; };      // extra < wgs <= kAttendShares
+  const long long x0 = share_at(blockIdx.x), x1 = share_at(blockIdx.x + 1);
 
   // ---- a part of a head that falls into the share
   struct Part {
-    int su, have, grp;        // super-unit, groups in front of it, its groups
+    int su, have;             // super-unit, groups in front of it
+    int grp, t0, m, len;      // its groups, first token, tokens, rows
     int b, h, off, take;      // sequence, KV head, first group of the part and how many
-    int t0, m, len;
   };
   long long x = x0;
   auto fill = [&](Part& c) {
-    const int rel = (int)(x - (long long)c.have * mult), hh = rel / c.grp;
+    const int l = c.su - block;
+    c.grp = from_lane(mine.grp, l);
+    c.t0 = from_lane(mine.t0, l);
+    c.m = from_lane(mine.m, l);
+    c.len = from_lane(mine.len, l);
+    const int rel = (int)(x - (long long)c.have * mult), hh = a.per_head ? 0 : rel / c.grp;
     c.off = rel - hh * c.grp;
     c.take = (int)(x1 - x < c.grp - c.off ? x1 - x : c.grp - c.off);
     c.b = a.per_head ? c.su / a.Hkv : c.su;
     c.h = a.per_head ? c.su - c.b * a.Hkv : hh;
-    c.t0 = __builtin_amdgcn_readfirstlane(first_token(a, c.b));
-    c.m = __builtin_amdgcn_readfirstlane(first_token(a, c.b + 1)) - c.t0;
-    c.len = __builtin_amdgcn_readfirstlane(rows_of(a, c.b, c.h));
   };
   Part cur;
   cur.su = -1;
   cur.have = 0;
-  for (int base = 0; base < supers; base += 64) {
-    if (base > 0) pre = wave_prefix(mine = base + lane < supers ? groups_of(a, base + lane) : 0);
+  for (;;) {
     const uint64_t in = __ballot((long long)(cur.have + pre) * mult > x0);
     if (in) {
       const int l = __builtin_ctzll(in);
-      cur.su = base + l;
-      cur.grp = __builtin_amdgcn_readlane(mine, l);
-      cur.have += __builtin_amdgcn_readlane(pre, l) - cur.grp;
+      cur.su = block + l;
+      cur.have += from_lane(pre, l) - from_lane(mine.grp, l);
       break;
     }
     cur.have += last_lane(pre);
+    block += 64;
+    if (block >= supers) return;
+    mine = super_unit(a, block + lane, supers);
+    pre = wave_prefix(mine.grp);
   }
-  if (cur.su < 0) return;
   fill(cur);
 
   // ---- what is in flight: a tile of K and of V, and the next part's queries
@@ -208,12 +219,20 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
     int next_entries = 0;
     bool go_on = x < x1;
     if (go_on) {
-      if (x >= (long long)(cur.have + cur.grp) * mult) {
+      if (x >= (long long)(cur.have + cur.grp) * mult) {      // the next super-unit that has groups
         next.have += cur.grp;
-        do {
-          if (++next.su >= supers) break;
-          next.grp = __builtin_amdgcn_readfirstlane(groups_of(a, next.su));
-        } while (next.grp == 0);
+        ++next.su;
+        for (;;) {
+          const uint64_t some = next.su - block < 64 ? __ballot(mine.grp > 0) >> (next.su - block) : 0;
+          if (some) {
+            next.su += __builtin_ctzll(some);
+            break;
+          }
+          block += 64;
+          next.su = block;
+          if (block >= supers) break;
+          mine = super_unit(a, block + lane, supers);
+        }
         go_on = next.su < supers;
       }
       if (go_on) {
@@ -224,8 +243,14 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
     const int rows = cur.m * a.G, unit = cur.b * a.Hkv + cur.h, len = cur.len;
     const bool whole = cur.take == cur.grp;
     if (cur.off == 0 && tid == 0) {     // the workgroups that the head falls to, from this one on, for the joining launch
-      const int left = (int)(x1 - x), rest = cur.grp - cur.take;
-      ((int2*)(a.ws + a.plan.info))[unit] = make_int2((int)blockIdx.x, left > 0 ? 1 : 1 + (rest + per - 1) / per);
+      int pieces = 1;
+      if (!whole) {     // the last one is the last of those that begin at or in front of its last group
+        const long long end = x - cur.take + cur.grp;
+        int w = (int)blockIdx.x + (int)((cur.grp - cur.take) / (each + 1));
+        while (share_at(w + 1) < end) ++w;
+        pieces = w - (int)blockIdx.x + 1;
+      }
+      ((int2*)(a.ws + a.plan.info))[unit] = make_int2((int)blockIdx.x, pieces);
     }
     const float qk = a.scale * (FP8 && a.kscale ? a.kscale[unit] : 1.0f);
     int vis[MT];            // keys that the row sees

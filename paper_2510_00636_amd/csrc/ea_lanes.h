@@ -44,4 +44,18 @@ __device__ __forceinline__ float wave_max(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add_int(int x) {
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, true);
+}
+// sums of x over the lanes up to and with this one
+__device__ __forceinline__ int wave_prefix(int x) {
+  x = dpp_add_int<0x111, 0xf>(x);
+  x = dpp_add_int<0x112, 0xf>(x);
+  x = dpp_add_int<0x114, 0xf>(x);
+  x = dpp_add_int<0x118, 0xf>(x);
+  x = dpp_add_int<0x142, 0xa>(x);   // the last lane of rows 0 and 2 to rows 1 and 3
+  return dpp_add_int<0x143, 0xc>(x);
+}
+
 }  // namespace ea

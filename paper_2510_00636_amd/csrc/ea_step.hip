@@ -3,6 +3,7 @@
 
 #include <type_traits>
 
+#include "ea_lanes.h"
 #include "ea_step.h"
 
 namespace ea {
@@ -14,7 +15,7 @@ namespace ea {
 // entries in front of the old ends, the list below its old end) is nowhere written, so the launch needs no order within.
 namespace {
 
-constexpr int kTableThreads = 256;
+constexpr int kTableThreads = 256, kTableTokens = 256;
 
 __device__ __forceinline__ int count_le(const int* sums, int n, int x) {     // how many of n ascending sums are <= x
   int lo = 0;
@@ -41,7 +42,7 @@ __global__ __launch_bounds__(kTableThreads) void k_block_tables(BlockTableArgs a
     const long long x = a.len_new[b];
     return x > 0 ? (x + bs - 1) >> a.sh : 0ll;
   };
-  const int per = (a.B + kTableThreads - 1) / kTableThreads, b0 = tid * per, b1 = min(b0 + per, a.B);
+  const int per = (a.B + kTableThreads - 1) / kTableThreads, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
   long long x[3] = {0, 0, 0};
   auto add = [&](int b) {
     const long long held = held_of(b), need = need_of(b), more = (long long)max(a.len_new[b], 0) - max(a.len_old[b], 0);
@@ -53,14 +54,9 @@ __global__ __launch_bounds__(kTableThreads) void k_block_tables(BlockTableArgs a
   long long incl[3];
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
-    long long s = x[i];
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const long long y = __shfl_up(s, d);
-      if (lane >= d) s += y;
-    }
-    if (lane == 63) wave_sum[i][wave] = s;
-    incl[i] = s;
+    // 40 bits (16 sequences of 2^31 each) as two numbers whose sums over a wavefront fit 32
+    incl[i] = ((long long)wave_prefix((int)(x[i] >> 20)) << 20) + wave_prefix((int)(x[i] & 0xfffff));
+    if (lane == 63) wave_sum[i][wave] = incl[i];
   }
   __syncthreads();
 #pragma unroll
@@ -106,22 +102,31 @@ __global__ __launch_bounds__(kTableThreads) void k_block_tables(BlockTableArgs a
     const long long at = count + back - 1 - r;
     if (at < a.num_blocks) a.free_list[at] = given((int)r);
   }
+  // slots and positions: a wavefront takes 256 tokens next to each other, whose first sequence is found once
   const long long tokens = a.n_tokens < total[2] ? a.n_tokens : total[2];
-  for (long long t = first; t < a.n_tokens; t += step) {
-    if (t >= tokens) {
-      a.slots[t] = -1;
-      continue;
+  for (long long t0 = ((long long)blockIdx.x * 4 + wave) * kTableTokens; t0 < a.n_tokens; t0 += (long long)gridDim.x * 4 * kTableTokens) {
+    const int b_first = t0 < tokens ? count_le(tok_to, a.B, (int)t0) : 0;
+    const long long t_last = min(t0 + kTableTokens, tokens) - 1;
+    const int span = t0 < tokens ? b_first + count_le(tok_to + b_first, a.B - b_first, (int)t_last) - b_first + 1 : 0;
+#pragma unroll
+    for (int k = 0; k < kTableTokens / 64; ++k) {
+      const long long t = t0 + k * 64 + lane;
+      if (t >= a.n_tokens) break;
+      if (t >= tokens) {
+        a.slots[t] = -1;
+        continue;
+      }
+      const int b = b_first + count_le(tok_to + b_first, span, (int)t);
+      const long long i = t - (b > 0 ? tok_to[b - 1] : 0), old = max(a.len_old[b], 0), row = old + i, j = row >> a.sh, held = held_of(b);
+      long long slot = -1;
+      if (served(b)) {
+        const long long block = j < held ? a.table[(long long)b * a.max_blocks + j]
+                                         : block_taken((b > 0 ? want_to[b - 1] : 0) + (j - held));
+        slot = (block << a.sh) + (row & (bs - 1));
+      }
+      a.slots[t] = slot;
+      a.pos[t] = (int)((a.seen ? (long long)a.seen[b] : old) + i);
     }
-    const int b = count_le(tok_to, a.B, (int)t);
-    const long long i = t - (b > 0 ? tok_to[b - 1] : 0), old = max(a.len_old[b], 0), row = old + i, j = row >> a.sh, held = held_of(b);
-    long long slot = -1;
-    if (served(b)) {
-      const long long block = j < held ? a.table[(long long)b * a.max_blocks + j]
-                                       : block_taken((b > 0 ? want_to[b - 1] : 0) + (j - held));
-      slot = (block << a.sh) + (row & (bs - 1));
-    }
-    a.slots[t] = slot;
-    a.pos[t] = (int)((a.seen ? (long long)a.seen[b] : old) + i);
   }
   if (blockIdx.x == 0) {
     for (int b = tid; b < a.B; b += kTableThreads) {
@@ -137,10 +142,11 @@ __global__ __launch_bounds__(kTableThreads) void k_block_tables(BlockTableArgs a
 }
 
 hipError_t launch_block_tables(const BlockTableArgs& a, hipStream_t st) {
-  long long wgs = (a.n_tokens + 511) / 512;
-  const long long moved = (a.num_blocks + 8191) / 8192;
+  // a workgroup per 1024 tokens, or per 2048 blocks that may move
+  long long wgs = (a.n_tokens + 4 * kTableTokens - 1) / (4 * kTableTokens);
+  const long long blocks = (long long)a.B * a.max_blocks, moved = ((blocks < a.num_blocks ? blocks : a.num_blocks) + 2047) / 2048;
   if (wgs < moved) wgs = moved;
-  wgs = wgs < 1 ? 1 : wgs > 128 ? 128 : wgs;
+  wgs = wgs < 1 ? 1 : wgs > 512 ? 512 : wgs;
   k_block_tables<<<(unsigned)wgs, kTableThreads, (size_t)a.B * 3 * sizeof(int), st>>>(a);
   return hipGetLastError();
 }
