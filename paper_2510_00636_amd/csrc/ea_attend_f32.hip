@@ -1,17 +1,23 @@
 // Attention over fp32 caches: everything in fp32, on v_mfma_f32_16x16x4_f32.
 //
-// A workgroup takes 16 (token, head) rows of a KV head, its four wavefronts every fourth 16 keys.  A lane loads 16 bytes of a key
-// (channels 16 s + 4 g ..) and of four values (channels 4 i ..): both products take their contraction, and the second its
-// channels, in the order that such loads bring them, so nothing is staged.
+// A wavefront takes 16 (token, head) rows of a KV head and 16 keys at a time.  A lane loads 16 bytes of a key (channels 16 s + 4 g ..)
+// and of four values (channels 4 i ..): both products take their contraction, and the second its channels, in the order that such
+// loads bring them, so nothing is staged.  Where there are rows enough for the chip, the four wavefronts of a workgroup have 16 of them
+// each and walk the same keys, which come to them out of the L1 cache; else all have the same rows and every eighth (d = 256: fourth)
+// 16 keys, and put their results together through LDS.
 #include "ea_attend.h"
 
 namespace ea {
 
-template <int D>
-__global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_f32(AttendArgs a) {
-  constexpr int kSteps = D / 16, kLoads = D / 64, kM = kAttendF32Rows;
-  __shared__ float pass_o[2][D / 4][64];
-  __shared__ float pass_ml[4][2][kM];
+namespace {
+template <int D, bool KEYS> constexpr int f32_waves() { return KEYS && D < 256 ? 8 : 4; }
+template <int D, bool KEYS> constexpr int f32_rows() { return KEYS ? kAttendF32Rows : kAttendF32LongRows; }
+}  // namespace
+
+template <int D, bool KEYS>
+__global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) void k_attend_f32(AttendArgs a) {
+  constexpr int kSteps = D / 16, kLoads = D / 64, kM = f32_rows<D, KEYS>(), kNW = f32_waves<D, KEYS>(), kPitch = D + 4;
+  extern __shared__ float pass_o[];          // KEYS: [wavefront][row][channel], and behind it maxima and sums
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, g = lane >> 4;
   const Piece piece = find_piece<kM>(a, blockIdx.x);
@@ -26,9 +32,10 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_f32(AttendAr
     if (key_lo >= key_hi) return;
     key_hi = min(key_hi, key_lo + piece.chunk);
   }
-  const int row = row0 + n16, tok = row / a.G, hd = row - tok * a.G;
+  const int my_rows = row0 + (KEYS ? 0 : wave * 16);
+  const int row = my_rows + n16, tok = row / a.G, hd = row - tok * a.G;
   const bool in = row < rows;
-  const int vis = in ? len - (m - 1 - tok) : len, vis_min = len - (m - 1 - row0 / a.G);
+  const int vis = in ? len - (m - 1 - tok) : len, vis_min = len - (m - 1 - my_rows / a.G);
   float4 q[kSteps];
   {
     const float* src = (const float*)a.q + (long long)(t0 + (in ? tok : 0)) * a.q_stride + (h * a.G + (in ? hd : 0)) * D;
@@ -45,21 +52,28 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_f32(AttendAr
 #pragma unroll
   for (int c = 0; c < D / 16; ++c) o[c] = (f32x4)0.0f;
   float mx = -__builtin_inff(), l = 0.0f;
-  for (int key = key_lo + wave * 16; key < key_hi; key += 64) {
-    float4 k[kSteps], v[4][kLoads];
+  // the next keys are on their way from the products that took the last ones on, and so the next values
+  float4 k[kSteps], v[4][kLoads];
+  auto load_k = [&](int key) {
     const long long kr = (long long)min(key + n16, key_hi - 1) * D;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) k[s] = *(const float4*)(kp + kr + s * 16);
+  };
+  auto load_v = [&](int key) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int vk = key + 4 * g + r;
-      const long long vr = (long long)min(vk, key_hi - 1) * D;
+      const long long vr = (long long)min(key + 4 * g + r, key_hi - 1) * D;
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        v[r][u] = *(const float4*)(vp + vr + u * 64);
-        if (vk >= key_hi) v[r][u] = make_float4(0, 0, 0, 0);
-      }
+      for (int u = 0; u < kLoads; ++u) v[r][u] = *(const float4*)(vp + vr + u * 64);
     }
+  };
+  const int first = key_lo + (KEYS ? wave * 16 : 0), stride = KEYS ? kNW * 16 : 16;
+  if (first < key_hi) {
+    load_k(first);
+    load_v(first);
+  }
+  for (int key = first; key < key_hi; key += stride) {
+    const bool more = key + stride < key_hi;
     f32x4 s0 = (f32x4)0.0f, s1 = (f32x4)0.0f;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
@@ -68,6 +82,8 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_f32(AttendAr
       s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[s].z, q[s].z, s0, 0, 0, 0);
       s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(k[s].w, q[s].w, s1, 0, 0, 0);
     }
+    if (more) load_k(key + stride);
+    __builtin_amdgcn_sched_barrier(0);
     s0 += s1;
     s0 *= a.scale;
     if (key + 16 > vis_min || key + 16 > key_hi)
@@ -90,6 +106,12 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_f32(AttendAr
       p[r] = pow2(s0[r] - from);
       l += p[r];
     }
+    if (key + 16 > key_hi)      // rows behind the last one weigh nothing, whatever they hold
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u)
+          if (key + 4 * g + r >= key_hi) v[r][u] = make_float4(0, 0, 0, 0);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -99,68 +121,81 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void k_attend_f32(AttendAr
         o[u * 4 + 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][u].z, p[r], o[u * 4 + 2], 0, 0, 0);
         o[u * 4 + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[r][u].w, p[r], o[u * 4 + 3], 0, 0, 0);
       }
+    if (more) load_v(key + stride);
+    __builtin_amdgcn_sched_barrier(0);
   }
-  // ---- the four wavefronts' results, as in the row kernel
   l = sum_xor16(sum_halves(l));
-  if (g == 0) {
-    pass_ml[wave][0][n16] = mx;
-    pass_ml[wave][1][n16] = l;
-  }
-  __syncthreads();
-  const float top = fmaxf(fmaxf(pass_ml[0][0][n16], pass_ml[1][0][n16]), fmaxf(pass_ml[2][0][n16], pass_ml[3][0][n16]));
-  const float from = top == -__builtin_inff() ? 0.0f : top;
-  float sum = 0.0f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) sum += pass_ml[w][1][n16] * pow2(pass_ml[w][0][n16] - from);
-  const float f = pow2(mx - from);
-#pragma unroll
-  for (int c = 0; c < D / 16; ++c) o[c] *= f;
-  if (wave >= 2)
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) pass_o[wave - 2][c * 4 + r][lane] = o[c][r];
-  __syncthreads();
-  if (wave < 2)
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        o[c][r] += pass_o[wave][c * 4 + r][lane];
-        if (wave == 1) pass_o[1][c * 4 + r][lane] = o[c][r];
-      }
-  __syncthreads();
-  if (wave != 0 || !in) return;
-  const long long at = (long long)(t0 + tok) * a.Hq + h * a.G + hd;
-  const long long slot = (long long)blockIdx.x * kM + n16;
-  const bool whole = piece.nsplit == 1, any = sum > 0.0f || sum != sum;
-  float* dst = whole ? (float*)a.out + at * D : (float*)(a.ws + a.plan.split_o) + slot * D;
-  const float by = !whole ? 1.0f : 1.0f / sum;
   // channel u 64 + (4 g + r) 4 + j of row n16 is o[u 4 + j][r]
-#pragma unroll
-  for (int u = 0; u < kLoads; ++u)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float4 x = make_float4(0, 0, 0, 0);
-      const int c = u * 4;
-      if (!whole || any)
-        x = make_float4((o[c][r] + pass_o[1][c * 4 + r][lane]) * by, (o[c + 1][r] + pass_o[1][c * 4 + 4 + r][lane]) * by,
-                        (o[c + 2][r] + pass_o[1][c * 4 + 8 + r][lane]) * by, (o[c + 3][r] + pass_o[1][c * 4 + 12 + r][lane]) * by);
-      *(float4*)(dst + u * 64 + (4 * g + r) * 4) = x;
+  const bool whole = piece.nsplit == 1;
+  auto store = [&](int r, int c4, float top, float sum, float4 x) {      // four channels of a row of the tile
+    const int rw = row0 + r, tk = rw / a.G;
+    const bool any = sum > 0.0f || sum != sum;
+    const float by = 1.0f / sum;
+    const long long at = (long long)(t0 + tk) * a.Hq + h * a.G + (rw - tk * a.G), slot = (long long)blockIdx.x * kM + r;
+    if (whole) {
+      *(float4*)((float*)a.out + at * D + c4) = any ? make_float4(x.x * by, x.y * by, x.z * by, x.w * by) : make_float4(0, 0, 0, 0);
+      if (a.lse && c4 == 0) a.lse[at] = natural_lse(top, sum);
+    } else {
+      *(float4*)((float*)(a.ws + a.plan.split_o) + slot * D + c4) = x;
+      if (c4 == 0) ((float2*)(a.ws + a.plan.split_ml))[slot] = make_float2(top, sum);
     }
-  if (g == 0) {
-    if (!whole) ((float2*)(a.ws + a.plan.split_ml))[slot] = make_float2(top, sum);
-    else if (a.lse) a.lse[at] = natural_lse(top, sum);
+  };
+  if constexpr (!KEYS) {
+    if (!in) return;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        store(row - row0, u * 64 + (4 * g + r) * 4, mx, l, make_float4(o[u * 4][r], o[u * 4 + 1][r], o[u * 4 + 2][r], o[u * 4 + 3][r]));
+  } else {
+    float2* pass_ml = (float2*)(pass_o + kNW * kM * kPitch);
+    if (g == 0) pass_ml[wave * kM + n16] = make_float2(mx, l);
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *(float4*)(pass_o + (wave * kM + n16) * kPitch + u * 64 + (4 * g + r) * 4) =
+            make_float4(o[u * 4][r], o[u * 4 + 1][r], o[u * 4 + 2][r], o[u * 4 + 3][r]);
+    __syncthreads();
+    constexpr int kLanes = D / 4;
+    for (int i = threadIdx.x; i < min(kM, rows - row0) * kLanes; i += kNW * 64) {
+      const int r = i / kLanes, c4 = i % kLanes * 4;
+      float top = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kNW; ++w) top = fmaxf(top, pass_ml[w * kM + r].x);
+      const float from = top == -__builtin_inff() ? 0.0f : top;
+      float4 acc = make_float4(0, 0, 0, 0);
+#pragma unroll
+      for (int w = 0; w < kNW; ++w) {
+        const float2 ml = pass_ml[w * kM + r];
+        const float f = pow2(ml.x - from);
+        const float4 y = *(const float4*)(pass_o + (w * kM + r) * kPitch + c4);
+        sum += ml.y * f;
+        acc.x += y.x * f; acc.y += y.y * f; acc.z += y.z * f; acc.w += y.w * f;
+      }
+      store(r, c4, top, sum, acc);
+    }
   }
 }
 
-hipError_t launch_attend_f32(const AttendArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)a.plan.grid;
-  if (a.D == 64) k_attend_f32<64><<<grid, 256, 0, st>>>(a);
-  else if (a.D == 128) k_attend_f32<128><<<grid, 256, 0, st>>>(a);
-  else k_attend_f32<256><<<grid, 256, 0, st>>>(a);
-  const hipError_t e = hipGetLastError();
+template <int D, bool KEYS>
+static hipError_t f32_of_shape(const AttendArgs& a, hipStream_t st) {
+  static LdsOptIn opt;
+  constexpr int kNW = f32_waves<D, KEYS>(), kM = f32_rows<D, KEYS>();
+  const size_t lds = KEYS ? (size_t)kNW * kM * (D + 4 + 2) * sizeof(float) : 0;
+  hipError_t e = opt.ensure((const void*)k_attend_f32<D, KEYS>, lds);
+  if (e != hipSuccess) return e;
+  k_attend_f32<D, KEYS><<<(unsigned)a.plan.grid, kNW * 64, lds, st>>>(a);
+  e = hipGetLastError();
   return e != hipSuccess || a.plan.most_pieces == 0 ? e : launch_attend_join(a, true, st);
+}
+
+hipError_t launch_attend_f32(const AttendArgs& a, hipStream_t st) {
+#define EA_CASE(DD) if (a.D == DD) return a.plan.tile_rows == kAttendF32Rows ? f32_of_shape<DD, true>(a, st) : f32_of_shape<DD, false>(a, st)
+  EA_CASE(64);
+  EA_CASE(128);
+#undef EA_CASE
+  return a.plan.tile_rows == kAttendF32Rows ? f32_of_shape<256, true>(a, st) : f32_of_shape<256, false>(a, st);
 }
 
 }  // namespace ea

@@ -56,7 +56,7 @@ struct PageMap {
 
 // Attention of a step's tokens: how a call is cut, and where its workspace holds what.
 constexpr int kAttendGroup = 128;       // keys of a group of the row kernel, whose workgroups take whole ones
-constexpr int kAttendF32Rows = 16;      // and of the fp32 kernel
+constexpr int kAttendF32Rows = 16, kAttendF32LongRows = 64;      // (token, head) rows of a workgroup of the fp32 kernel
 constexpr int kAttendShares = 512;      // most workgroups of the row kernel
 constexpr int64_t kAttendMaxTokens = (int64_t)1 << 24;
 struct AttendPlan {

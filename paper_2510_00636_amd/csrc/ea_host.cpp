@@ -342,13 +342,15 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   a.rows = !f32 && a.short_rows >= d.G && (most <= a.piece_rows || d.B > 1);
   a.tile = f32 || most > a.piece_rows;
   a.shares = 2 * num_cu < kAttendShares ? 2 * num_cu : kAttendShares;
-  a.tile_rows = f32 ? kAttendF32Rows : most > 128 ? 256 : 128;
+  // fp32: wavefronts over rows where those give every CU a workgroup, else over keys
+  if (!f32) a.tile_rows = most > 128 ? 256 : 128;
+  else a.tile_rows = most >= kAttendF32LongRows && n_tokens * d.G / kAttendF32LongRows * d.Hkv >= num_cu ? kAttendF32LongRows : kAttendF32Rows;
   // a sequence's last tile may be short: one more for each
   const int64_t tiles = n_tokens * d.G / a.tile_rows + d.B, slots = a.tile_rows == 256 ? num_cu : 2 * (int64_t)num_cu;
   a.grid = tiles * d.Hkv;
   a.per_slot = 1.0f / (float)slots;
   // more rounds of whole tiles than this share out the chip well enough
-  if (n_tokens * d.G / a.tile_rows * d.Hkv < 4 * slots && n > 64) {
+  if (n_tokens * d.G / a.tile_rows * d.Hkv < 4 * slots && n > 256) {
     a.most_pieces = (int)(2 * slots);
     if (a.grid < a.most_pieces) a.grid = a.most_pieces;
   }
