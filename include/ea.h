@@ -353,13 +353,14 @@ ea_status ea_append_fp8(const ea_params* p, const ea_new_rows* rows, const int32
  * sequence b in the step, token i (0 .. m-1) of query head g sees the rows j < len - (m - 1 - i) of its KV
  * head h, len = lengths[b] (paged) or lengths[b, h]:
  *   out = sum_j softmax_j(q . k_j / sqrt(d)) v_j,   lse = ln sum_j exp(q . k_j / sqrt(d)).
- * A token that sees no row gets zeros and -inf.  Rows from len on are never looked at, whatever they hold.
+ * A token that sees no row gets zeros and -inf.  Rows that a token does not see do not touch its results,
+ * whatever they hold; a value that is not finite in a row that it does see makes its channel not finite.
  *   q, out [n_tokens, Hq, d] in p->dtype (q_stride in the step, out dense), lse [n_tokens, Hq] fp32 or NULL
  *   n      no length is larger (HOST; larger ones count as n); 0 <= n <= 2^26
  * ea_attend: contiguous caches, bf16 or fp32; ea_attend_paged: bf16 pools; ea_attend_fp8: e4m3 bytes with
  * per-head scales as in ea_score_fp8 (q and out bf16, head_dim 128 or 256).
- * bf16: products of the bf16 values with fp32 sums; weights reach the second product as bf16 numbers,
- * sums and maxima stay fp32.  fp32: everything in fp32.
+ * bf16: products of the bf16 values with fp32 sums; weights reach the second product as bf16 numbers (where
+ * a sequence adds few tokens as the sum of two), sums and maxima stay fp32.  fp32: everything in fp32.
  * The result does not depend on n_tokens, but how a long head is cut, and so the last bits, may depend on
  * n, max_new and n_tokens.  Same call, same bits.  `ws`: ea_attend_workspace_bytes(), 256-byte aligned, the
  * rules of the other calls; that function returns 0 for invalid arguments and at least 256 otherwise.

@@ -57,7 +57,7 @@ __device__ __forceinline__ uint4 widen_fp8(uint2 w) {
   return make_uint4(lo(w.x), hi(w.x), lo(w.y), hi(w.y));
 }
 
-// Where row `row` (a multiple of 16, so that its 16 rows lie in one block) of unit (b, h) starts, in rows of the cache tensor.
+// Where row `row` of unit (b, h) starts, in rows of the cache tensor (the 16 rows from a multiple of 16 on lie in one block).
 // entry: the block's table entry (paged).
 __device__ __forceinline__ long long row_base(const AttendArgs& a, int b, int h, int row, int entry) {
   if (!a.pm.table) return ((long long)b * a.Hkv + h) * a.n_cap + row;
@@ -190,6 +190,43 @@ __device__ __forceinline__ Piece find_piece(const AttendArgs& a, int index) {
 // where the rows of a piece's partial result stand, and what the joining launch needs to find them
 __device__ __forceinline__ void note_cuts(const AttendArgs& a, const Piece& p, int index) {
   if (a.plan.most_pieces > 0 && p.first && threadIdx.x == 0) ((int4*)(a.ws + a.plan.cuts))[p.b] = make_int4(index, p.nsplit, p.chunk, p.tiles);
+}
+
+// ---- Values that a row does not see.  Behind the last cached row they are taken for zeros; but a step's own rows are seen by some of
+// its tokens and not by others, and a weight of zero times an infinity or a NaN there is a NaN.  So where such rows stand, values
+// that are not finite are taken for zeros too, and the kernel remembers that there was one: then, at the end, every row is given
+// those that it does see (their weights are positive, so what comes of them is the value itself).
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+// the bf16 pair w without its numbers that are not finite; `any` is set where there was one
+__device__ __forceinline__ uint32_t finite_pair(uint32_t w, bool& any) {
+  const bool lo = (w & 0x7f80u) == 0x7f80u, hi = (w & 0x7f800000u) == 0x7f800000u;
+  any |= lo || hi;
+  return (lo ? 0u : w & 0xffffu) | (hi ? 0u : w & 0xffff0000u);
+}
+// adds to x the four values at `channel` of rows lo .. hi - 1 that are not finite; kind 0 bf16, 1 e4m3, 2 fp32
+template <int D, int KIND>
+__device__ __forceinline__ void add_not_finite(const AttendArgs& a, int b, int h, int lo, int hi, int channel, float* x) {
+  for (int key = lo; key < hi; ++key) {
+    const long long at = row_base(a, b, h, key, table_entry(a, b, key)) * D + channel;
+    float v[4];
+    if constexpr (KIND == 2) {
+      const float4 w = *(const float4*)((const float*)a.v + at);
+      v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+    } else {
+      uint2 w;
+      if constexpr (KIND == 1) {
+        const uint4 t = widen_fp8(make_uint2(*(const uint32_t*)((const char*)a.v + at), 0u));
+        w = make_uint2(t.x, t.y);
+      } else {
+        w = *(const uint2*)((const __bf16*)a.v + at);
+      }
+      v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u);
+      v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (not_finite(v[i])) x[i] += v[i];
+  }
 }
 
 // base-2 logarithm of a row's sum and maximum -> natural log-sum-exp; -inf for a row that saw nothing

@@ -17,7 +17,7 @@ template <int D, bool KEYS> constexpr int f32_rows() { return KEYS ? kAttendF32R
 template <int D, bool KEYS>
 __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) void k_attend_f32(AttendArgs a) {
   constexpr int kSteps = D / 16, kLoads = D / 64, kM = f32_rows<D, KEYS>(), kNW = f32_waves<D, KEYS>(), kPitch = D + 4;
-  extern __shared__ float pass_o[];          // KEYS: [wavefront][row][channel], and behind it maxima and sums
+  extern __shared__ __attribute__((aligned(16))) float pass_o[];          // KEYS: [wavefront][row][channel], and behind it maxima and sums
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, g = lane >> 4;
   const Piece piece = find_piece<kM>(a, blockIdx.x);
@@ -32,6 +32,8 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
     if (key_lo >= key_hi) return;
     key_hi = min(key_hi, key_lo + piece.chunk);
   }
+  const int all_see = len - (m - 1 - row0 / a.G);        // rows from here on some of the tile's tokens do not see
+  bool bad = false;                                     // one of those has a value that is not finite
   const int my_rows = row0 + (KEYS ? 0 : wave * 16);
   const int row = my_rows + n16, tok = row / a.G, hd = row - tok * a.G;
   const bool in = row < rows;
@@ -106,12 +108,19 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
       p[r] = pow2(s0[r] - from);
       l += p[r];
     }
-    if (key + 16 > key_hi)      // rows behind the last one weigh nothing, whatever they hold
+    // rows behind the last one weigh nothing, whatever they hold
+    if (key + 16 > (all_see < key_hi ? all_see : key_hi))
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u)
-          if (key + 4 * g + r >= key_hi) v[r][u] = make_float4(0, 0, 0, 0);
+        for (int u = 0; u < kLoads; ++u) {
+          const bool there = key + 4 * g + r < key_hi, some = key + 4 * g + r >= all_see;
+          auto tame = [&](float& x) {
+            if (there && some && not_finite(x)) bad = true;
+            if (!there || (some && not_finite(x))) x = 0.0f;
+          };
+          tame(v[r][u].x); tame(v[r][u].y); tame(v[r][u].z); tame(v[r][u].w);
+        }
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -127,8 +136,14 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
   l = sum_xor16(sum_halves(l));
   // channel u 64 + (4 g + r) 4 + j of row n16 is o[u 4 + j][r]
   const bool whole = piece.nsplit == 1;
+  bool one_bad = false;
   auto store = [&](int r, int c4, float top, float sum, float4 x) {      // four channels of a row of the tile
     const int rw = row0 + r, tk = rw / a.G;
+    if (one_bad) {
+      float y[4] = {x.x, x.y, x.z, x.w};
+      add_not_finite<D, 2>(a, b, h, max(max(all_see, key_lo), 0), min(len - (m - 1 - tk), key_hi), c4, y);
+      x = make_float4(y[0], y[1], y[2], y[3]);
+    }
     const bool any = sum > 0.0f || sum != sum;
     const float by = 1.0f / sum;
     const long long at = (long long)(t0 + tk) * a.Hq + h * a.G + (rw - tk * a.G), slot = (long long)blockIdx.x * kM + r;
@@ -141,6 +156,7 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
     }
   };
   if constexpr (!KEYS) {
+    one_bad = __any(bad);      // of the wavefront, whose rows are its own
     if (!in) return;
 #pragma unroll
     for (int u = 0; u < kLoads; ++u)
@@ -156,7 +172,7 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
       for (int r = 0; r < 4; ++r)
         *(float4*)(pass_o + (wave * kM + n16) * kPitch + u * 64 + (4 * g + r) * 4) =
             make_float4(o[u * 4][r], o[u * 4 + 1][r], o[u * 4 + 2][r], o[u * 4 + 3][r]);
-    __syncthreads();
+    one_bad = __syncthreads_or(bad);
     constexpr int kLanes = D / 4;
     for (int i = threadIdx.x; i < min(kM, rows - row0) * kLanes; i += kNW * 64) {
       const int r = i / kLanes, c4 = i % kLanes * 4;

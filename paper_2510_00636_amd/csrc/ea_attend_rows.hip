@@ -89,9 +89,10 @@ template <int D, bool FP8, int MT>
 __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(AttendArgs a) {
   using S = RowShape<D, FP8>;
   constexpr int kM = 16 * MT, kPitch = D + 4;
-  extern __shared__ float lds[];
+  extern __shared__ __attribute__((aligned(16))) float lds[];
   float* pass_o = lds;
   float2* pass_ml = (float2*)(lds + 4 * kM * kPitch);
+  __shared__ int bad[2];   // a value that is not finite in a row that some of the part's tokens do not see: this part's, the next one's
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n16 = lane & 15, g = lane >> 4;
   const int supers = a.per_head ? a.B * a.Hkv : a.B, mult = a.per_head ? 1 : a.Hkv;
@@ -211,8 +212,10 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
   };
   entries = entries_of(cur, cur.off * kGroup + wave * 32);
   begin(cur);
+  if (tid == 0) bad[0] = 0;
+  __syncthreads();
 
-  for (;;) {
+  for (int parity = 0;; parity ^= 1) {
     x += cur.take;
     // ---- the part behind this one, and the entries of its blocks
     Part next = cur;
@@ -259,6 +262,7 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
       const int row = t * 16 + n16, tok = row / a.G;
       vis[t] = row < rows ? len - (cur.m - 1 - tok) : len;
     }
+    bool any_bad = false;
     f32x4 o[MT][S::kTiles];
     float mx[MT], l[MT];
 #pragma unroll
@@ -342,9 +346,13 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
         for (int j = 0; j < 8; ++j) {
           widen_piece<D, FP8>(vraw[j][u], w[j]);
           // rows behind the last one weigh nothing, whatever they hold
-          if (row + 32 > len && row + (j >> 2) * 16 + 4 * g + (j & 3) >= len)
+          const int key = row + (j >> 2) * 16 + 4 * g + (j & 3);
+          if (row + 32 > len && key >= len)
 #pragma unroll
             for (int c = 0; c < S::kCpl / 2; ++c) w[j][c] = 0u;
+          if (cur.m > 1 && ragged && key >= len - (cur.m - 1))
+#pragma unroll
+            for (int c = 0; c < S::kCpl / 2; ++c) w[j][c] = finite_pair(w[j][c], any_bad);
         }
 #pragma unroll
         for (int c = 0; c < S::kCpl; ++c) {
@@ -392,7 +400,9 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
             }
       }
     }
+    if (any_bad) bad[parity] = 1;
     __syncthreads();
+    if (tid == 0) bad[parity ^ 1] = 0;      // nobody looks at it until the next barrier
     // slot 0 of a workgroup: a head that began in front of it; slot 1: one that goes on behind it
     const long long slot = ((long long)blockIdx.x * 2 + (cur.off == 0 ? 1 : 0)) * kM;
     float* part_o = (float*)(a.ws + a.plan.part_o) + slot * D;
@@ -412,6 +422,12 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
         const float4 y = *(const float4*)(pass_o + (w * kM + r) * kPitch + c4);
         sum += ml[w].y * f;
         acc.x += y.x * f; acc.y += y.y * f; acc.z += y.z * f; acc.w += y.w * f;
+      }
+      if (bad[parity]) {
+        float y[4] = {acc.x, acc.y, acc.z, acc.w};
+        const int seen = len - (cur.m - 1 - r / a.G);
+        add_not_finite<D, FP8 ? 1 : 0>(a, cur.b, cur.h, max(max(len - (cur.m - 1), cur.off * kGroup), 0), min(seen, row_hi), c4, y);
+        acc = make_float4(y[0], y[1], y[2], y[3]);
       }
       if (whole) {
         write_row<D>(a, cur.t0, cur.h, unit, r, c4, top, sum, acc);

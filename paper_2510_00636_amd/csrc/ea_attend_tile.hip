@@ -82,7 +82,7 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
   constexpr int kKPitch = k_pitch<D, FP8>(), kKBytes = k_bytes<D, FP8, NW>(), kVPitch = v_pitch<D, FP8>(), kBuffer = buffer_bytes<D, FP8, NW>();
   constexpr int kStages = stages<FP8>();
   constexpr bool kOrdered = D < 256;                     // at d = 256 the registers are all taken without an order
-  extern __shared__ char lds[];
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n32 = lane & 31, hi = lane >> 5;
 
@@ -100,6 +100,9 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
     key_hi = min(key_hi, key_lo + piece.chunk);
   }
   const int unit = b * a.Hkv + h;
+  const int all_see = len - (m - 1 - row0 / a.G);        // rows from here on some of the tile's tokens do not see
+  __shared__ int bad;                                   // one of those has a value that is not finite
+  if (threadIdx.x == 0) bad = 0;
 
   const int row = row0 + wave * 32 + n32, tok = row / a.G, hd = row - tok * a.G;
   const bool in = row < rows;
@@ -172,29 +175,38 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
       }
     }
   };
-  // 8-bit rows: from registers to LDS, those behind the last one as zeros, which weigh nothing whatever stood there
-  auto stage = [&](int at, int buf) {
+  // 8-bit rows: from registers to LDS
+  auto stage = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < (FP8 ? kPasses : 0); ++i) {
       const int r = (NW * i) * kPer + my_row;
-      const uint32_t keep = at + r >= key_hi ? 0u : ~0u;
-      const u32x4 v = vraw[i] & keep;
       char* kd = lds + buf * kBuffer + r * kKPitch + my_piece * 32;
       char* vd = lds + buf * kBuffer + kKBytes + r * kVPitch + my_piece * 32;
       *(uint4*)kd = widen_fp8(make_uint2(kraw[i].x, kraw[i].y));
       *(uint4*)(kd + 16) = widen_fp8(make_uint2(kraw[i].z, kraw[i].w));
-      *(uint4*)vd = widen_fp8(make_uint2(v.x, v.y));
-      *(uint4*)(vd + 16) = widen_fp8(make_uint2(v.z, v.w));
+      *(uint4*)vd = widen_fp8(make_uint2(vraw[i].x, vraw[i].y));
+      *(uint4*)(vd + 16) = widen_fp8(make_uint2(vraw[i].z, vraw[i].w));
     }
   };
-  // bf16 rows: the tiles at `at` and behind it, buffers `buf` and buf + 1, have arrived.  Values behind the last row become zeros.
+  // The tiles from `at` on, kRound of them from buffer `buf`, stand in LDS where all wavefronts see them.  Values behind the last row
+  // become zeros there, and of those that not all tokens see the ones that are not finite.
+  constexpr int kRound = FP8 ? 1 : 2;
   auto arrived = [&](int at, int buf) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (!FP8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (at + 2 * kN > key_hi) {
-      const int nth = at + kN < key_hi ? 1 : 0;
-      u32x4* v = (u32x4*)(lds + (buf + nth) * kBuffer + kKBytes);
-      for (int i = (key_hi - at - nth * kN) * (D / 8) + (int)threadIdx.x; i < kN * (D / 8); i += NW * 64) v[i] = (u32x4)0u;
+    if (at + kRound * kN > (all_see < key_hi ? all_see : key_hi)) {
+      bool any = false;
+      for (int i = threadIdx.x; i < kRound * kN * (D / 8); i += NW * 64) {
+        const int nth = i / (kN * (D / 8)), in_tile = i % (kN * (D / 8)), row = in_tile / (D / 8), r = at + nth * kN + row;
+        u32x4* v = (u32x4*)(lds + (buf + nth) * kBuffer + kKBytes + row * kVPitch) + in_tile % (D / 8);
+        if (r >= key_hi) {
+          *v = (u32x4)0u;
+        } else if (r >= all_see) {
+          const u32x4 w = *v;
+          *v = u32x4{finite_pair(w.x, any), finite_pair(w.y, any), finite_pair(w.z, any), finite_pair(w.w, any)};
+        }
+      }
+      if (any) bad = 1;
       __syncthreads();
     }
   };
@@ -215,14 +227,11 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
     make_places(key_lo + kFirst * kN);
     look_up(key_lo + (kFirst + 1) * kN);
     if constexpr (FP8) {
-      stage(key_lo, 0);
+      stage(0);
       request(1);
       make_places(key_lo + 2 * kN);
-      look_up(key_lo + 3 * kN);
-      __syncthreads();
-    } else {
-      arrived(key_lo, 0);
     }
+    arrived(key_lo, 0);
   }
   // where the lane's operands stand: K's row n32, pieces 2 c + hi; V's rows 4 hi + .., 64-byte stretches c
   const int v_row = 4 * hi + ((lane & 15) >> 2);
@@ -320,19 +329,27 @@ __global__ __launch_bounds__(NW * 64, (D == 256 && NW == 4 ? 1 : 2)) void k_atte
     __builtin_amdgcn_s_setprio(0);
     if (next < key_hi) {
       if constexpr (FP8) {
-        stage(next, next_buf);
+        stage(next_buf);
         request(0);
         make_places(next + 2 * kN);
-        __syncthreads();
-      } else if (buf & 1) {
-        arrived(next, next_buf);
       }
+      if (FP8 || (buf & 1)) arrived(next, next_buf);
     }
   }
   if constexpr (!FP8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // nothing writes to LDS behind the workgroup's end
 
   l = sum_halves(l);
+  __syncthreads();
   if (!in) return;
+  if (bad)
+#pragma unroll
+    for (int c = 0; c < kCt; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        float x[4] = {o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]};
+        add_not_finite<D, FP8 ? 1 : 0>(a, b, h, max(max(all_see, key_lo), 0), min(vis, key_hi), c * 32 + r * 2 + hi * 4, x);
+        o[c][r] = x[0]; o[c][r + 1] = x[1]; o[c][r + 2] = x[2]; o[c][r + 3] = x[3];
+      }
   const long long at = (long long)(t0 + tok) * a.Hq + h * a.G + hd;
   // channel c 32 + (r / 4) 8 + hi 4 + r % 4 is o[c][r]
   if (piece.nsplit == 1) {

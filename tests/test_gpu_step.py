@@ -606,3 +606,83 @@ def test_calls_on_side_streams():
     torch.cuda.synchronize()
     for ((want, want_lse), _), k in zip(jobs, keep):
         assert np.array_equal(to_host(k[7]), want) and np.array_equal(k[8].cpu().numpy(), want_lse)
+
+
+# ------------------------------------------------------------------- values that are not finite, and what follows from them
+def spoil(k, v, lens, m, dt, where):
+    """Values that are not finite in rows of the step's own tokens: an infinity of either sign and a NaN, in different channels of
+    different heads."""
+    r = np.random.default_rng(8)
+    k, v = k.copy(), v.copy()
+    put = {"bf16": (0x7F80, 0xFF80, 0x7FC0), "f32": (np.inf, -np.inf, np.nan)}[dt]
+    B, H = lens.shape
+    for b in range(B):
+        if m[b] < 2:
+            continue
+        for h in range(H):
+            for x in put:
+                row = lens[b, h] - m[b] + int(r.integers(0, m[b]))
+                if row >= 0:
+                    v[b, h, row, int(r.integers(0, v.shape[-1]))] = x
+            if where == "keys":                      # a key that is not finite, of the last token: the others do not see it
+                k[b, h, lens[b, h] - 1, 3] = put[2]
+    return k, v
+
+
+@pytest.mark.parametrize("dt,hq,hkv,d,m", [("bf16", 8, 2, 128, [2, 3, 1]), ("bf16", 24, 1, 128, [1, 2, 1]), ("bf16", 6, 2, 64, [5, 2, 40]),
+                                          ("bf16", 8, 2, 128, [100, 1, 70]), ("bf16", 4, 2, 256, [3, 90, 2]), ("bf16", 16, 1, 64, [33, 200, 7]),
+                                          ("f32", 4, 2, 64, [2, 30, 1]), ("f32", 6, 2, 128, [4, 1, 170]), ("f32", 256, 4, 256, [2, 9, 70]),
+                                          ("fp8", 8, 2, 128, [3, 2, 1]), ("fp8", 4, 2, 256, [60, 150, 2])])
+@pytest.mark.parametrize("where", ["values", "keys"])
+def test_what_a_token_does_not_see_does_not_matter(dt, hq, hkv, d, m, where):
+    """A value that is not finite reaches the tokens that see its row and no others: theirs are what they are without it."""
+    import torch
+    r = np.random.default_rng(hq)
+    lens = r.integers(max(m), 400, (3, hkv))
+    lens[2, -1] = m[2]
+    q, cu, k, v, L = attend_inputs(hq + d, hq, hkv, d, "f32" if dt == "f32" else "bf16", lens, m)
+    p = ea.make_params(3, hq, hkv, d, kind("f32" if dt == "f32" else "bf16"))
+    cud, cap = i32(cu), k.shape[2]
+    step = ea.make_step(cud, q.shape[0], max(m))
+
+    def run(k, v):
+        out, lse = outputs(q, "f32" if dt == "f32" else "bf16")
+        ws = torch.empty(ea.attend_workspace_bytes(p, step, cap), dtype=torch.uint8, device="cuda").fill_(0xFF)
+        if dt == "fp8":
+            ea.attend_fp8(p, to_dev(q), step, to_dev(k), to_dev(v), None, None, i32(L), cap, cap, out, lse, ws)
+        else:
+            ea.attend(p, to_dev(q), step, to_dev(k), to_dev(v), i32(L), cap, cap, out, lse, ws)
+        torch.cuda.synchronize()
+        return widen(to_host(out)), lse.cpu().numpy()
+    if dt == "fp8":
+        k, v = (r.integers(0, 0x60, k.shape).astype(np.uint8) for _ in range(2))
+        bad_k, bad_v = k.copy(), v.copy()
+        for b in range(3):
+            for h in range(hkv):
+                if m[b] > 1:
+                    bad_v[b, h, L[b, h] - 1 - int(r.integers(0, m[b])), 5] = 0x7F
+                    if where == "keys":
+                        bad_k[b, h, L[b, h] - 1, 3] = 0x7F
+    else:
+        bad_k, bad_v = spoil(k, v, L, m, dt, where)
+    clean, clean_lse = run(k, v)
+    got, lse = run(bad_k, bad_v)
+    if dt == "fp8":
+        no = (bad_v & 0x7F) == 0x7F
+        vf = np.where(no, np.nan, X.fp8_e4m3_decode(np.where(no, 0, bad_v).astype(np.uint8)))
+    else:
+        vf = widen(bad_v)
+    for b in range(3):
+        for i in range(m[b]):
+            for x in range(hq):
+                h = x // (hq // hkv)
+                n, t = L[b, h] - (m[b] - 1 - i), cu[b] + i
+                seen = vf[b, h, :max(n, 0)]
+                if where == "keys" and m[b] > 1 and i == m[b] - 1:
+                    assert np.isnan(got[t, x]).all()
+                    continue
+                # an infinity times a weight whose lower part is zero is a NaN already: not finite is all that is promised
+                fine = np.isfinite(seen).all(0)
+                assert not np.isfinite(got[t, x][~fine]).any()
+                assert np.array_equal(got[t, x][fine], clean[t, x][fine])
+                assert lse[t, x] == clean_lse[t, x]
