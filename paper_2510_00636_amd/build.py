@@ -13,7 +13,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libea.so")
 SOURCES = ["ea_host.cpp", "ea_api.hip", "ea_stats.hip", "ea_score.hip", "ea_score_d64.hip", "ea_score_d128.hip", "ea_score_d128b.hip",
            "ea_score_d256.hip", "ea_score_fp8.hip", "ea_score_fp8b.hip", "ea_score_hw.hip", "ea_select.hip",
-           "ea_compact.hip", "ea_baselines.hip", "ea_frontend.hip", "ea_serve.hip", "ea_step.hip", "ea_attend_rows.hip",
+           "ea_compact.hip", "ea_baselines.hip", "ea_frontend.hip", "ea_serve.cpp", "ea_step.hip", "ea_attend_rows.hip",
            "ea_attend_tile.hip", "ea_attend_f32.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 instructions are switched off for the device pass (the host pass warns that it
