@@ -401,6 +401,8 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   int n = (vis + cut.z - 1) / cut.z;
   n = n < 1 ? 0 : n > cut.y ? cut.y : n;
   const int first = cut.x + (cut.w - 1 - tile) * cut.y * a.Hkv + h;
+  // (prefix sums that do not ascend can count more pieces than there are: none is looked for outside the workspace)
+  if (cut.y > a.plan.most_pieces || first < 0 || first + (n - 1) * a.Hkv >= a.plan.most_pieces) return;
   const float* po = (const float*)(a.ws + a.plan.split_o) + c4;
   const float2* part_ml = (const float2*)(a.ws + a.plan.split_ml);
   float top = -__builtin_inff(), sum = 0.0f;
