@@ -32,14 +32,9 @@ struct AttendArgs {
 };
 
 // the tokens of a sequence, clamped so that no list of prefix sums leads outside q and out
-__device__ __forceinline__ int first_token(const AttendArgs& a, int b) {
-  const int t = a.cu[b];
-  return t < 0 ? 0 : t > a.n_tokens ? a.n_tokens : t;
-}
-__device__ __forceinline__ int rows_of(const AttendArgs& a, int b, int h) {
-  const int t = a.lens[a.per_head ? b * a.Hkv + h : b];
-  return t < 0 ? 0 : t > a.n ? a.n : t;
-}
+__device__ __forceinline__ int clamped(int t, int most) { return t < 0 ? 0 : t > most ? most : t; }
+__device__ __forceinline__ int first_token(const AttendArgs& a, int b) { return clamped(a.cu[b], a.n_tokens); }
+__device__ __forceinline__ int rows_of(const AttendArgs& a, int b, int h) { return clamped(a.lens[a.per_head ? b * a.Hkv + h : b], a.n); }
 
 // exp2f of an argument that is -inf where a row is masked
 __device__ __forceinline__ float pow2(float x) { return exp2f(x); }

@@ -34,6 +34,9 @@ __device__ __forceinline__ Super super_unit(const AttendArgs& a, int su, int sup
   if (s.m >= 1 && s.m * a.G <= a.short_rows) s.grp = s.len < 1 ? 1 : (s.len + kGroup - 1) / kGroup;
   return s;
 }
+// element i of what no launch writes while it is read, the same for the whole wavefront
+template <class T>
+__device__ __forceinline__ T scalar(const T* p, long long i) { return ((const __attribute__((address_space(4))) T*)p)[i]; }
 __device__ __forceinline__ int from_lane(int x, int l) { return __builtin_amdgcn_readlane(x, l); }
 
 template <int D, bool FP8>
@@ -67,13 +70,12 @@ __device__ __forceinline__ void widen_piece(const VPiece<D, FP8>& p, uint32_t* o
   }
 }
 
-// four channels of a finished row
+// four channels of a finished row, whose values have the scale vs
 template <int D>
-__device__ __forceinline__ void write_row(const AttendArgs& a, int t0, int h, int unit, int row, int c4, float top, float sum, float4 acc) {
-  const int tok = row / a.G, hd = row - tok * a.G;
+__device__ __forceinline__ void write_row(const AttendArgs& a, int t0, int h, int tok, int hd, int c4, float vs, float top, float sum, float4 acc) {
   const long long at = (long long)(t0 + tok) * a.Hq + h * a.G + hd;
   const bool any = sum > 0.0f || sum != sum;
-  const float f = (a.vscale ? a.vscale[unit] : 1.0f) / sum;
+  const float f = vs / sum;
   *(uint2*)((__bf16*)a.out + at * D + c4) =
       any ? make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f)) : make_uint2(0u, 0u);
   if (a.lse && c4 == 0) a.lse[at] = natural_lse(top, sum);
@@ -86,7 +88,7 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, int t0, int h, in
 template <int D, int MT> constexpr int rows_lds_floats() { return 4 * 16 * MT * (D + 4) + 4 * 16 * MT * 2; }
 
 template <int D, bool FP8, int MT>
-__global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(AttendArgs a) {
+__global__ __launch_bounds__(256, (D == 256 && !FP8 ? 1 : 2)) void k_attend_rows(AttendArgs a) {
   using S = RowShape<D, FP8>;
   constexpr int kM = 16 * MT, kPitch = D + 4;
   extern __shared__ __attribute__((aligned(16))) float lds[];
@@ -148,23 +150,34 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
   }
   fill(cur);
 
-  // ---- what is in flight: a tile of K and of V, and the next part's queries
-  int entries = 0, window = 0;
-  auto entries_of = [&](const Part& c, int from) {      // of the wavefront's 32 tiles from row `from` on, two per tile, one in each lane
-    const int r = from + (lane >> 1) * kGroup + (lane & 1) * 16;
-    return table_entry(a, c.b, r < c.len ? r : c.len > 0 ? c.len - 1 : 0);
+  // ---- What is in flight: always a tile of K and behind it a tile of V, of this part or, at its end, of the next one; the next part's
+  // queries in front of them.  Loads are waited for in order, and the compiler counts what may be on its way behind the one that it
+  // waits for on the path with the fewest: so no path asks for fewer, a wavefront whose part of a head is over or empty asks for the
+  // head's last rows again, and what else is read on the way comes by scalar loads.
+  struct Blocks { int e0, e1; };      // table entries of a tile's halves
+  auto last_sub = [](const Part& c, int at) {           // the 16 rows from `at` on, or the head's last ones
+    const int last = c.len > 0 ? (c.len - 1) & ~15 : 0;
+    return at < last ? at : last;
+  };
+  auto look_up = [&](const Part& c, int at) {
+    Blocks e = {0, 0};
+    if (a.pm.table) {
+      const int32_t* t = a.pm.table + (long long)c.b * a.pm.max_blocks;
+      e.e0 = scalar(t, last_sub(c, at) >> a.pm.sh);
+      e.e1 = scalar(t, last_sub(c, at + 16) >> a.pm.sh);
+    }
+    return e;
   };
   u32x4 kraw[2][FP8 ? S::kSteps / 2 : S::kSteps];
   VPiece<D, FP8> vraw[8][S::kLoads];
   long long base[2];
   int lim[2];
-  auto place = [&](const Part& c, int at) {             // the two halves of the tile at row `at`: where they start, and their last row
+  auto place = [&](const Part& c, int at, int hi, Blocks e) {      // the tile at row `at`: where its halves start, and their last rows
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int r = at + t * 16 < c.len ? at + t * 16 : at;
-      const int e = __builtin_amdgcn_readlane(entries, (at - window) / kGroup * 2 + (r != at ? 1 : 0));
-      base[t] = row_base(a, c.b, c.h, r, e) * S::kBytes;
-      lim[t] = c.len - 1 - r < 15 ? c.len - 1 - r : 15;
+      const int r = last_sub(c, at + t * 16), last = c.len - 1 - r;
+      base[t] = row_base(a, c.b, c.h, r, t ? e.e1 : e.e0) * S::kBytes;
+      lim[t] = at >= hi ? 0 : last < 15 ? last : 15;      // (a tile that is not wanted: one row of it)
     }
   };
   auto load_k = [&]() {
@@ -187,31 +200,28 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
         vraw[j][u] = *(const VPiece<D, FP8>*)(p + at + u * (16 * S::kCpl * (FP8 ? 1 : 2)));
     }
   };
+  const uint32_t g_inverse = (65535u + a.G) / a.G;       // rows / G by a product: exact for rows and G up to 32
+  auto over_g = [&](int row) { return (int)((uint32_t)row * g_inverse >> 16); };
   // the query operand: row n16 (+ 16) of the head's rows (token, head of the group), channels as the keys' operand has them
   u32x4 q[MT][S::kSteps];
   auto load_q = [&](const Part& c) {
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-      const int row = t * 16 + n16, in = row < c.m * a.G ? row : 0, tok = in / a.G, hd = in - tok * a.G;
+      const int row = t * 16 + n16, in = row < c.m * a.G ? row : 0, tok = over_g(in), hd = in - tok * a.G;
       const __bf16* src = (const __bf16*)a.q + (long long)(c.t0 + tok) * a.q_stride + (c.h * a.G + hd) * D;
 #pragma unroll
       for (int s = 0; s < S::kSteps; ++s)
         q[t][s] = *(const u32x4*)(src + (FP8 ? (s >> 1) * 64 + g * 16 + (s & 1) * 8 : s * 32 + g * 8));
     }
   };
-  // the first loads of a part, in the order of what waits for them
-  auto begin = [&](const Part& c) {
-    const int row = c.off * kGroup + wave * 32;
-    window = row;
-    if (row < c.len) {
-      place(c, row);
-      load_k();
-      load_v();
-    }
+  auto begin = [&](const Part& c, Blocks e) {
+    const int at = c.off * kGroup + wave * 32;
+    place(c, at, c.len, e);
     load_q(c);
+    load_k();
+    load_v();
   };
-  entries = entries_of(cur, cur.off * kGroup + wave * 32);
-  begin(cur);
+  begin(cur, look_up(cur, cur.off * kGroup + wave * 32));
   if (tid == 0) bad[0] = 0;
   __syncthreads();
 
@@ -219,7 +229,7 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
     x += cur.take;
     // ---- the part behind this one, and the entries of its blocks
     Part next = cur;
-    int next_entries = 0;
+    Blocks first = {0, 0}, following_blocks = look_up(cur, (cur.off + 1) * kGroup + wave * 32);
     bool go_on = x < x1;
     if (go_on) {
       if (x >= (long long)(cur.have + cur.grp) * mult) {      // the next super-unit that has groups
@@ -240,7 +250,7 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
       }
       if (go_on) {
         fill(next);
-        next_entries = entries_of(next, next.off * kGroup + wave * 32);
+        first = look_up(next, next.off * kGroup + wave * 32);
       }
     }
     const int rows = cur.m * a.G, unit = cur.b * a.Hkv + cur.h, len = cur.len;
@@ -255,11 +265,11 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
       }
       ((int2*)(a.ws + a.plan.info))[unit] = make_int2((int)blockIdx.x, pieces);
     }
-    const float qk = a.scale * (FP8 && a.kscale ? a.kscale[unit] : 1.0f);
+    const float qk = a.scale * (FP8 && a.kscale ? scalar(a.kscale, unit) : 1.0f), vs = FP8 && a.vscale ? scalar(a.vscale, unit) : 1.0f;
     int vis[MT];            // keys that the row sees
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-      const int row = t * 16 + n16, tok = row / a.G;
+      const int row = t * 16 + n16, tok = over_g(row);
       vis[t] = row < rows ? len - (cur.m - 1 - tok) : len;
     }
     bool any_bad = false;
@@ -274,6 +284,7 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
     }
     const int row_hi = min((cur.off + cur.take) * kGroup, len);
     int row = cur.off * kGroup + wave * 32;
+    const bool no_tile = row >= row_hi;
     while (row < row_hi) {
       const int following = row + kGroup;
       // ---- S^T: 32 keys x 16 rows
@@ -295,15 +306,12 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
           for (int i = 0; i < MT; ++i)
             s[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, q[i][c]), s[i][t], 0, 0, 0);
         }
-      const bool more = following < row_hi;
-      if (more) {
-        if (following - window >= 32 * kGroup) {
-          entries = entries_of(cur, following);
-          window = following;
-        }
-        place(cur, following);
-        load_k();
-      }
+      const bool over = following >= row_hi && go_on;
+      if (over) load_q(next);
+      if (over) place(next, next.off * kGroup + wave * 32, next.len, first);
+      else place(cur, following, row_hi, following_blocks);
+      load_k();
+      following_blocks = look_up(cur, following + kGroup);
       __builtin_amdgcn_sched_barrier(0);
       // ---- weights.  The maximum that they are taken against moves only when a row's passes it by more than 2^8: their sum and
       // the weighted values stay far from either end of fp32 then, and the division at the end takes the factor out again.
@@ -369,15 +377,12 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
           }
         }
       }
-      if (more) load_v();
+      load_v();
       __builtin_amdgcn_sched_barrier(0);
       row = following;
     }
     // the next part's first tile is on its way while this one's results are put together
-    if (go_on) {
-      entries = next_entries;
-      begin(next);
-    }
+    if (go_on && no_tile) begin(next, first);
     __builtin_amdgcn_sched_barrier(0);
 
     // ---- the four wavefronts' results through LDS, once; then every thread makes four channels of a row of them
@@ -425,12 +430,12 @@ __global__ __launch_bounds__(256, (D * MT > 128 ? 1 : 2)) void k_attend_rows(Att
       }
       if (bad[parity]) {
         float y[4] = {acc.x, acc.y, acc.z, acc.w};
-        const int seen = len - (cur.m - 1 - r / a.G);
+        const int seen = len - (cur.m - 1 - over_g(r));
         add_not_finite<D, FP8 ? 1 : 0>(a, cur.b, cur.h, max(max(len - (cur.m - 1), cur.off * kGroup), 0), min(seen, row_hi), c4, y);
         acc = make_float4(y[0], y[1], y[2], y[3]);
       }
       if (whole) {
-        write_row<D>(a, cur.t0, cur.h, unit, r, c4, top, sum, acc);
+        write_row<D>(a, cur.t0, cur.h, over_g(r), r - over_g(r) * a.G, c4, vs, top, sum, acc);
       } else {
         *(float4*)(part_o + (long long)r * D + c4) = acc;
         if (c4 == 0) part_ml[r] = make_float2(top, sum);
@@ -456,6 +461,7 @@ __global__ __launch_bounds__(256) void k_attend_rows_join(AttendArgs a) {
   if (m < 1 || m * a.G > a.short_rows || row >= m * a.G) return;
   const int pieces = info.y;
   if (pieces <= 1) return;
+  const float vs = a.vscale ? a.vscale[unit] : 1.0f;
   const int way = threadIdx.x / kLanes, c4 = threadIdx.x % kLanes * 4;
   const float* po = (const float*)(a.ws + a.plan.part_o) + c4;
   const float2* part_ml = (const float2*)(a.ws + a.plan.part_ml);
@@ -488,7 +494,7 @@ __global__ __launch_bounds__(256) void k_attend_rows_join(AttendArgs a) {
   if (way != 0) return;
 #pragma unroll
   for (int w = 1; w < kWays; ++w) take(pass_ml[w], pass[w][c4 / 4]);
-  write_row<D>(a, t0, h, unit, row, c4, top, sum, acc);
+  write_row<D>(a, t0, h, row / a.G, row % a.G, c4, vs, top, sum, acc);
 }
 
 template <int D, bool FP8, int MT>
