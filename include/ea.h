@@ -339,7 +339,7 @@ typedef struct {
  *   ea_append_fp8    the same into e4m3 bytes: k / k_scale[b, h] and v / v_scale[b, h] (NULL = 1), rounded
  *                    to nearest even, saturating at +-448.  p->dtype EA_BF16, head_dim 128 or 256.
  * q_out [n_tokens, Hq, d] receives the rotated queries (with new->q; it may be q itself if that is dense).
- * k, v and q must not overlap the cache.  Two tokens with the same slot: either may be stored.
+ * k, v and q must not overlap the cache.  Two tokens with the same slot: the row holds pieces of either.
  * p->rope_layout as everywhere; horizon, epsilon and the window's fields are not used. */
 ea_status ea_append_paged(const ea_params* p, const ea_new_rows* rows, const int64_t* slots, void* k_pool, void* v_pool,
                           const ea_paged* pg, void* q_out, void* stream);

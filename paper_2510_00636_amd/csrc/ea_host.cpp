@@ -342,14 +342,18 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   a.rows = !f32 && a.short_rows >= d.G && (most <= a.piece_rows || d.B > 1);
   a.tile = f32 || most > a.piece_rows;
   a.shares = 2 * num_cu < kAttendShares ? 2 * num_cu : kAttendShares;
-  // fp32: wavefronts over rows where those give every CU a workgroup, else over keys
-  if (!f32) a.tile_rows = most > 128 ? 256 : 128;
+  // fp32: wavefronts over rows where those give every CU a workgroup, else over keys (1024 tokens of 2 x 8 KV heads over 2048 rows 655
+  // and 690 us, 64 tokens of 2 KV heads 21 and 14)
+  // bf16: 256 rows to a workgroup, 128 where no sequence has more (d = 128, 16 tokens of 4 heads over 16k rows 27 us, in one tile of 256
+  // 31; 40 tokens 38 and 37) but at d = 256, where registers leave one workgroup to a CU either way (64 tokens of 2 heads 62 and 54)
+  if (!f32) a.tile_rows = d.D < 256 && most <= 128 ? 128 : 256;
   else a.tile_rows = most >= kAttendF32LongRows && n_tokens * d.G / kAttendF32LongRows * d.Hkv >= num_cu ? kAttendF32LongRows : kAttendF32Rows;
   // a sequence's last tile may be short: one more for each
   const int64_t tiles = n_tokens * d.G / a.tile_rows + d.B, slots = a.tile_rows == 256 ? num_cu : 2 * (int64_t)num_cu;
   a.grid = tiles * d.Hkv;
   a.per_slot = 1.0f / (float)slots;
-  // more rounds of whole tiles than this share out the chip well enough
+  // More rounds of whole tiles than this share out the chip well enough, and keys that are this few are not worth a second launch (64
+  // tokens over 128 rows 17.6 us, with the plan and the joining launch 22.3; over 256 rows 25.0 and 25.2)
   if (n_tokens * d.G / a.tile_rows * d.Hkv < 4 * slots && n > 256) {
     a.most_pieces = (int)(2 * slots);
     if (a.grid < a.most_pieces) a.grid = a.most_pieces;

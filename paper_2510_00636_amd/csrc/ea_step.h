@@ -16,7 +16,6 @@ struct BlockTableArgs {
 };
 hipError_t launch_block_tables(const BlockTableArgs& a, hipStream_t st);
 
-constexpr int kAppendTokens = 4;        // of a workgroup in long calls
 struct AppendArgs {
   const void *q, *k, *v;
   void *q_out, *k_cache, *v_cache;
@@ -25,7 +24,8 @@ struct AppendArgs {
   const int64_t* slots;                 // or null: rows by cu and lens [B, Hkv], n_cap per head
   const float *k_scale, *v_scale;
   long long q_stride, k_stride, v_stride, n_cap, num_blocks;
-  int B, Hq, Hkv, n_tokens, sh, rope_layout, tokens_per_wg;
+  int B, Hq, Hkv, n_tokens, sh, rope_layout;
+  int first;                            // token of the launch
 };
 hipError_t launch_append(const AppendArgs& a, const Dims& d, hipStream_t st);
 

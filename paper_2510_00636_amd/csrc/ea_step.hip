@@ -152,9 +152,10 @@ hipError_t launch_block_tables(const BlockTableArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------------------------- new rows
-// A workgroup takes a few tokens: their angles go through LDS once (fp64 product and reduction to one turn, fp32 sine and
-// cosine), then every thread turns 8 pairs of channels of a head at a time and stores them.  Values take the same way
-// unturned.  Memory bounds it: every row is read and written once, 16 bytes a lane.
+// A workgroup takes 256 stretches of one token's rows: the token's angles go through LDS once (fp64 product and reduction to one turn,
+// fp32 sine and cosine), then every thread turns 8 pairs of channels of a head and stores them.  Values take the same way unturned.
+// Memory bounds long calls: every row is read and written once, 16 bytes a lane (8192 tokens of 32 + 8 + 8 heads of 128 channels
+// 32.5 us, 6.2 TB/s; four tokens to a workgroup 35.8); latency the short ones (48 tokens 3 us).
 namespace {
 
 template <typename T> struct Eight;                  // eight channels as they stand in memory
@@ -199,121 +200,119 @@ __device__ __forceinline__ uint2 bytes_of(const float* x) {
 
 template <int D, typename T, bool FP8>
 __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
-  __shared__ float2 turn[kAppendTokens][D / 2];
-  const int tid = threadIdx.x, first = blockIdx.x * a.tokens_per_wg;
-  const int count = min(a.tokens_per_wg, a.n_tokens - first);
+  __shared__ float2 turn[D / 2];
+  const int tid = threadIdx.x, token = a.first + blockIdx.x;
+  long long blk = 0;
+  int off = 0, b = 0, behind = 0;
+  if (a.slots) {
+    const long long slot = a.slots[token];
+    if (slot < 0 || slot >= (a.num_blocks << a.sh)) return;
+    blk = slot >> a.sh;
+    off = (int)(slot & ((1 << a.sh) - 1));
+  } else {
+    int lo = 0, hi = a.B;                            // the token's sequence: cu[lo] <= token < cu[hi]
+    if (token < a.cu[0] || token >= a.cu[a.B]) return;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (a.cu[mid] <= token) lo = mid; else hi = mid;
+    }
+    b = lo;
+    behind = a.cu[lo + 1] - token;
+  }
   if (a.inv_freq) {
-    for (int i = tid; i < count * (D / 2); i += 256) {
-      const int t = i / (D / 2), c = i % (D / 2);
+    for (int c = tid; c < D / 2; c += 256) {
       // whole turns taken out in fp64: what is left keeps 2^-31 of a turn at any position of 32 bits
-      double y = (double)a.pos[first + t] * a.inv_freq[c] * 0.15915494309189533577;
+      double y = (double)a.pos[token] * a.inv_freq[c] * 0.15915494309189533577;
       y -= rint(y);
       float si, co;
       sincospif((float)(2.0 * y), &si, &co);
-      turn[t][c] = make_float2(co, si);
+      turn[c] = make_float2(co, si);
     }
     __syncthreads();
   }
   constexpr int kPieces = D / 16;                      // of 8 channel pairs in a head
   const int heads = (a.q ? a.Hq : 0) + 2 * a.Hkv, q_heads = a.q ? a.Hq : 0;
-  for (int t = 0; t < count; ++t) {
-    const int token = first + t;
-    long long blk = 0;
-    int off = 0, b = 0, behind = 0;
-    if (a.slots) {
-      const long long slot = a.slots[token];
-      if (slot < 0 || slot >= (a.num_blocks << a.sh)) continue;
-      blk = slot >> a.sh;
-      off = (int)(slot & ((1 << a.sh) - 1));
+  for (int it = blockIdx.y * 256 + tid; it < heads * kPieces; it += gridDim.y * 256) {
+    const int head = it / kPieces, c = it % kPieces;
+    // channels: halves apart or next to each other
+    const bool is_q = head < q_heads, is_v = head >= q_heads + a.Hkv;
+    const int h = is_q ? head : is_v ? head - q_heads - a.Hkv : head - q_heads;
+    const T* src = is_q ? (const T*)a.q + token * a.q_stride : is_v ? (const T*)a.v + token * a.v_stride : (const T*)a.k + token * a.k_stride;
+    const int c0 = a.rope_layout ? c * 16 : c * 8, c1 = a.rope_layout ? c0 + 8 : c0 + D / 2;
+    const Eight<T> e0 = *(const Eight<T>*)(src + h * D + c0), e1 = *(const Eight<T>*)(src + h * D + c1);
+    float x[16], y[16];
+    widen(e0, x);
+    widen(e1, x + 8);
+    if (a.inv_freq && !is_v) {
+      const float2* w = &turn[c * 8];
+      if (a.rope_layout) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          y[2 * i] = fmaf(x[2 * i], w[i].x, -x[2 * i + 1] * w[i].y);
+          y[2 * i + 1] = fmaf(x[2 * i], w[i].y, x[2 * i + 1] * w[i].x);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          y[i] = fmaf(x[i], w[i].x, -x[i + 8] * w[i].y);
+          y[i + 8] = fmaf(x[i], w[i].y, x[i + 8] * w[i].x);
+        }
+      }
     } else {
-      int lo = 0, hi = a.B;                            // the token's sequence: cu[lo] <= token < cu[hi]
-      if (token < a.cu[0] || token >= a.cu[a.B]) continue;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.cu[mid] <= token) lo = mid; else hi = mid;
-      }
-      b = lo;
-      behind = a.cu[lo + 1] - token;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] = x[i];
     }
-    for (int it = blockIdx.y * 256 + tid; it < heads * kPieces; it += gridDim.y * 256) {
-      const int head = it / kPieces, c = it % kPieces;
-      // channels: halves apart or next to each other
-      const bool is_q = head < q_heads, is_v = head >= q_heads + a.Hkv;
-      const int h = is_q ? head : is_v ? head - q_heads - a.Hkv : head - q_heads;
-      const T* src = is_q ? (const T*)a.q + token * a.q_stride : is_v ? (const T*)a.v + token * a.v_stride : (const T*)a.k + token * a.k_stride;
-      const int c0 = a.rope_layout ? c * 16 : c * 8, c1 = a.rope_layout ? c0 + 8 : c0 + D / 2;
-      const Eight<T> e0 = *(const Eight<T>*)(src + h * D + c0), e1 = *(const Eight<T>*)(src + h * D + c1);
-      float x[16], y[16];
-      widen(e0, x);
-      widen(e1, x + 8);
-      if (a.inv_freq && !is_v) {
-        const float2* w = &turn[t][c * 8];
-        if (a.rope_layout) {
+    if (is_q) {
+      T* dst = (T*)a.q_out + ((long long)token * a.Hq + h) * D;
+      *(Eight<T>*)(dst + c0) = narrow(y, T());
+      *(Eight<T>*)(dst + c1) = narrow(y + 8, T());
+      continue;
+    }
+    long long row;
+    if (a.slots) {
+      row = ((blk * a.Hkv + h) << a.sh) + off;
+    } else {
+      const long long r = (long long)a.lens[b * a.Hkv + h] - behind;
+      if (r < 0 || r >= a.n_cap) continue;
+      row = ((long long)b * a.Hkv + h) * a.n_cap + r;
+    }
+    if constexpr (FP8) {
+      const float* scale = is_v ? a.v_scale : a.k_scale;
+      if (scale) {
+        const float s = scale[b * a.Hkv + h];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            y[2 * i] = fmaf(x[2 * i], w[i].x, -x[2 * i + 1] * w[i].y);
-            y[2 * i + 1] = fmaf(x[2 * i], w[i].y, x[2 * i + 1] * w[i].x);
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            y[i] = fmaf(x[i], w[i].x, -x[i + 8] * w[i].y);
-            y[i + 8] = fmaf(x[i], w[i].y, x[i + 8] * w[i].x);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) y[i] = x[i];
+        for (int i = 0; i < 16; ++i) y[i] /= s;
       }
-      if (is_q) {
-        T* dst = (T*)a.q_out + ((long long)token * a.Hq + h) * D;
-        *(Eight<T>*)(dst + c0) = narrow(y, T());
-        *(Eight<T>*)(dst + c1) = narrow(y + 8, T());
-        continue;
-      }
-      long long row;
-      if (a.slots) {
-        row = ((blk * a.Hkv + h) << a.sh) + off;
-      } else {
-        const long long r = (long long)a.lens[b * a.Hkv + h] - behind;
-        if (r < 0 || r >= a.n_cap) continue;
-        row = ((long long)b * a.Hkv + h) * a.n_cap + r;
-      }
-      if constexpr (FP8) {
-        const float* scale = is_v ? a.v_scale : a.k_scale;
-        if (scale) {
-          const float s = scale[b * a.Hkv + h];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) y[i] /= s;
-        }
-        uint8_t* dst = (uint8_t*)(is_v ? a.v_cache : a.k_cache) + row * D;
-        *(uint2*)(dst + c0) = bytes_of(y);
-        *(uint2*)(dst + c1) = bytes_of(y + 8);
-      } else {
-        T* dst = (T*)(is_v ? a.v_cache : a.k_cache) + row * D;
-        *(Eight<T>*)(dst + c0) = narrow(y, T());
-        *(Eight<T>*)(dst + c1) = narrow(y + 8, T());
-      }
+      uint8_t* dst = (uint8_t*)(is_v ? a.v_cache : a.k_cache) + row * D;
+      *(uint2*)(dst + c0) = bytes_of(y);
+      *(uint2*)(dst + c1) = bytes_of(y + 8);
+    } else {
+      T* dst = (T*)(is_v ? a.v_cache : a.k_cache) + row * D;
+      *(Eight<T>*)(dst + c0) = narrow(y, T());
+      *(Eight<T>*)(dst + c1) = narrow(y + 8, T());
     }
   }
 }
 
 hipError_t launch_append(const AppendArgs& given, const Dims& d, hipStream_t st) {
   AppendArgs a = given;
-  // few tokens: a workgroup for each, and several where the heads give them something to do
-  a.tokens_per_wg = a.n_tokens >= 2048 ? kAppendTokens : 1;
   const int items = ((a.q ? a.Hq : 0) + 2 * a.Hkv) * (d.D / 16);
-  const dim3 grid((a.n_tokens + a.tokens_per_wg - 1) / a.tokens_per_wg, a.tokens_per_wg == 1 ? (items + 255) / 256 : 1);
+  constexpr int kMost = 1 << 23;      // (2^32 threads to a launch)
+  for (a.first = 0; a.first < a.n_tokens; a.first += kMost) {
+    const dim3 grid(a.n_tokens - a.first < kMost ? a.n_tokens - a.first : kMost, items < 65535 * 256 ? (items + 255) / 256 : 65535);
 #define EA_CASE(DD)                                                       \
-  if (d.D == DD) {                                                        \
-    if (d.kv_fp8) {                                                       \
-      if constexpr (DD > 64) k_append<DD, __bf16, true><<<grid, 256, 0, st>>>(a);   \
-    } else if (d.dtype == EA_BF16) k_append<DD, __bf16, false><<<grid, 256, 0, st>>>(a); \
-    else k_append<DD, float, false><<<grid, 256, 0, st>>>(a);             \
+    if (d.D == DD) {                                                        \
+      if (d.kv_fp8) {                                                       \
+        if constexpr (DD > 64) k_append<DD, __bf16, true><<<grid, 256, 0, st>>>(a);   \
+      } else if (d.dtype == EA_BF16) k_append<DD, __bf16, false><<<grid, 256, 0, st>>>(a); \
+      else k_append<DD, float, false><<<grid, 256, 0, st>>>(a);             \
   }
-  EA_CASE(64) EA_CASE(128) EA_CASE(256)
+    EA_CASE(64) EA_CASE(128) EA_CASE(256)
 #undef EA_CASE
-  return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace ea
