@@ -13,6 +13,8 @@ namespace ea {
 // workgroup makes for itself (48 KiB of LDS for the largest batch), so that none waits for another.  The i-th block taken is
 // the i-th one given back, or else comes off the list's end; one given back and not taken goes onto it.  What is read (table
 // entries in front of the old ends, the list below its old end) is nowhere written, so the launch needs no order within.
+// Latency bounds it: lengths, sums, a search, a table entry, a store.  48 sequences of a token each 3.5 us, 512 sequences with 370k
+// tokens 11 us.
 namespace {
 
 constexpr int kTableThreads = 256, kTableTokens = 256;
