@@ -301,7 +301,8 @@ ea_status ea_compress_layer_fp8(const ea_params* p, const void* q_win, int64_t w
  *   slots, pos    [n_tokens] int64 / int32: of the i-th new token of sequence b the pool row
  *                 block * block_size + offset that its row len_old + i has, and its position seen[b] + i;
  *                 slots is -1 for the tokens of a sequence that was not served and from cu_tokens[B] on,
- *                 where pos is left as it was.  Both may be NULL where n_tokens is 0.
+ *                 where pos is left as it was.  Both may be NULL where n_tokens is 0.  (ea_attend's results for
+ *                 the tokens of a sequence that was not served mean nothing.)
  *   seen          [B] int32: tokens the sequence has seen so far; NULL: len_old
  * All are DEVICE pointers (int32: 4-byte aligned, slots 8).  Blocks given back come first and are
  * taken again first, sequences in order; a sequence is served if the blocks wanted up to and with it
@@ -368,7 +369,7 @@ ea_status ea_append_fp8(const ea_params* p, const ea_new_rows* rows, const int32
 typedef struct {
   const int32_t* cu_tokens; /* DEVICE [B + 1], ascending from 0                                      */
   int64_t n_tokens;         /* tokens that q, out and lse have room for                              */
-  int64_t max_new;          /* no sequence adds more (HOST); tokens beyond that many may be left out  */
+  int64_t max_new;          /* no sequence adds more (HOST): the tokens of one that does may be left out */
   int64_t q_stride;         /* elements from token to token of q, a multiple of 16 bytes; 0 = Hq * d   */
 } ea_step;
 size_t ea_attend_workspace_bytes(const ea_params* p, const ea_step* step, int64_t n);
