@@ -109,6 +109,38 @@ def test_prefix_sums_that_make_no_sense(dt, cu):
             assert bool((x[:100] == 7.0).all()) and bool((x[120:] == 7.0).all())
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (4, 2, 256), (20, 1, 64)])
+def test_a_sequence_that_adds_more_than_it_was_said_to(hq, hkv, d):
+    """Its tokens may be left out; the others' are what they are."""
+    q, cu, k, v, L = attend_inputs(hq, hq, hkv, d, "bf16", [300, 70, 500, 260], [1, 2, 90, 1])
+    got, lse = attend_heads(q, cu, k, v, L, "bf16", k.shape[2], k.shape[2], 2)
+    keep = np.r_[0:3, cu[3]:cu[4]]
+    few = [0, 1, 3]
+    check_attend(got[keep], lse[keep], q[keep], np.array([0, 1, 3, 4]), k[few], v[few], L[few], "bf16")
+
+
+def test_more_new_rows_than_a_launch_has():
+    import torch
+    t, hq, hkv, d, bs = (1 << 23) + 3, 1, 1, 64, 16
+    if torch.cuda.mem_get_info()[0] < 8 << 30:
+        pytest.skip("needs 8 GB")
+    here = np.array([0, 77, (1 << 23) - 1, 1 << 23, t - 1])
+    slots = torch.full((t,), -1, dtype=torch.int64, device="cuda")
+    slots[to_dev(here)] = torch.arange(5, device="cuda") * 7
+    x = torch.zeros(t, 2, d, dtype=torch.bfloat16, device="cuda")
+    rows = store(np.random.default_rng(1).standard_normal((5, 2, d)), "bf16")
+    x[to_dev(here)] = to_dev(rows)
+    pools = [torch.full((4, hkv, bs, d), 5.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    table = i32([[0]])
+    ea.append_paged(ea.make_params(1, hq, hkv, d, ea.EA_BF16), ea.make_new_rows(None, x[:, :1], x[:, 1:]), slots, pools[0], pools[1],
+                    ea.make_paged(table, bs, 4))
+    torch.cuda.synchronize()
+    for i, pool in enumerate(pools):
+        want = np.full((64, d), 5.0)
+        want[np.arange(5) * 7] = widen(rows)[:, i]
+        assert np.array_equal(widen(to_host(pool)).reshape(64, d), want)
+
+
 # ------------------------------------------------------------------------------------------ joins, views, scales
 @pytest.mark.parametrize("hq,hkv,d,m", [(16, 2, 64, [300, 1]), (16, 4, 128, [290, 3]), (16, 8, 256, [260, 2])])
 def test_long_rows_cut_and_joined(hq, hkv, d, m):
