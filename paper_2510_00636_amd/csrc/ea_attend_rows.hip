@@ -183,6 +183,13 @@ __global__ __launch_bounds__(256, (D == 256 && !FP8 ? 1 : 2)) void k_attend_rows
       v_rows[t] = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)a.v + base), 0, n * S::kBytes, 0x27000);
     }
   };
+  auto place_none = [&]() {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      k_rows[t] = __builtin_amdgcn_make_buffer_rsrc((void*)a.k, 0, 0, 0x27000);
+      v_rows[t] = __builtin_amdgcn_make_buffer_rsrc((void*)a.v, 0, 0, 0x27000);
+    }
+  };
   constexpr int kPiece = S::kCpl * (FP8 ? 1 : 2);        // bytes of a lane's load of V
   const int k_at = n16 * S::kBytes + g * 16, v_at = 4 * g * S::kBytes + n16 * kPiece;
   auto load_k = [&]() {
@@ -218,8 +225,8 @@ __global__ __launch_bounds__(256, (D == 256 && !FP8 ? 1 : 2)) void k_attend_rows
   };
   auto begin = [&](const Part& c, Blocks e) {
     const int at = c.off * kGroup + wave * 32;
-    place(c, at, c.len, e);
     load_q(c);
+    place(c, at, c.len, e);
     load_k();
     load_v();
   };
@@ -231,7 +238,8 @@ __global__ __launch_bounds__(256, (D == 256 && !FP8 ? 1 : 2)) void k_attend_rows
     x += cur.take;
     // ---- the part behind this one, and the entries of its blocks
     Part next = cur;
-    Blocks first = {0, 0}, following_blocks = look_up(cur, (cur.off + 1) * kGroup + wave * 32);
+    Blocks first = {0, 0}, following_blocks = {0, 0};
+    if (cur.take > 1) following_blocks = look_up(cur, (cur.off + 1) * kGroup + wave * 32);
     bool go_on = x < x1;
     if (go_on) {
       if (x >= (long long)(cur.have + cur.grp) * mult) {      // the next super-unit that has groups
@@ -311,9 +319,10 @@ __global__ __launch_bounds__(256, (D == 256 && !FP8 ? 1 : 2)) void k_attend_rows
       const bool over = following >= row_hi && go_on;
       if (over) load_q(next);
       if (over) place(next, next.off * kGroup + wave * 32, next.len, first);
-      else place(cur, following, row_hi, following_blocks);
+      else if (following < row_hi) place(cur, following, row_hi, following_blocks);
+      else place_none();
       load_k();
-      following_blocks = look_up(cur, following + kGroup);
+      if (following + kGroup < row_hi) following_blocks = look_up(cur, following + kGroup);
       __builtin_amdgcn_sched_barrier(0);
       // ---- weights.  The maximum that they are taken against moves only when a row's passes it by more than 2^8: their sum and
       // the weighted values stay far from either end of fp32 then, and the division at the end takes the factor out again.
