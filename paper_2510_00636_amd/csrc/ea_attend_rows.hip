@@ -105,7 +105,13 @@ __global__ __launch_bounds__(256, (D == 256 && !FP8 ? 1 : 2)) void k_attend_rows
   int pre = wave_prefix(mine.grp), total = last_lane(pre), block = 0;
   for (int base = 64; base < supers; base += 64) total += last_lane(wave_prefix(super_unit(a, base + lane, supers).grp));
   const long long all = (long long)total * mult, wgs = all < gridDim.x ? all : gridDim.x;
-  if (blockIdx.x >= wgs) return;      // (a head's pieces are those of neighbours: no share in between is empty)
+  // for the joining launch, of a head that begins here: the head, this workgroup, and to how many the head falls from here on; by
+  // heads, or by workgroups, in which no more than one head goes on behind the end (-1: none does)
+  int4* info = (int4*)(a.ws + a.plan.info);
+  auto nothing = [&]() {
+    if (a.plan.by_share && tid == 0) info[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  };
+  if (blockIdx.x >= wgs) return nothing();            // (a head's pieces are those of neighbours: no share in between is empty)
   // all w / wgs without a 64-bit division where there is none to do
   const bool small = all < (1ll << 31);
   const long long each = small ? (long long)((uint32_t)all / (uint32_t)wgs) : all / wgs;
@@ -145,7 +151,7 @@ __global__ __launch_bounds__(256, (D == 256 && !FP8 ? 1 : 2)) void k_attend_rows
     }
     cur.have += last_lane(pre);
     block += 64;
-    if (block >= supers) return;
+    if (block >= supers) return nothing();
     mine = super_unit(a, block + lane, supers);
     pre = wave_prefix(mine.grp);
   }
@@ -265,15 +271,20 @@ __global__ __launch_bounds__(256, (D == 256 && !FP8 ? 1 : 2)) void k_attend_rows
     }
     const int rows = cur.m * a.G, unit = cur.b * a.Hkv + cur.h, len = cur.len;
     const bool whole = cur.take == cur.grp;
-    if (cur.off == 0 && tid == 0) {     // the workgroups that the head falls to, from this one on, for the joining launch
+    const bool begins = cur.off == 0;
+    if (tid == 0 && (begins || !go_on)) {
       int pieces = 1;
-      if (!whole) {     // the last one is the last of those that begin at or in front of its last group
+      if (begins && !whole) {     // the last one is the last of those that begin at or in front of its last group
         const long long end = x - cur.take + cur.grp;
         int w = (int)blockIdx.x + (int)((cur.grp - cur.take) / (each + 1));
         while (share_at(w + 1) < end) ++w;
         pieces = w - (int)blockIdx.x + 1;
       }
-      ((int2*)(a.ws + a.plan.info))[unit] = make_int2((int)blockIdx.x, pieces);
+      if (!a.plan.by_share) {
+        if (begins) info[unit] = make_int4(unit, (int)blockIdx.x, pieces, 0);
+      } else if (!go_on) {
+        info[blockIdx.x] = make_int4(pieces > 1 ? unit : -1, (int)blockIdx.x, pieces, 0);
+      }
     }
     const float qk = a.scale * (FP8 && a.kscale ? scalar(a.kscale, unit) : 1.0f), vs = FP8 && a.vscale ? scalar(a.vscale, unit) : 1.0f;
     int vis[MT];            // keys that the row sees
@@ -460,12 +471,14 @@ __global__ __launch_bounds__(256) void k_attend_rows_join(AttendArgs a) {
   constexpr int kLanes = D / 4, kWays = 256 / kLanes, kRounds = 8;
   __shared__ float4 pass[kWays][kLanes];
   __shared__ float2 pass_ml[kWays];
-  const int unit = blockIdx.x / a.short_rows, row = blockIdx.x - unit * a.short_rows;
+  const int nth = blockIdx.x / a.short_rows, row = blockIdx.x - nth * a.short_rows;
+  const int4 info = ((const int4*)(a.ws + a.plan.info))[nth];
+  const int unit = a.plan.by_share ? info.x : nth;
+  if (unit < 0) return;
   const int b = unit / a.Hkv, h = unit - b * a.Hkv;
-  const int2 info = ((const int2*)(a.ws + a.plan.info))[unit];
   const int t0 = first_token(a, b), m = first_token(a, b + 1) - t0;
   if (m < 1 || m * a.G > a.short_rows || row >= m * a.G) return;
-  const int pieces = info.y;
+  const int pieces = info.z;
   if (pieces <= 1) return;
   const float vs = a.vscale ? a.vscale[unit] : 1.0f;
   const int way = threadIdx.x / kLanes, c4 = threadIdx.x % kLanes * 4;
@@ -486,7 +499,7 @@ __global__ __launch_bounds__(256) void k_attend_rows_join(AttendArgs a) {
 #pragma unroll
     for (int k = 0; k < kRounds; ++k) {
       const int i = i0 + k * kWays < pieces ? i0 + k * kWays : i0;
-      const long long slot = ((long long)(info.x + i) * 2 + (i == 0 ? 1 : 0)) * a.plan.piece_rows + row;
+      const long long slot = ((long long)(info.y + i) * 2 + (i == 0 ? 1 : 0)) * a.plan.piece_rows + row;
       ml[k] = part_ml[slot];
       y[k] = *(const float4*)(po + slot * D);
     }
@@ -512,7 +525,7 @@ static hipError_t rows_of_height(const AttendArgs& a, hipStream_t st) {
   k_attend_rows<D, FP8, MT><<<a.plan.shares, 256, bytes, st>>>(a);
   const hipError_t e2 = hipGetLastError();
   if (e2 != hipSuccess) return e2;
-  k_attend_rows_join<D><<<a.B * a.Hkv * a.short_rows, 256, 0, st>>>(a);
+  k_attend_rows_join<D><<<(a.plan.by_share ? a.plan.shares : a.B * a.Hkv) * a.short_rows, 256, 0, st>>>(a);
   return hipGetLastError();
 }
 template <int D, bool FP8>

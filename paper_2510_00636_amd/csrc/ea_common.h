@@ -64,6 +64,7 @@ struct AttendPlan {
   int mt;             // 16-row operands of the row kernel
   int short_rows;     // most (token, head) rows of a sequence that is the row kernel's
   int shares;         // its workgroups
+  int by_share;       // the joining launch looks at every workgroup's last head, not at every head
   int piece_rows;     // rows reserved for a partial result
   int tile_rows;      // (token, head) rows of a workgroup of the tile kernel
   int64_t grid;       // its workgroups: as many as there may be pieces

@@ -365,7 +365,9 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
     return at;
   };
   if (a.rows) {
-    a.info = take((size_t)d.units() * 2 * sizeof(int32_t));
+    // no more heads are cut than there are workgroups (512 sequences of 20 rows, 4096 heads: joining 12 us, by workgroups 5)
+    a.by_share = d.units() > a.shares;
+    a.info = take((size_t)(a.by_share ? a.shares : d.units()) * 4 * sizeof(int32_t));
     a.part_o = take((size_t)a.shares * 2 * a.piece_rows * d.D * sizeof(float));
     a.part_ml = take((size_t)a.shares * 2 * a.piece_rows * 2 * sizeof(float));
   }

@@ -60,6 +60,24 @@ def test_many_sequences_with_a_length_per_head(dt, hq, hkv, d, single):
     check_attend(got, lse, q, cu, k, v, L, dt)
 
 
+@pytest.mark.parametrize("hq,hkv,d,B", [(8, 2, 128, 300), (4, 4, 64, 150), (16, 8, 256, 70)])
+@pytest.mark.parametrize("heads", [False, True])
+def test_more_heads_than_workgroups(hq, hkv, d, B, heads):
+    """Short heads by the dozen to a workgroup, and some long ones over several."""
+    r = np.random.default_rng(B)
+    lens = r.integers(0, 60, (B, hkv if heads else 1))
+    for _ in range(4):
+        lens[r.integers(0, B), r.integers(0, lens.shape[1])] = r.integers(400, 1200)
+    m = np.where(r.random(B) < 0.9, 1, r.integers(0, 4, B))
+    q, cu, k, v, L = attend_inputs(B, hq, hkv, d, "bf16", lens if heads else lens[:, 0], m, room=1)
+    if heads:
+        got, lse = attend_heads(q, cu, k, v, L, "bf16", k.shape[2], k.shape[2], 3)
+    else:
+        got, lse = run_paged(q, cu, k, v, L, 32)
+    check_attend(got, lse, q, cu, k, v, L, "bf16")
+    assert (widen(got)[cu[-1]:] == 7.0).all() and (lse[cu[-1]:] == 7.0).all()
+
+
 def test_fp32_prompt():
     """Enough rows for the kernel whose wavefronts lie over the rows."""
     q, cu, k, v, L = attend_inputs(5, 8, 8, 64, "f32", [1100, 1000], [1100, 948])
