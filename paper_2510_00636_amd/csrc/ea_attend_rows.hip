@@ -1,4 +1,4 @@
-// Attention of few (token, head) rows per KV head: single tokens, and stretches of a few.
+// Attention of few (token, head) rows per KV head, up to 16, 32 or 64: single tokens, and stretches of a few.
 //
 // The cache is read once and that bounds it (4 G d operations for 4 d bytes of a pair; 4 sequences of 131k rows 349 us, 6.15 TB/s of
 // the 6.16 that a large read has on this card), so the whole chip reads all the time:
@@ -89,7 +89,7 @@ __device__ __forceinline__ void write_row(const AttendArgs& a, int t0, int h, in
 template <int D, int MT> constexpr int rows_lds_floats() { return 4 * 16 * MT * (D + 4) + 4 * 16 * MT * 2; }
 
 template <int D, bool FP8, int MT>
-__global__ __launch_bounds__(256, (D == 256 && !FP8 ? 1 : 2)) void k_attend_rows(AttendArgs a) {
+__global__ __launch_bounds__(256, (D * MT > 256 || (D == 256 && !FP8) ? 1 : 2)) void k_attend_rows(AttendArgs a) {
   using S = RowShape<D, FP8>;
   constexpr int kM = 16 * MT, kPitch = D + 4;
   extern __shared__ __attribute__((aligned(16))) float lds[];
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256, (D == 256 && !FP8 ? 1 : 2)) void k_attend_rows
         else vraw[j][u].w = __builtin_amdgcn_raw_buffer_load_b64(v_rows[j >> 2], at, 0, 0);
       }
   };
-  const uint32_t g_inverse = (65535u + a.G) / a.G;       // rows / G by a product: exact for rows and G up to 32
+  const uint32_t g_inverse = (65535u + a.G) / a.G;       // rows / G by a product: exact for rows and G up to 64
   auto over_g = [&](int row) { return (int)((uint32_t)row * g_inverse >> 16); };
   // the query operand: row n16 (+ 16) of the head's rows (token, head of the group), channels as the keys' operand has them
   u32x4 q[MT][S::kSteps];
@@ -531,7 +531,8 @@ static hipError_t rows_of_height(const AttendArgs& a, hipStream_t st) {
 template <int D, bool FP8>
 static hipError_t rows_of_type(const AttendArgs& a, hipStream_t st) {
   if constexpr (D < 256)
-    if (a.plan.mt == 2) return rows_of_height<D, FP8, 2>(a, st);
+    if (a.plan.mt == 4) return rows_of_height<D, FP8, 4>(a, st);
+  if (a.plan.mt == 2) return rows_of_height<D, FP8, 2>(a, st);
   return rows_of_height<D, FP8, 1>(a, st);
 }
 

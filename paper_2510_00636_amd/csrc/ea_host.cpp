@@ -335,17 +335,21 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   const bool f32 = d.dtype != EA_BF16;
   if (max_new > n_tokens) max_new = n_tokens;
   const int64_t most = max_new * d.G;         // (token, head) rows of a sequence and KV head
-  a.mt = most > 16 && most <= 32 && d.D <= 128 ? 2 : 1;
+  // Up to 64 rows where their results fit the registers (d = 256: 32): 8 sequences over 4096 rows with 16 tokens of 4 heads 38.7 us, as
+  // stretches 45.9, with 16 of 2 heads at d = 256 57 and 78 (8-bit rows 37.5 and 79).  One short sequence loses up to a tenth (d = 64,
+  // 16k rows 23.5 and 21.6), and so do many (48 over 512 rows 47.5 and 42.5).
+  a.mt = most <= 16 ? 1 : most <= 32 ? 2 : most <= 64 && d.D <= 128 ? 4 : 1;
   a.piece_rows = 16 * a.mt;
   a.short_rows = (int)(most < a.piece_rows ? most : a.piece_rows);
   // one sequence is one kernel's; of several that may be long some may be short
   a.rows = !f32 && a.short_rows >= d.G && (most <= a.piece_rows || d.B > 1);
   a.tile = f32 || most > a.piece_rows;
-  a.shares = 2 * num_cu < kAttendShares ? 2 * num_cu : kAttendShares;
+  a.shares = a.mt * d.D > 256 ? num_cu : 2 * num_cu;      // as many as run at once
+  if (a.shares > kAttendShares) a.shares = kAttendShares;
   // fp32: wavefronts over rows where those give every CU a workgroup, else over keys (1024 tokens of 2 x 8 KV heads over 2048 rows 655
   // and 690 us, 64 tokens of 2 KV heads 21 and 14)
-  // bf16: 256 rows to a workgroup, 128 where no sequence has more (d = 128, 16 tokens of 4 heads over 16k rows 27 us, in one tile of 256
-  // 31; 40 tokens 38 and 37) but at d = 256, where registers leave one workgroup to a CU either way (64 tokens of 2 heads 62 and 54)
+  // bf16: 256 rows to a workgroup, 128 where no sequence has more (d = 128, 32 tokens of 4 heads over 16k rows 32 us, in one tile of 256
+  // 35; 40 tokens 38 and 37) but at d = 256, where registers leave one workgroup to a CU either way (64 tokens of 2 heads 62 and 54)
   if (!f32) a.tile_rows = d.D < 256 && most <= 128 ? 128 : 256;
   else a.tile_rows = most >= kAttendF32LongRows && n_tokens * d.G / kAttendF32LongRows * d.Hkv >= num_cu ? kAttendF32LongRows : kAttendF32Rows;
   // a sequence's last tile may be short: one more for each
@@ -365,7 +369,7 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
     return at;
   };
   if (a.rows) {
-    // no more heads are cut than there are workgroups (512 sequences of 20 rows, 4096 heads: joining 12 us, by workgroups 5)
+    // no more heads are cut than there are workgroups (512 sequences of 20 rows, 4096 heads: joining 12 us, by workgroups 3.5)
     a.by_share = d.units() > a.shares;
     a.info = take((size_t)(a.by_share ? a.shares : d.units()) * 4 * sizeof(int32_t));
     a.part_o = take((size_t)a.shares * 2 * a.piece_rows * d.D * sizeof(float));

@@ -78,6 +78,34 @@ def test_more_heads_than_workgroups(hq, hkv, d, B, heads):
     assert (widen(got)[cu[-1]:] == 7.0).all() and (lse[cu[-1]:] == 7.0).all()
 
 
+@pytest.mark.parametrize("dt,hq,hkv,d,m", [("bf16", 8, 2, 64, [5, 16, 1, 9]), ("bf16", 12, 4, 128, [5, 12, 1, 21]), ("bf16", 4, 2, 256, [5, 12, 1, 16]),
+                                          ("bf16", 20, 1, 256, [1, 1, 0, 1]), ("bf16", 33, 1, 128, [1, 1, 1, 1]), ("fp8", 8, 2, 128, [5, 16, 1, 9]),
+                                          ("fp8", 4, 2, 256, [5, 12, 1, 16]), ("fp8", 33, 1, 128, [1, 1, 0, 1])])
+def test_rows_of_all_heights(dt, hq, hkv, d, m):
+    """Two and four operands of 16 rows, over heads that are cut and heads that see less than they add."""
+    import torch
+    r = np.random.default_rng(hq + d)
+    lens = r.integers(0, 800, (4, hkv))
+    lens[1, 0], lens[3, -1] = 3000, max(m[3] - 1, 0)
+    q, cu, k, v, L = attend_inputs(d, hq, hkv, d, "bf16" if dt == "bf16" else "f32", lens, m, room=1)
+    cap = k.shape[2]
+    if dt == "bf16":
+        got, lse = attend_heads(q, cu, k, v, L, "bf16", cap, cap, max(m))
+    else:
+        q = store(q.astype(np.float64), "bf16")
+        (k8, ks), (v8, vs) = (quantize_fp8(np.nan_to_num(x.astype(np.float64))) for x in (k, v))
+        p = ea.make_params(4, hq, hkv, d, ea.EA_BF16)
+        cud = i32(cu)
+        step, (out, lse) = ea.make_step(cud, q.shape[0], max(m)), outputs(q, "bf16")
+        ws = torch.empty(ea.attend_workspace_bytes(p, step, cap), dtype=torch.uint8, device="cuda").fill_(0xFF)
+        ea.attend_fp8(p, to_dev(q), step, to_dev(k8), to_dev(v8), to_dev(ks), to_dev(vs), i32(L), cap, cap, out, lse, ws)
+        torch.cuda.synchronize()
+        got, lse = to_host(out), lse.cpu().numpy()
+        k, v = (X.fp8_e4m3_decode(x) * s.astype(np.float64)[:, :, None, None] for x, s in ((k8, ks), (v8, vs)))
+    check_attend(got, lse, q, cu, k, v, L, "bf16")
+    assert (widen(got)[cu[-1]:] == 7.0).all() and (lse[cu[-1]:] == 7.0).all()
+
+
 def test_fp32_prompt():
     """Enough rows for the kernel whose wavefronts lie over the rows."""
     q, cu, k, v, L = attend_inputs(5, 8, 8, 64, "f32", [1100, 1000], [1100, 948])
