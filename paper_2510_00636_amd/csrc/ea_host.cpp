@@ -338,7 +338,10 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   // Up to 64 rows where their results fit the registers (d = 256: 32): 8 sequences over 4096 rows with 16 tokens of 4 heads 38.7 us, as
   // stretches 45.9, with 16 of 2 heads at d = 256 57 and 78 (8-bit rows 37.5 and 79).  One short sequence loses up to a tenth (d = 64,
   // 16k rows 23.5 and 21.6), and so do many (48 over 512 rows 47.5 and 42.5).
-  a.mt = most <= 16 ? 1 : most <= 32 ? 2 : most <= 64 && d.D <= 128 ? 4 : 1;
+  // Where some add more, the rows of single tokens: 24 sequences of up to 8192 rows, 3 of them adding 500 tokens, with 20 heads to a KV
+  // head at d = 256 381 -> 275 us, 24 at d = 128 217 -> 195 (64 at d = 64 157 and 158).
+  const int64_t fit = most <= (d.D <= 128 ? 64 : 32) ? most : d.G;
+  a.mt = fit <= 16 ? 1 : fit <= 32 ? 2 : fit <= 64 && d.D <= 128 ? 4 : 1;
   a.piece_rows = 16 * a.mt;
   a.short_rows = (int)(most < a.piece_rows ? most : a.piece_rows);
   // one sequence is one kernel's; of several that may be long some may be short
