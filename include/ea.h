@@ -354,7 +354,8 @@ ea_status ea_append_fp8(const ea_params* p, const ea_new_rows* rows, const int32
  * sequence b in the step, token i (0 .. m-1) of query head g sees the rows j < len - (m - 1 - i) of its KV
  * head h, len = lengths[b] (paged) or lengths[b, h]:
  *   out = sum_j softmax_j(q . k_j / sqrt(d)) v_j,   lse = ln sum_j exp(q . k_j / sqrt(d)).
- * A token that sees no row gets zeros and -inf.  Rows that a token does not see do not touch its results,
+ * A token that sees no row gets zeros and -inf, as does one whose logits are all -inf; a logit that it sees and that is
+ * NaN or +inf makes NaN of its out and its lse.  Rows that a token does not see do not touch its results,
  * whatever they hold; a value that is not finite in a row that it does see makes its channel not finite.
  *   q, out [n_tokens, Hq, d] in p->dtype (q_stride in the step, out dense), lse [n_tokens, Hq] fp32 or NULL
  *   n      no length is larger (HOST; larger ones count as n); 0 <= n <= 2^26

@@ -225,9 +225,10 @@ __device__ __forceinline__ void add_not_finite(const AttendArgs& a, int b, int h
   }
 }
 
-// base-2 logarithm of a row's sum and maximum -> natural log-sum-exp; -inf for a row that saw nothing
+// base-2 logarithm of a row's sum and maximum -> natural log-sum-exp; -inf for a row that saw nothing (and for no other: a sum
+// that is not a number has no logarithm either)
 __device__ __forceinline__ float natural_lse(float m, float l) {
-  return l > 0.0f ? fmaf(m, 0.6931471805599453f, logf(l)) : -__builtin_inff();
+  return l == 0.0f ? -__builtin_inff() : fmaf(m, 0.6931471805599453f, logf(l));
 }
 
 hipError_t launch_attend(const AttendArgs& a, const Dims& d, hipStream_t st);

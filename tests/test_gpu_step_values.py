@@ -1,0 +1,85 @@
+"""What a model's step makes of values at the ends of their types, far positions and loose bounds.
+
+Tolerances, derived before the first run, stand at each test.  A rounding is off by at most half a step: bf16 2^-8, fp32 2^-24,
+relative."""
+import numpy as np
+import pytest
+
+from ea_inputs import inv_freq_table, widen
+from ea_inputs.torch_io import to_dev, to_host
+from oracle import ea_extensions as X
+from oracle import ea_step as S
+import paper_2510_00636_amd as ea
+from tests.test_gpu_step import HALF, attend_bounds, attend_inputs, i32, kind, outputs, store
+
+pytestmark = pytest.mark.gpu
+
+
+def run_heads(q, cu, k, v, lens, dt, max_new=None, n=None, scales=(None, None)):
+    """The attention over contiguous caches, as stored (dt: bf16, f32 or fp8); out as fp64 numbers."""
+    import torch
+    B, hkv, cap, d = k.shape
+    st = "f32" if dt == "f32" else "bf16"
+    p = ea.make_params(B, q.shape[1], hkv, d, kind(st))
+    cud, n = i32(cu), cap if n is None else n
+    step = ea.make_step(cud, q.shape[0], int(np.diff(cu).max()) if max_new is None else max_new)
+    out, lse = outputs(q, st)
+    ws = torch.empty(ea.attend_workspace_bytes(p, step, n), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    qd, kd, vd, ld = to_dev(q), to_dev(k), to_dev(v), i32(lens)
+    if dt == "fp8":
+        ks, vs = (None if s is None else to_dev(s) for s in scales)
+        ea.attend_fp8(p, qd, step, kd, vd, ks, vs, ld, n, cap, out, lse, ws)
+    else:
+        ea.attend(p, qd, step, kd, vd, ld, n, cap, out, lse, ws)
+    torch.cuda.synchronize()
+    return widen(to_host(out)), lse.cpu().numpy()
+
+
+def tokens(cu, lens, g):
+    """(token, query head, sequence, KV head, rows that it sees) of every result"""
+    for b in range(len(cu) - 1):
+        m = cu[b + 1] - cu[b]
+        for i in range(m):
+            for h in range(lens.shape[1]):
+                for x in range(h * g, (h + 1) * g):
+                    yield cu[b] + i, x, b, h, max(0, int(lens[b, h]) - (m - 1 - i))
+
+
+# whole heads and heads that several workgroups share, few rows and stretches, every type
+KERNELS = [("bf16", 8, 2, 128, [2, 1, 1], [40, 5000, 1]), ("bf16", 6, 2, 64, [3, 5, 2], [90, 5000, 1]), ("bf16", 4, 2, 256, [1, 4, 2], [70, 4000, 1]),
+           ("bf16", 8, 2, 128, [100, 1, 70], [300, 20, 5000]), ("bf16", 16, 2, 64, [60, 3, 200], [61, 20, 3000]),
+           ("bf16", 4, 2, 256, [90, 2, 70], [200, 20, 3000]), ("fp8", 8, 2, 128, [2, 1, 90], [40, 3000, 2500]),
+           ("fp8", 4, 2, 256, [3, 60, 2], [5, 2000, 1]), ("f32", 4, 2, 64, [2, 30, 1], [40, 3000, 20]), ("f32", 8, 8, 64, [1500, 548, 2], [1500, 548, 1]),
+           ("f32", 3, 3, 256, [2, 9, 70], [4, 900, 300])]
+
+
+@pytest.mark.parametrize("dt,hq,hkv,d,m,lens", KERNELS)
+@pytest.mark.parametrize("what", ["nan", "infinite logit"])
+def test_a_sum_that_is_not_a_number_is_none_in_the_logarithm_either(dt, hq, hkv, d, m, lens, what):
+    """lse is -inf where a token sees no row and nowhere else: a key of NaN, or one whose logit is +inf, makes a NaN of the sum.
+    Tokens that do not see that key have what they have without it."""
+    if dt == "fp8" and what != "nan":
+        pytest.skip("no infinities in these bytes")
+    r = np.random.default_rng(d)
+    st, g = "f32" if dt == "f32" else "bf16", hq // hkv
+    lens = np.repeat(np.array(lens)[:, None], hkv, axis=1)
+    q, cu, k, v, L = attend_inputs(d + hq, hq, hkv, d, st, lens, m)
+    if dt == "fp8":
+        k, v = (r.integers(0, 0x60, k.shape).astype(np.uint8) for _ in range(2))
+    bad, row = k.copy(), lens[:, 0] - 1 - np.array(m) // 2
+    put = {"bf16": (0x7FC0, 0x7F80), "f32": (np.nan, np.inf), "fp8": (0x7F, None)}[dt][what != "nan"]
+    q[..., 3] = store(np.array([0.5]), st)[0]                  # so that an infinite key has an infinite logit, and no NaN
+    for b in range(3):
+        if row[b] >= 0:
+            bad[b, :, row[b], 3] = put
+    clean, clean_lse = run_heads(q, cu, k, v, L, dt)
+    got, lse = run_heads(q, cu, bad, v, L, dt)
+    for t, x, b, h, n in tokens(cu, L, g):
+        if n == 0:
+            assert (got[t, x] == 0).all() and lse[t, x] == -np.inf
+        elif n > row[b] >= 0:
+            assert np.isnan(got[t, x]).all() and np.isnan(lse[t, x]), (t, x, lse[t, x])
+        else:
+            assert np.isfinite(lse[t, x]) and np.isfinite(got[t, x]).all()
+            if what == "nan":      # (an infinite logit moves the maximum that its neighbours' weights are taken against)
+                assert np.array_equal(got[t, x], clean[t, x]) and lse[t, x] == clean_lse[t, x]
