@@ -225,10 +225,20 @@ __device__ __forceinline__ void add_not_finite(const AttendArgs& a, int b, int h
   }
 }
 
+// ---- Weights.  The maximum that a row's are taken against moves only when a logit passes it by more than kLag powers of two, which
+// saves most of the products that a move costs.  So that no weight passes one all the same (a value times 2^8 can pass the end of
+// fp32 where the value itself, and the result, do not) a weight is 2^-kLag of the power of two: the sums of weights and of weighted
+// values have the factor alike, and only the logarithm of the sum has to take it out again.
+constexpr float kLag = 8.0f;
+// the largest logit of a row as the reference that its weights are taken against: one that stays the same number plus and minus kLag
+__device__ __forceinline__ float reference(float top) { return (top + kLag) - kLag; }
+// what is subtracted from a row's logits: its reference and kLag; -inf (nothing seen so far) is taken for zero
+__device__ __forceinline__ float subtrahend(float m) { return m == -__builtin_inff() ? 0.0f : m + kLag; }
+
 // base-2 logarithm of a row's sum and maximum -> natural log-sum-exp; -inf for a row that saw nothing (and for no other: a sum
-// that is not a number has no logarithm either)
+// that is not a number has no logarithm either).  The sum is 2^-kLag of what it stands for.
 __device__ __forceinline__ float natural_lse(float m, float l) {
-  return l == 0.0f ? -__builtin_inff() : fmaf(m, 0.6931471805599453f, logf(l));
+  return l == 0.0f ? -__builtin_inff() : fmaf(m, 0.6931471805599453f, logf(l * 256.0f));
 }
 
 hipError_t launch_attend(const AttendArgs& a, const Dims& d, hipStream_t st);

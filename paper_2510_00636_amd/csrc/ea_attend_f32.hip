@@ -94,7 +94,7 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
       for (int r = 0; r < 4; ++r)
         if (key + 4 * g + r >= vis || key + 4 * g + r >= key_hi) s0[r] = -__builtin_inff();
     float top = fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3]));
-    if (__any(top > mx + 8.0f)) {
+    if (__any(top > mx + kLag)) {
       top = fmaxf(max_xor16(max_xor32(top)), mx);
       const float f = mx == -__builtin_inff() ? 0.0f : pow2(mx - top);
       mx = top;
@@ -102,11 +102,12 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) o[c] *= f;
     }
+    // (2^-kLag as a factor of its own: logits close to their maximum lose no bits to it)
     const float from = mx == -__builtin_inff() ? 0.0f : mx;
     float p[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      p[r] = pow2(s0[r] - from);
+      p[r] = pow2(s0[r] - from) * 0.00390625f;
       l += p[r];
     }
     // rows behind the last one weigh nothing, whatever they hold

@@ -335,8 +335,7 @@ __global__ __launch_bounds__(256, (D * MT > 256 || (D == 256 && !FP8) ? 1 : 2)) 
       load_k();
       if (following + kGroup < row_hi) following_blocks = look_up(cur, following + kGroup);
       __builtin_amdgcn_sched_barrier(0);
-      // ---- weights.  The maximum that they are taken against moves only when a row's passes it by more than 2^8: their sum and
-      // the weighted values stay far from either end of fp32 then, and the division at the end takes the factor out again.
+      // ---- weights (see kLag).
       // A weight reaches the second product as two bf16 numbers, which together are as good as fp32 next to the values' eight
       // bits: the matrix cores have time for it here.
       const bool ragged = row + 32 > len - (cur.m - 1);
@@ -351,15 +350,15 @@ __global__ __launch_bounds__(256, (D * MT > 256 || (D == 256 && !FP8) ? 1 : 2)) 
             if (row + (i >> 2) * 16 + 4 * g + (i & 3) >= vis[t]) s[t][i >> 2][i & 3] = -__builtin_inff();
         float top = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])),
                           fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
-        if (__any(top > mx[t] + 8.0f)) {
-          top = fmaxf(max_xor16(max_xor32(top)), mx[t]);
+        if (__any(top > mx[t] + kLag)) {
+          top = reference(fmaxf(max_xor16(max_xor32(top)), mx[t]));
           const float f = mx[t] == -__builtin_inff() ? 0.0f : pow2(mx[t] - top);
           mx[t] = top;
           l[t] *= f;
 #pragma unroll
           for (int c = 0; c < S::kTiles; ++c) o[t][c] *= f;
         }
-        const float from = mx[t] == -__builtin_inff() ? 0.0f : mx[t];
+        const float from = subtrahend(mx[t]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float lo = pow2(s[t][i >> 1][(i & 1) * 2] - from), hi = pow2(s[t][i >> 1][(i & 1) * 2 + 1] - from);

@@ -292,16 +292,15 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
     top *= qk;
-    // the maximum that weights are taken against moves only when a row's passes it by more than 2^8
-    if (__any(top > mx + 8.0f)) {
-      top = fmaxf(max_xor32(top), mx);
+    if (__any(top > mx + kLag)) {
+      top = reference(fmaxf(max_xor32(top), mx));
       const float f = mx == -__builtin_inff() ? 0.0f : pow2(mx - top);
       mx = top;
       l *= f;
 #pragma unroll
       for (int c = 0; c < kCt; ++c) o[c] *= f;
     }
-    const float from = mx == -__builtin_inff() ? 0.0f : mx;
+    const float from = subtrahend(mx);
     // weights of 16 keys at a time, one block ahead of the products that take them
     uint32_t p[kKt * 2][4];
     auto weigh = [&](int kb) {

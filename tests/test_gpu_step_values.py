@@ -83,3 +83,32 @@ def test_a_sum_that_is_not_a_number_is_none_in_the_logarithm_either(dt, hq, hkv,
             assert np.isfinite(lse[t, x]) and np.isfinite(got[t, x]).all()
             if what == "nan":      # (an infinite logit moves the maximum that its neighbours' weights are taken against)
                 assert np.array_equal(got[t, x], clean[t, x]) and lse[t, x] == clean_lse[t, x]
+
+
+@pytest.mark.parametrize("dt,hq,hkv,d,m", [("bf16", 64, 64, 128, 1), ("bf16", 128, 64, 64, 2), ("bf16", 64, 64, 256, 1), ("bf16", 8, 4, 128, 60),
+                                          ("bf16", 32, 4, 64, 90), ("bf16", 8, 4, 256, 70), ("f32", 8, 4, 64, 3), ("f32", 8, 4, 256, 30),
+                                          ("f32", 16, 16, 64, 1100)])
+@pytest.mark.parametrize("steps", [3.0, 7.5])
+def test_large_values_weigh_at_most_once(dt, hq, hkv, d, m, steps):
+    """One row of each head's 1600 has values of 2^126, and a logit that lies `steps` powers of two above the others', less than what moves
+    the maximum that weights are taken against.  The result is below 2^126, so it has to be finite: no weight may pass one.
+
+    The other values are zeros, so the result is 2^126 w / sum, where the exponent is off by the logit's error: d products and sums
+    and two roundings of a logit of at most 8 ln 2 (d + 10) 2^-24 8, and 2^-22 of the power; the sum of at most 1600 weights 2^-24 * 1600 / 8
+    + 64 2^-24; a weight's rounding to bf16 2^-8, and the result's."""
+    n = 1600
+    q, k, v = (store(np.zeros(s), dt) for s in ((m, hq, d), (1, hkv, n, d), (1, hkv, n, d)))
+    q[..., 0] = store(np.ones(1), dt)[0]
+    for h in range(hkv):                                       # all tokens see it, and some of whoever reads it have read others before
+        k[0, h, n - m - 5 - h * 71 % 481, 0] = store(np.array([steps * np.log(2.0) * np.sqrt(d)]), dt)[0]
+        v[0, h, n - m - 5 - h * 71 % 481] = store(np.array([2.0 ** 126]), dt)[0]
+    cu, lens = np.array([0, m]), np.full((1, hkv), n)
+    got, lse = run_heads(q, cu, k, v, lens, dt)
+    logit = widen(k)[0, 0].max() / np.sqrt(d)
+    seen = n - (m - 1 - np.arange(m))
+    z = np.exp(logit) + seen - 1
+    want = 2.0 ** 126 * np.exp(logit) / z
+    assert np.isfinite(got).all()
+    e = 8 * (d + 10) * 2.0 ** -24 + 2.0 ** -22 + 264 * 2.0 ** -24 + 2 * HALF[dt]
+    assert (np.abs(got / want[:, None, None] - 1) <= e).all(), np.abs(got / want[:, None, None] - 1).max() / e
+    assert (np.abs(lse - np.log(z)[:, None]) <= 8 * (d + 10) * 2.0 ** -24 + 2.0 ** -21 + 264 * 2.0 ** -24 + 2.0 ** -22 * np.log(z)[:, None]).all()
