@@ -112,3 +112,53 @@ def test_large_values_weigh_at_most_once(dt, hq, hkv, d, m, steps):
     e = 8 * (d + 10) * 2.0 ** -24 + 2.0 ** -22 + 264 * 2.0 ** -24 + 2 * HALF[dt]
     assert (np.abs(got / want[:, None, None] - 1) <= e).all(), np.abs(got / want[:, None, None] - 1).max() / e
     assert (np.abs(lse - np.log(z)[:, None]) <= 8 * (d + 10) * 2.0 ** -24 + 2.0 ** -21 + 264 * 2.0 ** -24 + 2.0 ** -22 * np.log(z)[:, None]).all()
+
+
+# --------------------------------------------------------------------------------------- weights as two numbers
+def opposite_values(seed, hq, hkv, d, dt, lens, m):
+    """Small logits, and values that take turns in sign: the result is small next to the values, so that what its own rounding
+    may be off by does not cover what a weight's rounding to one bf16 number would make."""
+    r = np.random.default_rng(seed)
+    B, n = len(m), int(np.max(lens))
+    cu = np.concatenate([[0], np.cumsum(m)])
+    q = store(0.02 * r.standard_normal((int(cu[-1]), hq, d)), "bf16")
+    k = r.standard_normal((B, hkv, n, d))
+    v = (1.0 + r.random((B, hkv, 1, d))) * np.where(np.arange(n) % 2, -1.0, 1.0)[:, None]
+    if dt == "fp8":
+        k8, v8 = (torch_e4m3(x) for x in (k, v))
+        return q, cu, k8, v8, X.fp8_e4m3_decode(k8), X.fp8_e4m3_decode(v8)
+    ks, vs = store(k, "bf16"), store(v, "bf16")
+    return q, cu, ks, vs, widen(ks), widen(vs)
+
+
+def torch_e4m3(x):
+    import torch
+    return torch.from_numpy(x).to(torch.float32).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+
+
+def two_number_bounds(want, n, d):
+    """As attend_bounds, where a weight reaches the second product as the sum of two bf16 numbers: what the second one leaves is
+    2^-8 of what the first one leaves, 2^-16 of the weight."""
+    tol, tol_lse = attend_bounds(want, "bf16", n, d)
+    return tol - (HALF["bf16"] - 2.0 ** -16) * want[2], tol_lse
+
+
+@pytest.mark.parametrize("dt,hq,hkv,d,m,max_new", [
+    ("bf16", 8, 2, 128, [1, 1, 1], 1), ("bf16", 8, 2, 128, [8, 3, 1], 8), ("bf16", 8, 2, 128, [16, 1, 9], 16), ("bf16", 14, 2, 64, [2, 1, 1], 2),
+    ("bf16", 40, 1, 64, [1, 1, 1], 1), ("bf16", 4, 2, 256, [1, 8, 16], 16), ("bf16", 20, 1, 256, [1, 1, 1], 1), ("bf16", 24, 1, 128, [1, 1, 1], 300),
+    ("fp8", 8, 2, 128, [1, 2, 4], 4), ("fp8", 8, 2, 128, [16, 3, 1], 16), ("fp8", 16, 8, 256, [1, 16, 3], 16), ("bf16", 8, 2, 128, [1], 1)])
+@pytest.mark.parametrize("n", [40, 900])
+def test_few_tokens_have_weights_of_two_numbers(dt, hq, hkv, d, m, max_new, n):
+    """Whatever the bounds say that there might be: with up to 16, 32 or 64 (token, head) rows per KV head a result is off by little
+    more than its own rounding."""
+    lens = np.array([[n - 2 * b] * hkv for b in range(len(m))])
+    q, cu, k, v, kf, vf = opposite_values(n + d, hq, hkv, d, dt, lens, m)
+    room = np.concatenate([q, np.zeros((max(0, max_new - len(q)), hq, d), dtype=q.dtype)])
+    got, lse = run_heads(room, cu, k, v, lens, dt, max_new=max_new)
+    t = len(q)
+    want = S.attend(widen(q), cu, kf, vf, lens)
+    tol, tol_lse = two_number_bounds(want, n, d)
+    worst = np.abs(got[:t] - want[0]) / tol
+    assert worst.max() <= 1, worst.max()
+    assert (np.abs(lse[:t] - want[1]) <= tol_lse).all()
+    assert (got[t:] == 7.0).all() and (lse[t:] == 7.0).all()
