@@ -361,12 +361,14 @@ ea_status ea_append_fp8(const ea_params* p, const ea_new_rows* rows, const int32
  *   n      no length is larger (HOST; larger ones count as n); 0 <= n <= 2^26
  * ea_attend: contiguous caches, bf16 or fp32; ea_attend_paged: bf16 pools; ea_attend_fp8: e4m3 bytes with
  * per-head scales as in ea_score_fp8 (q and out bf16, head_dim 128 or 256).
- * bf16: products of the bf16 values with fp32 sums; weights reach the second product as bf16 numbers (where
- * a sequence adds few tokens as the sum of two), sums and maxima stay fp32.  fp32: everything in fp32.
+ * bf16: products of the bf16 values with fp32 sums; weights reach the second product as bf16 numbers, those of
+ * sequences that add few tokens as the sum of two, sums and maxima stay fp32.  Few are up to 64 (token, head) rows per
+ * KV head (32 at d = 256) where max_new allows no sequence more than these, else up to G rounded up to 16, 32 or 64,
+ * so single tokens always (but not G > 32 at d = 256).  fp32: everything in fp32.
  * Values are weighted and summed in fp32 before the division, by weights of at most one: the sum of a token's |weight * value| has to
  * stay below 2^128.
- * The result does not depend on n_tokens, but how a long head is cut, and so the last bits, may depend on
- * n, max_new and n_tokens.  Same call, same bits.  `ws`: ea_attend_workspace_bytes(), 256-byte aligned, the
+ * How a long head is cut, and so the last bits, may depend on n, max_new and n_tokens; which sequences add few tokens
+ * on the smaller of max_new and n_tokens alone.  Same call, same bits.  `ws`: ea_attend_workspace_bytes(), 256-byte aligned, the
  * rules of the other calls; that function returns 0 for invalid arguments and at least 256 otherwise.
  * out must not overlap q or the cache. */
 typedef struct {

@@ -344,8 +344,10 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   a.mt = fit <= 16 ? 1 : fit <= 32 ? 2 : fit <= 64 && d.D <= 128 ? 4 : 1;
   a.piece_rows = 16 * a.mt;
   a.short_rows = (int)(most < a.piece_rows ? most : a.piece_rows);
-  // one sequence is one kernel's; of several that may be long some may be short
-  a.rows = !f32 && a.short_rows >= d.G && (most <= a.piece_rows || d.B > 1);
+  // max_new is a bound: whatever it allows, sequences that turn out to add few tokens are the row kernel's, with its weights.  One
+  // sequence's stretch pays two launches that find nothing to do (64 tokens of 32 heads over 128 rows 14.6 -> 17.9 us, over 16k 42 -> 46, 300
+  // tokens 103 -> 107), and its single tokens under a bound of 500 have their own kernel (4096 rows 27.9 -> 17.6, 32k 61 -> 36)
+  a.rows = !f32 && a.short_rows >= d.G;
   a.tile = f32 || most > a.piece_rows;
   a.shares = a.mt * d.D > 256 ? num_cu : 2 * num_cu;      // as many as run at once
   if (a.shares > kAttendShares) a.shares = kAttendShares;

@@ -146,7 +146,9 @@ def two_number_bounds(want, n, d):
 @pytest.mark.parametrize("dt,hq,hkv,d,m,max_new", [
     ("bf16", 8, 2, 128, [1, 1, 1], 1), ("bf16", 8, 2, 128, [8, 3, 1], 8), ("bf16", 8, 2, 128, [16, 1, 9], 16), ("bf16", 14, 2, 64, [2, 1, 1], 2),
     ("bf16", 40, 1, 64, [1, 1, 1], 1), ("bf16", 4, 2, 256, [1, 8, 16], 16), ("bf16", 20, 1, 256, [1, 1, 1], 1), ("bf16", 24, 1, 128, [1, 1, 1], 300),
-    ("fp8", 8, 2, 128, [1, 2, 4], 4), ("fp8", 8, 2, 128, [16, 3, 1], 16), ("fp8", 16, 8, 256, [1, 16, 3], 16), ("bf16", 8, 2, 128, [1], 1)])
+    ("fp8", 8, 2, 128, [1, 2, 4], 4), ("fp8", 8, 2, 128, [16, 3, 1], 16), ("fp8", 16, 8, 256, [1, 16, 3], 16), ("bf16", 8, 2, 128, [1], 1),
+    # one sequence, with bounds as a captured step has them
+    ("bf16", 8, 2, 128, [1], 500), ("bf16", 40, 8, 128, [3], 200), ("bf16", 4, 2, 256, [8], 64), ("fp8", 8, 2, 128, [4], 90)])
 @pytest.mark.parametrize("n", [40, 900])
 def test_few_tokens_have_weights_of_two_numbers(dt, hq, hkv, d, m, max_new, n):
     """Whatever the bounds say that there might be: with up to 16, 32 or 64 (token, head) rows per KV head a result is off by little
