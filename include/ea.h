@@ -340,7 +340,7 @@ typedef struct {
  *   ea_append_fp8    the same into e4m3 bytes: k / k_scale[b, h] and v / v_scale[b, h] (NULL = 1), rounded
  *                    to nearest even, saturating at +-448.  p->dtype EA_BF16, head_dim 128 or 256.
  * q_out [n_tokens, Hq, d] receives the rotated queries (with new->q; it may be q itself if that is dense).
- * k, v and q must not overlap the cache.  Two tokens with the same slot: the row holds pieces of either.
+ * k, v and q must not overlap the cache.  EA_ERR_UNSUPPORTED beyond 2^24 tokens.  Two tokens with the same slot: the row holds pieces of either.
  * p->rope_layout as everywhere; horizon, epsilon and the window's fields are not used. */
 ea_status ea_append_paged(const ea_params* p, const ea_new_rows* rows, const int64_t* slots, void* k_pool, void* v_pool,
                           const ea_paged* pg, void* q_out, void* stream);
@@ -370,7 +370,9 @@ ea_status ea_append_fp8(const ea_params* p, const ea_new_rows* rows, const int32
  * How a long head is cut, and so the last bits, may depend on n, max_new and n_tokens; which sequences add few tokens
  * on the smaller of max_new and n_tokens alone.  Same call, same bits.  `ws`: ea_attend_workspace_bytes(), 256-byte aligned, the
  * rules of the other calls; that function returns 0 for invalid arguments and at least 256 otherwise.
- * out must not overlap q or the cache. */
+ * out must not overlap q or the cache.
+ * EA_ERR_UNSUPPORTED: n_tokens > 2^24; and unless max_new lets no sequence add more than few tokens (fp32: always) also
+ * (n_tokens * G / r + B) * Hkv > 2^22 with r = 128 (fp32: 16), and pools whose blocks have 4 GiB or more with all KV heads. */
 typedef struct {
   const int32_t* cu_tokens; /* DEVICE [B + 1], ascending from 0                                      */
   int64_t n_tokens;         /* tokens that q, out and lse have room for                              */

@@ -58,7 +58,7 @@ struct PageMap {
 constexpr int kAttendGroup = 128;       // keys of a group of the row kernel, whose workgroups take whole ones
 constexpr int kAttendF32Rows = 16, kAttendF32LongRows = 64;      // (token, head) rows of a workgroup of the fp32 kernel
 constexpr int kAttendShares = 512;      // most workgroups of the row kernel
-constexpr int64_t kAttendMaxTokens = (int64_t)1 << 24;
+constexpr int64_t kAttendMaxTokens = (int64_t)1 << 24, kAttendMaxGrid = (int64_t)1 << 22;
 struct AttendPlan {
   int rows, tile;     // the row kernel serves sequences of few (token, head) rows per KV head, the tile (or fp32) kernel the others
   int mt;             // 16-row operands of the row kernel

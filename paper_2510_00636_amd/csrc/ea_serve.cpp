@@ -35,12 +35,12 @@ static ea_status attend(const Dims& d, const void* q, const ea_step* step, const
   const size_t cache = (pm ? ((size_t)pm->num_blocks << pm->sh) * d.Hkv : (size_t)d.units() * n_cap) * d.D * d.esize();
   if (overlap(out, out_bytes, k, cache) || overlap(out, out_bytes, v, cache)) return EA_ERR_INVALID_ARG;
   a.plan = make_attend_plan(d, n, step->n_tokens, step->max_new, kPlanCus);
+  // Workgroups of up to 512 threads, 2^32 threads to a launch.  (The launches of few rows are no larger than 512 shares, their
+  // joining one than 512 times 64 rows; the stretches' joining one comes with few tiles only.)
+  if (a.plan.tile && a.plan.grid > kAttendMaxGrid) return EA_ERR_UNSUPPORTED;
+  // the stretches' kernel steps over a block by a 32-bit number of bytes
+  if (pm && a.plan.tile && (((uint64_t)d.Hkv << pm->sh) * d.D * d.esize()) >> 32) return EA_ERR_UNSUPPORTED;
   if (ws_bytes < a.plan.total) return EA_ERR_WORKSPACE;
-  // (workgroups of up to 512 threads, 2^32 threads to a launch)
-  const int64_t most = (int64_t)1 << 22;
-  if (a.plan.grid > most || (int64_t)d.units() * a.plan.short_rows > most) return EA_ERR_UNSUPPORTED;
-  // (the kernels step over a block by a 32-bit number of bytes)
-  if (pm && (((uint64_t)d.Hkv << pm->sh) * d.D * d.esize()) >> 32) return EA_ERR_UNSUPPORTED;
   if (step->n_tokens == 0) return EA_OK;
   a.q = q; a.k = k; a.v = v; a.cu = step->cu_tokens; a.lens = lengths; a.kscale = kscale; a.vscale = vscale;
   a.out = out; a.lse = lse; a.ws = (char*)ws;

@@ -164,3 +164,55 @@ def test_few_tokens_have_weights_of_two_numbers(dt, hq, hkv, d, m, max_new, n):
     assert worst.max() <= 1, worst.max()
     assert (np.abs(lse[:t] - want[1]) <= tol_lse).all()
     assert (got[t:] == 7.0).all() and (lse[t:] == 7.0).all()
+
+
+# ------------------------------------------------------------------------------------------- calls that are large
+def test_many_heads_that_add_few_tokens():
+    """131072 heads of up to four rows, under a bound of 16 tokens: no launch grows with heads times bound."""
+    r = np.random.default_rng(4)
+    B, hq, hkv, d, cap = 4096, 128, 32, 64, 4
+    m = np.where(r.random(B) < 0.9, 1, r.integers(0, 4, B))
+    lens = r.integers(0, cap + 1, (B, hkv))
+    q, cu, k, v, L = attend_inputs(1, hq, hkv, d, "bf16", lens, m, cap=cap)
+    got, lse = run_heads(q, cu, k, v, L, "bf16", max_new=16)
+    assert (lse[:cu[-1]] != 7.0).all()
+    some = np.unique(np.r_[0, 1, 2, r.integers(0, B, 12), B - 1])
+    at = np.concatenate([np.arange(cu[b], cu[b + 1]) for b in some])
+    part = np.concatenate([[0], np.cumsum(m[some])])
+    want = S.attend(widen(q[at]), part, widen(k[some]), widen(v[some]), L[some])
+    tol, tol_lse = attend_bounds(want, "bf16", cap, d)
+    assert (np.abs(got[at] - want[0]) <= tol).all()
+    none = want[1] == -np.inf
+    assert (lse[at][none] == -np.inf).all() and (np.abs(lse[at][~none] - want[1][~none]) <= tol_lse[~none]).all()
+
+
+def test_blocks_of_four_gib():
+    """A block that has 4 GiB with its heads together: few tokens read it, stretches are refused."""
+    import torch
+    B, heads, d, bs, nb, n = 1, 128, 256, 65536, 2, 70
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    q, cu, k, v, L = attend_inputs(2, heads, heads, d, "bf16", [n], [1])
+    pools = [torch.full((nb, heads, bs, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for pool, x in zip(pools, (k, v)):
+        pool[1, :, :n] = to_dev(x[0])
+    p, cud, table = ea.make_params(B, heads, heads, d, ea.EA_BF16), i32(cu), i32([[1]])
+    pg, (out, lse), qd = ea.make_paged(table, bs, nb), outputs(q, "bf16"), to_dev(q)
+    for bound in (1, 40):
+        room = torch.zeros(bound, heads, d, dtype=torch.bfloat16, device="cuda")
+        room[:1] = qd
+        to = torch.zeros_like(room)
+        step = ea.make_step(cud, bound, bound)
+        ws = torch.empty(ea.attend_workspace_bytes(p, step, n), dtype=torch.uint8, device="cuda")
+        if bound == 40:
+            with pytest.raises(ea.EaError) as e:
+                ea.attend_paged(p, room, step, pools[0], pools[1], pg, i32(L[:, 0]), n, to, None, ws)
+            assert e.value.code == 2 and not to.any()
+            continue
+        ea.attend_paged(p, room, step, pools[0], pools[1], pg, i32(L[:, 0]), n, out, lse, ws)
+        torch.cuda.synchronize()
+        want = S.attend(widen(q), cu, widen(k), widen(v), L)
+        tol, tol_lse = attend_bounds(want, "bf16", n, d)
+        assert (np.abs(widen(to_host(out)) - want[0]) <= tol).all() and (np.abs(lse.cpu().numpy() - want[1]) <= tol_lse).all()
+    pools.clear()
+    torch.cuda.empty_cache()

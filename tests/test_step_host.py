@@ -134,3 +134,18 @@ def test_new_rows_take_views_of_one_projection():
         ea.make_new_rows(None, k.transpose(0, 1), v)
     with pytest.raises(ValueError):
         ea.make_new_rows(None, k[..., ::2], v)
+
+
+def test_limits_come_before_the_workspace(lib):
+    """What no workspace helps is said first, and what the launches of few rows do not need is no limit."""
+    def call(p, t, new, hq, pg=None, wsb=16):
+        st = EaStep(2 * OK, t, new, 0)
+        f = (lib.ea_attend_paged, (byref(pg), at(6), 16)) if pg else (lib.ea_attend, (at(6), 16, 16))
+        return f[0](byref(p), VP(1 << 50), byref(st), at(4), at(5), *f[1], VP(1 << 52), None, at(8), wsb, None)
+    heads = bf16(batch=1 << 14, hq=64, hkv=64)
+    assert call(heads, 1 << 24, 1 << 20, 64) == 2                            # stretches: too many tiles
+    assert call(heads, 1 << 24, 16, 64) == 3                                 # few tokens each: no tiles
+    assert call(bf16(batch=1 << 14, hq=64, hkv=64, dtype=ea.EA_F32), 1 << 24, 1, 64) == 2
+    big = EaPaged(10 * OK, 65536, 1, 2)
+    assert call(bf16(batch=1, hq=128, hkv=128, d=256), 4, 40, 128, big) == 3 # (no sequence adds more than 4 of 4 tokens)
+    assert call(bf16(batch=1, hq=128, hkv=128, d=256), 40, 40, 128, big) == 2
