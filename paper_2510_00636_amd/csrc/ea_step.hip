@@ -223,12 +223,17 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
   }
   if (a.inv_freq) {
     for (int c = tid; c < D / 2; c += 256) {
-      // whole turns taken out in fp64: what is left keeps 2^-31 of a turn at any position of 32 bits
-      double y = (double)a.pos[token] * a.inv_freq[c] * 0.15915494309189533577;
-      y -= rint(y);
+#pragma clang fp contract(off)
+      // The angle is the fp64 product.  Its whole half turns go out in fp64, with what the product with 1 / pi rounded away and what fp64
+      // leaves of that number: without, an angle near 2^31 is off by 2^-24 of a turn.  What is left goes in as an fp32 number and its
+      // remainder, by which sine and cosine turn on, so that they are off by those functions' own error at any position.
+      const double angle = (double)a.pos[token] * a.inv_freq[c], inv_pi = 0.31830988618379067154, inv_pi_lo = -1.9678676675182485e-17;
+      const double turns = angle * inv_pi, whole = 2.0 * rint(0.5 * turns);
+      const double rest = (turns - whole) + fma(angle, inv_pi_lo, fma(angle, inv_pi, -turns));
+      const float half_turns = (float)rest, more = (float)(rest - (double)half_turns) * 3.14159265f;
       float si, co;
-      sincospif((float)(2.0 * y), &si, &co);
-      turn[c] = make_float2(co, si);
+      sincospif(half_turns, &si, &co);
+      turn[c] = make_float2(fmaf(-si, more, co), fmaf(co, more, si));
     }
     __syncthreads();
   }

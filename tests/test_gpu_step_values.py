@@ -216,3 +216,31 @@ def test_blocks_of_four_gib():
         assert (np.abs(widen(to_host(out)) - want[0]) <= tol).all() and (np.abs(lse.cpu().numpy() - want[1]) <= tol_lse).all()
     pools.clear()
     torch.cuda.empty_cache()
+
+
+# ----------------------------------------------------------------------------------------------- far positions
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("far", [1 << 12, 1 << 24, 1 << 31])
+def test_angles_of_far_positions(d, inter, far):
+    """Pairs (1, 0) become (cos, sin) of their angle, the fp64 product of position and frequency.  What the reduction leaves is rounded
+    to fp32 with its remainder kept, sine and cosine of it are off by two steps at most (2 * 2^-24 below one), the remainder's sum by
+    half a step."""
+    import torch
+    r = np.random.default_rng(far % 1000 + d)
+    t = 3000
+    pos = r.integers(far // 2, far, t)
+    pos[0] = far - 1
+    x = np.zeros((t, 2, d), dtype=np.float32)
+    x[:, :, slice(0, None, 2) if inter else slice(0, d // 2)] = 1.0
+    inv = inv_freq_table(d, 1e4)
+    q, cache = torch.zeros(t, 1, d, device="cuda"), [torch.zeros(1, 1, t, d, device="cuda") for _ in range(2)]
+    xd = to_dev(x)
+    p = ea.make_params(1, 1, 1, d, ea.EA_F32, rope_layout=int(inter))
+    rows = ea.make_new_rows(xd[:, :1], xd[:, 1:], xd[:, 1:], i32(pos), to_dev(inv))
+    ea.append(p, rows, i32([0, t]), i32([[t]]), cache[0], cache[1], t, q)
+    torch.cuda.synchronize()
+    want = S.rotate(x.astype(np.float64), pos, inv, inter)
+    tol = 2 * 2.0 ** -24 + 2.0 ** -25
+    for got, w in ((to_host(q)[:, 0], want[:, 0]), (to_host(cache[0])[0, 0], want[:, 1])):
+        assert np.abs(got - w).max() <= tol, np.abs(got - w).max() / tol
