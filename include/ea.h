@@ -366,7 +366,8 @@ ea_status ea_append_fp8(const ea_params* p, const ea_new_rows* rows, const int32
  * KV head (32 at d = 256) where max_new allows no sequence more than these, else up to G rounded up to 16, 32 or 64,
  * so single tokens always (but not G > 32 at d = 256).  fp32: everything in fp32.
  * Values are weighted and summed in fp32 before the division, by weights of at most one: the sum of a token's |weight * value| has to
- * stay below 2^128.
+ * stay below 2^128.  Numbers below 2^-126, values, weights and results, may count as zeros in bf16 and 8-bit caches; in fp32 they do
+ * not, but weighted values are whole multiples of 2^-149.
  * How a long head is cut, and so the last bits, may depend on n, max_new and n_tokens; which sequences add few tokens
  * on the smaller of max_new and n_tokens alone.  Same call, same bits.  `ws`: ea_attend_workspace_bytes(), 256-byte aligned, the
  * rules of the other calls; that function returns 0 for invalid arguments and at least 256 otherwise.

@@ -244,3 +244,26 @@ def test_angles_of_far_positions(d, inter, far):
     tol = 2 * 2.0 ** -24 + 2.0 ** -25
     for got, w in ((to_host(q)[:, 0], want[:, 0]), (to_host(cache[0])[0, 0], want[:, 1])):
         assert np.abs(got - w).max() <= tol, np.abs(got - w).max() / tol
+
+
+# ---------------------------------------------------------------------------------------------- small values
+@pytest.mark.parametrize("dt,hq,hkv,d,m", [("bf16", 8, 2, 128, 1), ("bf16", 4, 2, 64, 1), ("bf16", 4, 2, 256, 2), ("bf16", 8, 2, 128, 60), ("bf16", 16, 2, 64, 90),
+                                          ("bf16", 4, 2, 256, 70), ("f32", 4, 2, 64, 3), ("f32", 4, 2, 256, 30), ("f32", 8, 8, 64, 2100)])
+def test_values_below_the_smallest_normal_number(dt, hq, hkv, d, m):
+    """Values of 1 to 15 times 2^-130 that all weigh the same: in fp32 a token has the mean of those that it sees, in bf16 that or zero.
+
+    A weight is 2^-8, or a number above that: products are whole multiples of 2^-138 and so are their sums, exact as long as they stay
+    below 2^-126 and rounded to 24 bits above; the quotient is off by 2^-22 of itself and half of fp32's last step, 2^-150."""
+    r = np.random.default_rng(d + m)
+    n = 2400
+    m = min(m, n)
+    k, v = np.zeros((1, hkv, n, d)), r.integers(1, 16, (1, hkv, n, d)) * 2.0 ** -130
+    qs, ks, vs = store(r.standard_normal((m, hq, d)), dt), store(k, dt), store(v, dt)
+    assert np.array_equal(widen(vs), v)
+    cu, lens = np.array([0, m]), np.full((1, hkv), n)
+    got, lse = run_heads(qs, cu, ks, vs, lens, dt)
+    seen = n - (m - 1 - np.arange(m))
+    want = (np.cumsum(v[0], axis=1)[:, seen - 1] / seen[:, None]).transpose(1, 0, 2)      # [m, hkv, d]
+    want = np.repeat(want, hq // hkv, axis=1)
+    tol = 2.0 ** -22 * want + 2.0 ** -150 if dt == "f32" else 2.0 ** -126
+    assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
