@@ -112,7 +112,8 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
   const bool in = row < rows;
   const int vis = in ? len - (m - 1 - tok) : len;
   const int vis_min = len - (m - 1 - (row0 + wave * 32) / a.G);      // of the wavefront's rows
-  // (a scale's sign goes to the queries, so that logits order like their products, and a scale of zero leaves masked ones -inf)
+  // (a scale's sign goes to the queries, so that logits order like their products, and a scale of zero leaves masked ones -inf; so
+  // does a scale that is not a number, which goes to the queries, too)
   const float scale = FP8 && a.kscale ? a.kscale[unit] : 1.0f, qk = a.scale * fmaxf(fabsf(scale), 1e-30f);
   bf16x8 q[kSteps];
   {
@@ -122,6 +123,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
       bf16x8 w = *(const bf16x8*)(src + s * 16 + hi * 8);
       if (!in) w = (bf16x8)(__bf16)0.0f;
       if (FP8 && scale < 0.0f) w = -w;
+      if (FP8 && scale != scale) w = (bf16x8)(__bf16)scale;
       q[s] = w;
     }
   }

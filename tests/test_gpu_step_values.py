@@ -267,3 +267,23 @@ def test_values_below_the_smallest_normal_number(dt, hq, hkv, d, m):
     want = np.repeat(want, hq // hkv, axis=1)
     tol = 2.0 ** -22 * want + 2.0 ** -150 if dt == "f32" else 2.0 ** -126
     assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
+
+
+@pytest.mark.parametrize("d", [128, 256])
+@pytest.mark.parametrize("m", [[1, 1], [2, 90], [100, 80]])
+def test_a_scale_that_is_not_a_number(d, m):
+    """What a head's scale makes of its keys reaches every token that sees one of them; a token that sees none has zeros and -inf."""
+    r = np.random.default_rng(d)
+    lens = np.array([[300, m[0] - 1], [700, 500]])
+    cu = np.concatenate([[0], np.cumsum(m)])
+    q = store(r.standard_normal((int(cu[-1]), 8, d)), "bf16")
+    k, v = (r.integers(0, 0x60, (2, 2, 700, d)).astype(np.uint8) for _ in range(2))
+    ks = np.array([[1.0, np.nan], [np.nan, 0.5]], dtype=np.float32)
+    got, lse = run_heads(q, cu, k, v, lens, "fp8", scales=(ks, None))
+    for t, x, b, h, n in tokens(cu, lens, 4):
+        if n == 0:
+            assert (got[t, x] == 0).all() and lse[t, x] == -np.inf
+        elif np.isnan(ks[b, h]):
+            assert np.isnan(got[t, x]).all() and np.isnan(lse[t, x])
+        else:
+            assert np.isfinite(got[t, x]).all() and np.isfinite(lse[t, x])
