@@ -356,18 +356,34 @@ def block_tables(p, pg, len_old, len_new, free_list, free_in, len_out, free_out,
 
 
 def _token_stride(t):
-    """Elements from one token to the next of t [n_tokens, heads, d]; a token's heads have to stand together."""
-    if t.stride(-1) != 1 or t.stride(-2) != t.shape[-1]:
-        raise ValueError("the heads of a token must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else 0
+    """Elements from one token to the next of t [n_tokens, heads, d]; a token's heads have to stand together, and no two tokens in
+    one place (0 would stand for dense rows, more of them than there are)."""
+    if t.dim() != 3 or t.stride(-1) != 1 or (t.shape[-2] > 1 and t.stride(-2) != t.shape[-1]):
+        raise ValueError("rows are [tokens, heads, d], the heads of a token contiguous")
+    if t.shape[0] < 2:
+        return 0
+    if t.stride(0) < t.shape[-2] * t.shape[-1]:
+        raise ValueError("tokens must not share memory")
+    return t.stride(0)
 
 
 def make_new_rows(q, k, v, pos=None, inv_freq=None):
-    """ea_new_rows for tensors q (or None) [n_tokens, Hq, d], k, v [n_tokens, Hkv, d]; views into one projection's rows will do."""
+    """ea_new_rows for tensors q (or None) [n_tokens, Hq, d], k, v [n_tokens, Hkv, d]; views into one projection's rows will do.
+    pos int32 [n_tokens or more], inv_freq float64 [d / 2]."""
     def ptr(t):
         return None if t is None else t.data_ptr()
-    r = EaNewRows(ptr(q), ptr(k), ptr(v), 0 if q is None else _token_stride(q), _token_stride(k), _token_stride(v), k.shape[0],
-                  ptr(pos), ptr(inv_freq))
+    strides = [0 if t is None else _token_stride(t) for t in (q, k, v)]
+    # the library reads as many rows of each as k has
+    if v.shape != k.shape or (q is not None and (q.shape[0], q.shape[2]) != (k.shape[0], k.shape[2])):
+        raise ValueError("q, k and v must have the same tokens and channels, k and v the same heads")
+    if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
+        raise ValueError("q, k and v must have one type")
+    if inv_freq is not None:
+        if pos is None or pos.numel() < k.shape[0] or pos.element_size() != 4 or not pos.is_contiguous():
+            raise ValueError("pos must be int32, one for each token")
+        if inv_freq.numel() != k.shape[2] // 2 or inv_freq.element_size() != 8 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be float64 [d / 2]")
+    r = EaNewRows(ptr(q), ptr(k), ptr(v), *strides, k.shape[0], ptr(pos), ptr(inv_freq))
     r.tensors = (q, k, v, pos, inv_freq)      # alive as long as the addresses are kept
     return r
 

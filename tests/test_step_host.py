@@ -149,3 +149,27 @@ def test_limits_come_before_the_workspace(lib):
     big = EaPaged(10 * OK, 65536, 1, 2)
     assert call(bf16(batch=1, hq=128, hkv=128, d=256), 4, 40, 128, big) == 3 # (no sequence adds more than 4 of 4 tokens)
     assert call(bf16(batch=1, hq=128, hkv=128, d=256), 40, 40, 128, big) == 2
+
+
+def test_new_rows_that_are_not_there():
+    """Tensors whose rows the library would read past: expanded ones, too few of q, v or the positions, other types."""
+    import torch
+    bf = dict(dtype=torch.bfloat16)
+    q, k, v = (torch.zeros(6, h, 64, **bf) for h in (4, 2, 2))
+    pos, inv = torch.zeros(6, dtype=torch.int32), torch.zeros(32, dtype=torch.float64)
+    assert ea.make_new_rows(q, k, v, pos, inv).n_tokens == 6
+    one = torch.zeros(1, 2, 64, **bf)
+    for bad in ((None, one.expand(6, 2, 64), v), (None, k, one.expand(6, 2, 64)), (torch.zeros(1, 4, 64, **bf).expand(6, 4, 64), k, v),
+                (None, k.as_strided((6, 2, 64), (64, 64, 1)), v),               # tokens over one another
+                (q[:5], k, v), (None, k, v[:5]), (None, k, torch.zeros(6, 3, 64, **bf)), (torch.zeros(6, 4, 128, **bf), k, v),
+                (q.float(), k, v), (None, k, v.float()), (None, k.view(6, 128), v)):
+        with pytest.raises(ValueError):
+            ea.make_new_rows(*bad, pos, inv)
+    for bad in ((pos[:5], inv), (None, inv), (pos.long(), inv), (pos, inv[:31]), (pos, inv.float()), (torch.zeros(12, dtype=torch.int32)[::2], inv)):
+        with pytest.raises(ValueError):
+            ea.make_new_rows(q, k, v, *bad)
+    assert ea.make_new_rows(None, k, v, None, None).k_stride == 128             # stored as they are
+    # one token is one place, whatever its stride; one head is contiguous, whatever the stride between heads
+    assert ea.make_new_rows(None, one.expand(1, 2, 64), one).k_stride == 0
+    thin = torch.zeros(1, 6, 64, **bf).transpose(0, 1)
+    assert thin.stride(1) != 64 and ea.make_new_rows(None, thin, thin).k_stride == 64
