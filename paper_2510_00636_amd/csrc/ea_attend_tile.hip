@@ -41,10 +41,12 @@ template <int D, bool FP8> __host__ __device__ constexpr int k_row(int row) {
 }
 
 // 16 bytes per lane from base + at to LDS address `to` and on, lanes in order.  Nothing waits for it but the s_waitcnt in front of
-// the barrier behind which the tile is read; the compiler, told of such a load, would wait at the next read of any LDS.  (m0 is
-// nobody else's here: LDS instructions of this chip do not read it.)
+// the barrier behind which the tile is read; the compiler, told of such a load, would wait at the next read of any LDS.  m0,
+// which the load takes its address from when it is issued, is left as it was: the compiler does not let it be named as changed.
 __device__ __forceinline__ void to_lds(uint32_t to, const void* base, uint32_t at) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(to), "v"(at), "s"(base) : "memory");
+  uint32_t m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "s"(to), "v"(at), "s"(base) : "memory");
 }
 
 // The order in which a block's instructions are issued: operands from LDS a few products ahead (left to itself the compiler
