@@ -325,8 +325,6 @@ ea_status ea_compact(const ea_params* p, const void* k, const void* v, int64_t n
   return EA_OK;
 }
 
-// ea_paged -> PageMap, validated on the host (the table's entries are device memory: the kernels
-// clamp them into the pool)
 // unordered: the order-free compaction (perm_out then receives the source row of every position)
 // pm: the caches are block pools (n_cap is then not used)
 static ea_status compress_impl(const ea_params* p, const void* q_win, int64_t window,

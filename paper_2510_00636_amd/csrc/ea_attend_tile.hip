@@ -5,8 +5,8 @@
 // lane then holds half of the keys of its row, and what it holds is, as it stands, the operand of the second product if V^T has
 // its keys in the same order.  V^T comes out of the row-major tile by ds_read_b64_tr_b16.
 //
-// 2048 tokens of 32 heads over 32k rows, d = 128: 1010 us, 1120 TFLOP/s of the 1189 that a large library product has on this card; the
-// matrix cores are busy in 58 % of the cycles at the 1.79 GHz that the chip's power leaves.  d = 256 1030 TFLOP/s (1100 without block
+// 2048 tokens of 32 heads over 32k rows, d = 128: 997 us (980 to 1046 from card to card), 1137 TFLOP/s of the 1189 that a large library
+// product has; the matrix cores are busy in 54 % of the cycles at the 1.85 GHz that the chip's power leaves.  d = 256 1030 TFLOP/s (1100 without block
 // tables), d = 64 780 (its exponentials cost as much as its products), 8-bit rows 980.
 #include "ea_attend.h"
 
@@ -305,7 +305,11 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
       for (int c = 0; c < kCt; ++c) o[c] *= f;
     }
     const float from = subtrahend(mx);
-    // weights of 16 keys at a time, one block ahead of the products that take them
+    // Weights of 16 keys at a time, one block ahead of the products that take them, each rounded to one bf16 number; the sum is of the
+    // unrounded ones.  The matrix cores bound this kernel, and they have no product of wider weights with bf16 values: as the sum of
+    // two numbers (as in the kernel of few rows, which the cache's bytes bound) 2048 tokens over 34k rows take 1422 us and not 997, 2 x
+    // 1024 over 4096 rows 121 and not 93 at d = 64, 190 and not 147 at d = 256.  What one number costs in turn is 2^-8 of the weighted
+    // mean of |v| at most, and measured errors of 1.3 to 1.4 times those of results that are only rounded at the end.
     uint32_t p[kKt * 2][4];
     auto weigh = [&](int kb) {
 #pragma unroll

@@ -304,6 +304,7 @@ WsLayout make_ws_layout(const Dims& d, int64_t n, int64_t window) {
   return w;
 }
 
+// ea_paged -> PageMap (the table's entries are device memory: the kernels clamp them into the pool)
 ea_status check_paged(const Dims& d, const ea_paged* pg, int64_t n, PageMap* pm) {
   if (!pg || !pg->block_table || ((uintptr_t)pg->block_table & 3u)) return EA_ERR_INVALID_ARG;
   const int64_t bs = pg->block_size;
@@ -349,7 +350,8 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   // tokens 103 -> 107), and its single tokens under a bound of 500 have their own kernel (4096 rows 27.9 -> 17.6, 32k 61 -> 36)
   a.rows = !f32 && a.short_rows >= d.G;
   a.tile = f32 || most > a.piece_rows;
-  a.shares = a.mt * d.D > 256 ? num_cu : 2 * num_cu;      // as many as run at once
+  // as many as run at once (but at d = 256 over bf16 rows, whose registers let half of them in at a time)
+  a.shares = a.mt * d.D > 256 ? num_cu : 2 * num_cu;
   if (a.shares > kAttendShares) a.shares = kAttendShares;
   // fp32: wavefronts over rows where those give every CU a workgroup, else over keys (1024 tokens of 2 x 8 KV heads over 2048 rows 655
   // and 690 us, 64 tokens of 2 KV heads 21 and 14)

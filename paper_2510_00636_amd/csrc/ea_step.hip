@@ -156,8 +156,9 @@ hipError_t launch_block_tables(const BlockTableArgs& a, hipStream_t st) {
 // ---------------------------------------------------------------------------------- new rows
 // A workgroup takes 256 stretches of one token's rows: the token's angles go through LDS once (fp64 product and reduction to one turn,
 // fp32 sine and cosine), then every thread turns 8 pairs of channels of a head and stores them.  Values take the same way unturned.
-// Memory bounds long calls: every row is read and written once, 16 bytes a lane (8192 tokens of 32 + 8 + 8 heads of 128 channels
-// 32.5 us, 6.2 TB/s; four tokens to a workgroup 35.8); latency the short ones (48 tokens 3 us).
+// Memory bounds long calls: every row is read and written once, 16 bytes a lane (8192 tokens of 32 + 8 + 8 heads of 128 channels 40.6
+// us with cold caches, 4.96 TB/s, where a large copy has 4.89; 201 MB, which the last-level cache holds, in a row 32.5, four tokens to
+// a workgroup 35.8); latency the short ones (48 tokens 3 us).
 namespace {
 
 template <typename T> struct Eight;                  // eight channels as they stand in memory
