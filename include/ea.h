@@ -373,7 +373,8 @@ ea_status ea_append_fp8(const ea_params* p, const ea_new_rows* rows, const int32
  * rules of the other calls; that function returns 0 for invalid arguments and at least 256 otherwise.
  * out must not overlap q or the cache.
  * EA_ERR_UNSUPPORTED: n_tokens > 2^24; and unless max_new lets no sequence add more than few tokens (fp32: always) also
- * (n_tokens * G / r + B) * Hkv > 2^22 with r = 128 (fp32: 16), and pools whose blocks have 4 GiB or more with all KV heads. */
+ * (n_tokens * G / r + B) * Hkv > 2^22, with r = 128 or 256 (fp32: 16 or 64) as the call is cut, and pools whose blocks
+ * have 4 GiB or more with all KV heads. */
 typedef struct {
   const int32_t* cu_tokens; /* DEVICE [B + 1], ascending from 0                                      */
   int64_t n_tokens;         /* tokens that q, out and lse have room for                              */

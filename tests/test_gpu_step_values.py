@@ -53,13 +53,11 @@ KERNELS = [("bf16", 8, 2, 128, [2, 1, 1], [40, 5000, 1]), ("bf16", 6, 2, 64, [3,
            ("f32", 3, 3, 256, [2, 9, 70], [4, 900, 300])]
 
 
-@pytest.mark.parametrize("dt,hq,hkv,d,m,lens", KERNELS)
-@pytest.mark.parametrize("what", ["nan", "infinite logit"])
-def test_a_sum_that_is_not_a_number_is_none_in_the_logarithm_either(dt, hq, hkv, d, m, lens, what):
+@pytest.mark.parametrize("what,dt,hq,hkv,d,m,lens", [(w, *x) for x in KERNELS for w in ("nan", "infinite logit")
+                                                     if x[0] != "fp8" or w == "nan"])      # (these bytes have no infinities)
+def test_a_sum_that_is_not_a_number_is_none_in_the_logarithm_either(what, dt, hq, hkv, d, m, lens):
     """lse is -inf where a token sees no row and nowhere else: a key of NaN, or one whose logit is +inf, makes a NaN of the sum.
     Tokens that do not see that key have what they have without it."""
-    if dt == "fp8" and what != "nan":
-        pytest.skip("no infinities in these bytes")
     r = np.random.default_rng(d)
     st, g = "f32" if dt == "f32" else "bf16", hq // hkv
     lens = np.repeat(np.array(lens)[:, None], hkv, axis=1)
@@ -83,6 +81,34 @@ def test_a_sum_that_is_not_a_number_is_none_in_the_logarithm_either(dt, hq, hkv,
             assert np.isfinite(lse[t, x]) and np.isfinite(got[t, x]).all()
             if what == "nan":      # (an infinite logit moves the maximum that its neighbours' weights are taken against)
                 assert np.array_equal(got[t, x], clean[t, x]) and lse[t, x] == clean_lse[t, x]
+
+
+@pytest.mark.parametrize("dt,hq,hkv,d,m,lens", [x for x in KERNELS if x[0] != "fp8"])
+def test_logits_that_are_all_minus_infinity(dt, hq, hkv, d, m, lens):
+    """Such a token has zeros and -inf, like one that sees nothing; a logit of -inf among others weighs nothing."""
+    st, g = "f32" if dt == "f32" else "bf16", hq // hkv
+    lens = np.repeat(np.array(lens)[:, None], hkv, axis=1)
+    q, cu, k, v, L = attend_inputs(d + hq, hq, hkv, d, st, lens, m)
+    q[..., 3] = store(np.array([0.5]), st)[0]
+    minus = 0xFF80 if dt == "bf16" else -np.inf
+    k[0, :, :, 3] = minus
+    last = np.maximum(lens[2, 0] - m[2] - 1, 0)                # of the third sequence one row that all its tokens see, if there is one
+    k[2, :, last, 3] = minus
+    got, lse = run_heads(q, cu, k, v, L, dt)
+    for t, x, b, h, n in tokens(cu, L, g):
+        if b == 0 or n == 0 or (b == 2 and last == 0 and n == 1):
+            assert (got[t, x] == 0).all() and lse[t, x] == -np.inf
+        else:
+            assert np.isfinite(got[t, x]).all() and np.isfinite(lse[t, x])
+    at = cu[2] + m[2] - 1                                      # the last token, by numbers
+    n = int(lens[2, 0])
+    for x in range(hq):
+        keep = np.arange(n) != last
+        if not keep.any():
+            continue
+        want = S.attend_head(widen(q[at:at + 1, x]), widen(k[2, x // g, :n][keep]), widen(v[2, x // g, :n][keep]), n - 1, 1)
+        tol, tol_lse = attend_bounds(tuple(np.asarray(w) for w in want), dt, n, d)
+        assert (np.abs(got[at, x] - want[0][0]) <= tol[0]).all() and abs(lse[at, x] - want[1][0]) <= tol_lse[0]
 
 
 @pytest.mark.parametrize("dt,hq,hkv,d,m", [("bf16", 64, 64, 128, 1), ("bf16", 128, 64, 64, 2), ("bf16", 64, 64, 256, 1), ("bf16", 8, 4, 128, 60),
