@@ -310,7 +310,7 @@ ea_status ea_compress_layer_fp8(const ea_params* p, const void* q_win, int64_t w
  * and going back restores list and count.  len_out, free_out, cu_tokens, slots and pos must not
  * overlap the inputs: a loop keeps two of each and swaps them.  One launch, no scratch.
  * EA_ERR_UNSUPPORTED beyond EA_BLOCK_TABLES_MAX_BATCH sequences, for block sizes that are not a power of
- * two in [16, 65536], and for more than 2^31 - 1 blocks.  p: batch only is used (the rest has to make sense, too). */
+ * two in [16, 65536], and for more than 2^31 - 1 blocks or table entries.  p: batch only is used (the rest has to make sense, too). */
 #define EA_BLOCK_TABLES_MAX_BATCH 4096
 ea_status ea_block_tables(const ea_params* p, const ea_paged* pg, const int32_t* len_old, const int32_t* len_new,
                           int32_t* free_list, const int32_t* free_in, int32_t* len_out, int32_t* free_out,

@@ -111,6 +111,8 @@ ea_status ea_block_tables(const ea_params* p, const ea_paged* pg, const int32_t*
   PageMap pm;
   if ((s = check_paged(d, pg, 1, &pm)) != EA_OK) return s;
   if (d.B > EA_BLOCK_TABLES_MAX_BATCH || pg->num_blocks > 0x7fffffff) return EA_ERR_UNSUPPORTED;
+  // (blocks are counted in 32 bits, those given back too, of which lengths that make no sense may claim a whole table)
+  if ((int64_t)d.B * pg->max_blocks > 0x7fffffff) return EA_ERR_UNSUPPORTED;
   if (n_tokens < 0 || n_tokens > 0x7fffffff) return EA_ERR_INVALID_ARG;
   const void* ints[] = {len_old, len_new, free_list, free_in, len_out, free_out, cu_tokens};
   for (const void* x : ints)

@@ -173,3 +173,12 @@ def test_new_rows_that_are_not_there():
     assert ea.make_new_rows(None, one.expand(1, 2, 64), one).k_stride == 0
     thin = torch.zeros(1, 6, 64, **bf).transpose(0, 1)
     assert thin.stride(1) != 64 and ea.make_new_rows(None, thin, thin).k_stride == 64
+
+
+def test_block_tables_of_more_entries_than_32_bits_count(lib):
+    def call(batch, max_blocks):
+        pg = EaPaged(1 << 50, 16, max_blocks, 100)
+        # free_out lies over free_in: what passes the limit is turned away by the next check
+        return lib.ea_block_tables(byref(bf16(batch=batch)), byref(pg), at(0), at(1), at(2), at(3), at(4), at(3), at(6), 0, None, None, None, None)
+    assert call(4096, 1 << 19) == 2 and call(2, 1 << 30) == 2 and call(3, 0x7fffffff) == 2
+    assert call(4096, (1 << 19) - 1) == 1 and call(1, 0x7fffffff) == 1
