@@ -225,7 +225,7 @@ __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
   if (a.inv_freq) {
     for (int c = tid; c < D / 2; c += 256) {
 #pragma clang fp contract(off)
-      // The angle is the fp64 product.  Its whole half turns go out in fp64, with what the product with 1 / pi rounded away and what fp64
+      // The angle is the fp64 product.  Its whole turns, in halves, go out in fp64, with what the product with 1 / pi rounded away and what fp64
       // leaves of that number: without, an angle near 2^31 is off by 2^-24 of a turn.  What is left goes in as an fp32 number and its
       // remainder, by which sine and cosine turn on, so that they are off by those functions' own error at any position.
       const double angle = (double)a.pos[token] * a.inv_freq[c], inv_pi = 0.31830988618379067154, inv_pi_lo = -1.9678676675182485e-17;
