@@ -392,6 +392,95 @@ ea_status ea_attend_fp8(const ea_params* p, const void* q, const ea_step* step, 
                         const float* k_scale, const float* v_scale, const int32_t* lengths, int64_t n, int64_t n_cap,
                         void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- Pools of quantised rows (MX): pools as in ea_paged whose elements have 8 or 4 bits, and where every 32 channels of a row
+ * share a power of two that is made from the row itself when it is stored; no scale has to be known in advance.
+ *   k, v              [num_blocks, Hkv, block_size, d] elements: e4m3 bytes (EA_MXFP8), or e2m1 (EA_MXFP4), two to a byte, the even
+ *                     channel in its low half
+ *   k_scale, v_scale  [num_blocks, Hkv, block_size, d / 32] bytes e; channel c of a row is element * 2^(e - 127) (exact in bf16 from 2^-126 on), and
+ *                     NaN where e is 255.
+ * All are DEVICE pointers, 16-byte aligned, and apart from each other.  p->dtype is the type of the model's own rows and must be EA_BF16; head_dim 64, 128 or 256. */
+typedef enum { EA_MXFP8 = 0, EA_MXFP4 = 1 } ea_mx_format;
+typedef struct {
+  void* k;
+  void* v;
+  uint8_t* k_scale;
+  uint8_t* v_scale;
+  int32_t format; /* ea_mx_format */
+} ea_mx;
+
+/* ea_append_paged into MX pools.  Keys are rotated in fp64 (angles as everywhere), rounded to fp32 as queries are, and quantised:
+ * the 32 channels of a group get the least e from 10 on with max|x| <= 448 * 2^(e - 127) (e2m1: 6), elements are rounded to
+ * nearest even.  Elements that would read back as more than bf16's largest number are the largest that does not.  A group that has a NaN or an
+ * infinity (a rotated channel of 2^128 or more, too) gets e = 255.  Quantising what was read back gives the same values again. */
+ea_status ea_append_mx(const ea_params* p, const ea_new_rows* rows, const int64_t* slots, const ea_mx* mx, const ea_paged* pg,
+                       void* q_out, void* stream);
+
+/* Reads back: rows j < lengths[b] (at most n, HOST) of every sequence as bf16 into row j of k_out and v_out [B, Hkv, n_cap, d],
+ * exactly (numbers below 2^-126, which ea_append_mx does not write, may be rounded or become zeros); rows from there on are left as they were.  k_out or v_out may be NULL.  What a compress pass scores, for instance.
+ * n <= n_cap. */
+ea_status ea_read_mx(const ea_params* p, const ea_mx* mx, const ea_paged* pg, const int32_t* lengths, int64_t n, int64_t n_cap,
+                     void* k_out, void* v_out, void* stream);
+
+/* ea_attend_paged over MX pools: its arithmetic on the values that the elements stand for.  Workspace: ea_attend_workspace_bytes(). */
+ea_status ea_attend_mx(const ea_params* p, const void* q, const ea_step* step, const ea_mx* mx, const ea_paged* pg,
+                       const int32_t* lengths, int64_t n, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Drafted trees.  A step's tokens of a sequence may form a tree instead of a chain: several continuations that the model looks at
+ * in one step, of which the branch that it confirms is kept.  They stand parents in front of their children, and stand in the
+ * cache in that order. */
+#define EA_TREE_MAX 256 /* most tokens that a sequence adds */
+typedef struct {
+  uint64_t* sees; /* DEVICE [n_tokens, words], 8-byte aligned: bit j % 64 of word j / 64: the token sees the j-th of its sequence's tokens */
+  int32_t words;  /* 64 * words >= max_new, words <= EA_TREE_MAX / 64                                                          */
+} ea_tree;
+
+/* Masks and positions from parents.  parents [n_tokens] int32: of a token the number of its parent among its sequence's tokens; none
+ * if it is negative or not in front of the token itself.  Written: tree->sees, the token itself, its parent, that one's, ...; pos
+ * (nullable) [n_tokens] int32 = seen[b] (NULL: 0) + the number of tokens above it, for ea_append_paged.  Rows behind the last
+ * token are left as they were, and so are those of a sequence's tokens from the 64 * words-th on. */
+ea_status ea_tree_masks(const ea_params* p, const ea_step* step, const int32_t* parents, const ea_tree* tree, const int32_t* seen,
+                        int32_t* pos, void* stream);
+
+/* Attention of such a step: with m tokens of sequence b in the step, token i sees the rows j < len - m of its KV head, and row
+ * len - m + j where bit j of its mask is set.  Else ea_attend (bf16 or fp32), ea_attend_paged and ea_attend_mx: empty rows, values
+ * that are not finite in rows that a token does not see, workspaces and bounds.  Masks need not come from a tree. */
+ea_status ea_attend_tree(const ea_params* p, const void* q, const ea_step* step, const ea_tree* tree, const void* k, const void* v,
+                         const int32_t* lengths, int64_t n, int64_t n_cap, void* out, float* lse, void* ws, size_t ws_bytes,
+                         void* stream);
+ea_status ea_attend_tree_paged(const ea_params* p, const void* q, const ea_step* step, const ea_tree* tree, const void* k_pool,
+                               const void* v_pool, const ea_paged* pg, const int32_t* lengths, int64_t n, void* out, float* lse,
+                               void* ws, size_t ws_bytes, void* stream);
+ea_status ea_attend_tree_mx(const ea_params* p, const void* q, const ea_step* step, const ea_tree* tree, const ea_mx* mx,
+                            const ea_paged* pg, const int32_t* lengths, int64_t n, void* out, float* lse, void* ws, size_t ws_bytes,
+                            void* stream);
+
+/* The branch that the model confirms.  tokens [n_tokens] int32: what was drafted; target [n_tokens]: what the model answers behind
+ * each of them.  A sequence's first token is accepted (it was the last answer); then, again and again, the first of the children
+ * of the last accepted one that is what the model answers there.
+ *   path [B, max_new] int32: numbers of the accepted tokens, ascending, -1 behind them is NOT written: entries stay as they were
+ *   n_path [B] int32: how many; 0 where the sequence adds no token
+ *   next [B] int32: the model's answer behind the last one; -1 where there is none
+ * Tokens from the EA_TREE_MAX-th or max_new-th on are not looked at. */
+ea_status ea_tree_accept(const ea_params* p, const ea_step* step, const int32_t* tokens, const int32_t* parents, const int32_t* target,
+                         int32_t* path, int32_t* n_path, int32_t* next, void* stream);
+
+/* The branch's rows become the sequence's next ones, in place: with m tokens of sequence b in the step, row len - m + path[b, j]
+ * of every KV head moves to row len - m + j for j < n_path[b]; len_out = len - m + n_path.  len = lengths[b] counts the step's rows in
+ * (per head lengths[b, h] and len_out[b, h] for ea_keep_path).  path and n_path as ea_tree_accept writes them: a path counts as ended in
+ * front of the first number that is not larger than the one before it, or not one of the sequence's tokens.  Rows from len_out on are
+ * not needed any more; ea_block_tables takes their blocks back.
+ *   slots (nullable; of ea_block_tables): where the slot of a sequence's first token is -1 it was not served, has no such rows, and
+ *   keeps what it has: len_out = len.
+ * ea_keep_path: contiguous caches of any dtype (EA_FP8_E4M3: rows of d bytes); ea_keep_path_paged: bf16 pools.
+ * step: cu_tokens, n_tokens and max_new; len_out must not overlap lengths. */
+ea_status ea_keep_path(const ea_params* p, const ea_step* step, const int32_t* path, const int32_t* n_path, void* k, void* v,
+                       const int32_t* lengths, int64_t n_cap, int32_t* len_out, void* stream);
+ea_status ea_keep_path_paged(const ea_params* p, const ea_step* step, const int32_t* path, const int32_t* n_path, void* k_pool,
+                             void* v_pool, const ea_paged* pg, const int64_t* slots, const int32_t* lengths, int32_t* len_out,
+                             void* stream);
+ea_status ea_keep_path_mx(const ea_params* p, const ea_step* step, const int32_t* path, const int32_t* n_path, const ea_mx* mx,
+                          const ea_paged* pg, const int64_t* slots, const int32_t* lengths, int32_t* len_out, void* stream);
+
 /* Listing 1: int(n * (1 - ratio)) in IEEE double, truncated toward zero; -1 if ratio is
  * outside [0, 1] or n < 0.  Host only. */
 int64_t ea_n_keep(int64_t n, double ratio);

@@ -40,6 +40,18 @@ class EaStep(ctypes.Structure):
                 ("q_stride", ctypes.c_int64)]
 
 
+EA_MXFP8, EA_MXFP4 = 0, 1
+
+
+class EaMx(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("format", ctypes.c_int32)]
+
+
+class EaTree(ctypes.Structure):
+    _fields_ = [("sees", ctypes.c_void_p), ("words", ctypes.c_int32)]
+
+
 def lib_path():
     """In-tree libea.so; the environment variable EA_LIBRARY names another build of it."""
     return os.environ.get("EA_LIBRARY") or os.path.join(_HERE, "libea.so")
@@ -122,6 +134,18 @@ def load_library():
     lib.ea_attend_paged.argtypes = [P, VP, ST, VP, VP, PG, VP, I64, VP, VP, VP, SZ, VP]
     lib.ea_attend_fp8.restype = ctypes.c_int
     lib.ea_attend_fp8.argtypes = [P, VP, ST, VP, VP, VP, VP, VP, I64, I64, VP, VP, VP, SZ, VP]
+    MX, TR = ctypes.POINTER(EaMx), ctypes.POINTER(EaTree)
+    for name, args in (("append_mx", [P, NR, VP, MX, PG, VP, VP]), ("read_mx", [P, MX, PG, VP, I64, I64, VP, VP, VP]),
+                       ("attend_mx", [P, VP, ST, MX, PG, VP, I64, VP, VP, VP, SZ, VP]),
+                       ("tree_masks", [P, ST, VP, TR, VP, VP, VP]), ("tree_accept", [P, ST, VP, VP, VP, VP, VP, VP, VP]),
+                       ("attend_tree", [P, VP, ST, TR, VP, VP, VP, I64, I64, VP, VP, VP, SZ, VP]),
+                       ("attend_tree_paged", [P, VP, ST, TR, VP, VP, PG, VP, I64, VP, VP, VP, SZ, VP]),
+                       ("attend_tree_mx", [P, VP, ST, TR, MX, PG, VP, I64, VP, VP, VP, SZ, VP]),
+                       ("keep_path", [P, ST, VP, VP, VP, VP, VP, I64, VP, VP]),
+                       ("keep_path_paged", [P, ST, VP, VP, VP, VP, PG, VP, VP, VP, VP]),
+                       ("keep_path_mx", [P, ST, VP, VP, MX, PG, VP, VP, VP, VP])):
+        f = getattr(lib, "ea_" + name)
+        f.restype, f.argtypes = ctypes.c_int, args
     lib.ea_compress_layer_timed.restype = ctypes.c_int
     lib.ea_compress_layer_timed.argtypes = [P, VP, I64, I64, VP, I64, VP, VP, I64, I64, I64, VP, SZ, VP,
                                             ctypes.POINTER(ctypes.c_float)]
@@ -429,6 +453,82 @@ def attend_fp8(p, q, step, k8, v8, k_scale, v_scale, lengths, n, n_cap, out, lse
     _check(load_library().ea_attend_fp8(p, _addr(q), step, _addr(k8), _addr(v8), _addr(k_scale),
                                         _addr(v_scale), _addr(lengths), int(n), int(n_cap), _addr(out), _addr(lse), _addr(ws),
                                         _nbytes(ws), _now(stream)), "ea_attend_fp8")
+
+
+def make_mx(k, v, k_scale, v_scale, fmt):
+    """ea_mx for pools [num_blocks, Hkv, block_size, d (EA_MXFP4: d / 2)] of bytes and their scales [num_blocks, Hkv, block_size, d / 32]."""
+    for x, s in ((k, k_scale), (v, v_scale)):
+        if x.element_size() != 1 or s.element_size() != 1 or not x.is_contiguous() or not s.is_contiguous():
+            raise ValueError("elements and scales are contiguous tensors of bytes")
+        if x.shape[:-1] != s.shape[:-1] or x.shape[-1] * (2 if fmt == EA_MXFP4 else 1) != s.shape[-1] * 32:
+            raise ValueError("a row has one scale for 32 channels")
+    if k.shape != v.shape:
+        raise ValueError("k and v must have the same shape")
+    m = EaMx(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), int(fmt))
+    m.tensors = (k, v, k_scale, v_scale)
+    return m
+
+
+def append_mx(p, rows, slots, mx, pg, q_out=None, stream=None):
+    _check(load_library().ea_append_mx(p, rows, _addr(slots), mx, pg, _addr(q_out), _now(stream)), "ea_append_mx")
+
+
+def read_mx(p, mx, pg, lengths, n, n_cap, k_out, v_out, stream=None):
+    _check(load_library().ea_read_mx(p, mx, pg, _addr(lengths), int(n), int(n_cap), _addr(k_out), _addr(v_out), _now(stream)), "ea_read_mx")
+
+
+def attend_mx(p, q, step, mx, pg, lengths, n, out, lse, ws, stream=None):
+    _check(load_library().ea_attend_mx(p, _addr(q), step, mx, pg, _addr(lengths), int(n), _addr(out), _addr(lse), _addr(ws),
+                                       _nbytes(ws), _now(stream)), "ea_attend_mx")
+
+
+def make_tree(sees):
+    """ea_tree for a tensor of masks [n_tokens, words] int64 on the device."""
+    if sees.dim() != 2 or sees.element_size() != 8 or not sees.is_contiguous():
+        raise ValueError("masks are [tokens, words] of 64 bits, contiguous")
+    t = EaTree(sees.data_ptr(), int(sees.shape[1]))
+    t.tensors = (sees,)
+    return t
+
+
+def tree_masks(p, step, parents, tree, pos=None, seen=None, stream=None):
+    """Writes the masks that tree points at, too."""
+    _check(load_library().ea_tree_masks(p, step, _addr(parents), tree, _addr(seen), _addr(pos), _now(stream)), "ea_tree_masks")
+
+
+def tree_accept(p, step, tokens, parents, target, path, n_path, next_token, stream=None):
+    _check(load_library().ea_tree_accept(p, step, _addr(tokens), _addr(parents), _addr(target), _addr(path), _addr(n_path),
+                                         _addr(next_token), _now(stream)), "ea_tree_accept")
+
+
+def attend_tree(p, q, step, tree, k, v, lengths, n, n_cap, out, lse, ws, stream=None):
+    _check(load_library().ea_attend_tree(p, _addr(q), step, tree, _addr(k), _addr(v), _addr(lengths), int(n), int(n_cap), _addr(out),
+                                         _addr(lse), _addr(ws), _nbytes(ws), _now(stream)), "ea_attend_tree")
+
+
+def attend_tree_paged(p, q, step, tree, k_pool, v_pool, pg, lengths, n, out, lse, ws, stream=None):
+    _check(load_library().ea_attend_tree_paged(p, _addr(q), step, tree, _addr(k_pool), _addr(v_pool), pg, _addr(lengths), int(n),
+                                               _addr(out), _addr(lse), _addr(ws), _nbytes(ws), _now(stream)), "ea_attend_tree_paged")
+
+
+def attend_tree_mx(p, q, step, tree, mx, pg, lengths, n, out, lse, ws, stream=None):
+    _check(load_library().ea_attend_tree_mx(p, _addr(q), step, tree, mx, pg, _addr(lengths), int(n), _addr(out), _addr(lse),
+                                            _addr(ws), _nbytes(ws), _now(stream)), "ea_attend_tree_mx")
+
+
+def keep_path(p, step, path, n_path, k, v, lengths, n_cap, len_out, stream=None):
+    _check(load_library().ea_keep_path(p, step, _addr(path), _addr(n_path), _addr(k), _addr(v), _addr(lengths), int(n_cap),
+                                       _addr(len_out), _now(stream)), "ea_keep_path")
+
+
+def keep_path_paged(p, step, path, n_path, k_pool, v_pool, pg, lengths, len_out, slots=None, stream=None):
+    _check(load_library().ea_keep_path_paged(p, step, _addr(path), _addr(n_path), _addr(k_pool), _addr(v_pool), pg, _addr(slots),
+                                             _addr(lengths), _addr(len_out), _now(stream)), "ea_keep_path_paged")
+
+
+def keep_path_mx(p, step, path, n_path, mx, pg, lengths, len_out, slots=None, stream=None):
+    _check(load_library().ea_keep_path_mx(p, step, _addr(path), _addr(n_path), mx, pg, _addr(slots), _addr(lengths), _addr(len_out),
+                                          _now(stream)), "ea_keep_path_mx")
 
 
 N_STAGES = 6

@@ -29,6 +29,11 @@ struct AttendArgs {
   int only_long;                  // the tile kernel leaves sequences of up to short_rows (token, head) rows to the row kernel
   int short_rows;
   float scale;                    // log2(e) / sqrt(d): weights are powers of two
+  const uint8_t *kscale8, *vscale8;       // MX pools: a byte for 32 channels of a row
+  int mx;                         // bits of an element of such pools, 0: others
+  const uint64_t* sees;           // trees: which of its sequence's new rows a token sees, `words` words each; null: those up to its own
+  int words;
+  int f32;                        // rows are fp32
   AttendPlan plan;
 };
 
@@ -242,6 +247,7 @@ __device__ __forceinline__ float natural_lse(float m, float l) {
 }
 
 hipError_t launch_attend(const AttendArgs& a, const Dims& d, hipStream_t st);
+hipError_t launch_attend_wave(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_rows(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_tile(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_f32(const AttendArgs& a, hipStream_t st);

@@ -1,7 +1,9 @@
 // extern "C" entry points of a model's step over its cache: host-side validation, then the launches on the caller's stream.
 // No allocation, no synchronisation, no state.
 #include "ea_attend.h"
+#include "ea_mx.h"
 #include "ea_step.h"
+#include "ea_tree.h"
 
 namespace ea {
 
@@ -13,14 +15,41 @@ static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 constexpr int kPlanCus = 256;      // a plan, and with it the size of its workspace, is the same wherever it is made
 
 hipError_t launch_attend(const AttendArgs& a, const Dims& d, hipStream_t st) {
+  if (a.mx || a.sees) return launch_attend_wave(a, d, st);
   hipError_t e = hipSuccess;
   if (a.plan.rows) e = launch_attend_rows(a, d, st);
   if (e != hipSuccess || !a.plan.tile) return e;
   return d.dtype == EA_BF16 ? launch_attend_tile(a, d, st) : launch_attend_f32(a, st);
 }
 
-static ea_status attend(const Dims& d, const void* q, const ea_step* step, const void* k, const void* v, const PageMap* pm,
-                        const float* kscale, const float* vscale, const int32_t* lengths, bool per_head, int64_t n,
+// MX pools: four tensors of their own
+static ea_status check_mx(const Dims& d, const ea_mx* mx, const PageMap& pm, size_t* bytes, size_t* scales) {
+  if (!mx || !aligned(mx->k, 16) || !aligned(mx->v, 16) || !aligned(mx->k_scale, 16) || !aligned(mx->v_scale, 16)) return EA_ERR_INVALID_ARG;
+  if (mx->format != EA_MXFP8 && mx->format != EA_MXFP4) return EA_ERR_UNSUPPORTED;
+  const size_t rows = ((size_t)pm.num_blocks << pm.sh) * d.Hkv;
+  *bytes = rows * (mx->format == EA_MXFP8 ? d.D : d.D / 2);
+  *scales = rows * (d.D / 32);
+  const struct { const void* at; size_t bytes; } part[4] = {{mx->k, *bytes}, {mx->v, *bytes}, {mx->k_scale, *scales}, {mx->v_scale, *scales}};
+  for (int i = 0; i < 4; ++i)
+    for (int j = i + 1; j < 4; ++j)
+      if (overlap(part[i].at, part[i].bytes, part[j].at, part[j].bytes)) return EA_ERR_INVALID_ARG;
+  return EA_OK;
+}
+static bool over_mx(const void* at, size_t n, const ea_mx* mx, size_t bytes, size_t scales) {
+  return overlap(at, n, mx->k, bytes) || overlap(at, n, mx->v, bytes) || overlap(at, n, mx->k_scale, scales) || overlap(at, n, mx->v_scale, scales);
+}
+
+static ea_status check_tree(const ea_step* step, const ea_tree* tree) {
+  if (!step || !tree) return EA_ERR_INVALID_ARG;
+  if (tree->words < 1 || step->max_new > (int64_t)64 * tree->words) return EA_ERR_INVALID_ARG;
+  if (tree->words > EA_TREE_MAX / 64) return EA_ERR_UNSUPPORTED;
+  if (step->n_tokens > 0 && !aligned(tree->sees, 8)) return EA_ERR_INVALID_ARG;
+  return EA_OK;
+}
+
+// mx: k and v are its elements.  tree: null, or which new rows a token sees
+static ea_status attend(const Dims& d, const void* q, const ea_step* step, const ea_tree* tree, const void* k, const void* v, const PageMap* pm,
+                        const float* kscale, const float* vscale, const ea_mx* mx, const int32_t* lengths, bool per_head, int64_t n,
                         int64_t n_cap, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
   ea_status s = check_step(d, step, n);
   if (s != EA_OK) return s;
@@ -32,8 +61,15 @@ static ea_status attend(const Dims& d, const void* q, const ea_step* step, const
   a.q_stride = step->q_stride ? step->q_stride : (long long)d.Hq * d.D;
   const size_t rows = (size_t)step->n_tokens, out_bytes = rows * d.Hq * d.D * es;
   if (overlap(out, out_bytes, q, rows ? ((rows - 1) * a.q_stride + (size_t)d.Hq * d.D) * es : 0)) return EA_ERR_INVALID_ARG;
-  const size_t cache = (pm ? ((size_t)pm->num_blocks << pm->sh) * d.Hkv : (size_t)d.units() * n_cap) * d.D * d.esize();
-  if (overlap(out, out_bytes, k, cache) || overlap(out, out_bytes, v, cache)) return EA_ERR_INVALID_ARG;
+  if (mx) {
+    size_t bytes, scales;
+    if ((s = check_mx(d, mx, *pm, &bytes, &scales)) != EA_OK) return s;
+    if (over_mx(out, out_bytes, mx, bytes, scales)) return EA_ERR_INVALID_ARG;
+  } else {
+    const size_t cache = (pm ? ((size_t)pm->num_blocks << pm->sh) * d.Hkv : (size_t)d.units() * n_cap) * d.D * d.esize();
+    if (overlap(out, out_bytes, k, cache) || overlap(out, out_bytes, v, cache)) return EA_ERR_INVALID_ARG;
+  }
+  if (tree && overlap(out, out_bytes, tree->sees, rows * tree->words * 8)) return EA_ERR_INVALID_ARG;
   a.plan = make_attend_plan(d, n, step->n_tokens, step->max_new, kPlanCus);
   // Workgroups of up to 512 threads, 2^32 threads to a launch.  (The launches of few rows are no larger than 512 shares, their
   // joining one than 512 times 64 rows; the stretches' joining one comes with few tiles only.)
@@ -48,41 +84,88 @@ static ea_status attend(const Dims& d, const void* q, const ea_step* step, const
   a.n_cap = n_cap;
   a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.G; a.D = d.D;
   a.n = (int)n; a.n_tokens = (int)step->n_tokens; a.per_head = per_head;
+  a.f32 = d.dtype == EA_F32;
+  if (mx) {
+    a.mx = mx->format == EA_MXFP8 ? 8 : 4;
+    a.kscale8 = mx->k_scale;
+    a.vscale8 = mx->v_scale;
+  }
+  if (tree) {
+    a.sees = tree->sees;
+    a.words = tree->words;
+  }
   a.only_long = a.plan.rows;
   a.short_rows = a.plan.short_rows;
   a.scale = (float)(1.4426950408889634074 / (d.D == 64 ? 8.0 : d.D == 256 ? 16.0 : 11.313708498984760390));
   return launch_attend(a, d, (hipStream_t)stream) == hipSuccess ? EA_OK : EA_ERR_DEVICE;
 }
 
-static ea_status append(const Dims& d, const ea_new_rows* r, AppendArgs a, size_t cache, void* q_out, void* stream) {
+// what a call reads of the new rows and writes of the queries: q, k, v, q_out
+struct NewBytes { const void* at[4]; size_t bytes[4]; };
+static NewBytes bytes_of_rows(const Dims& d, const ea_new_rows* r, const AppendArgs& a) {
+  const size_t es = d.dtype == EA_BF16 ? 2 : 4, n = (size_t)r->n_tokens, qd = (size_t)d.Hq * d.D, kd = (size_t)d.Hkv * d.D;
+  return {{r->q, r->k, r->v, a.q_out},
+          {r->q ? ((n - 1) * a.q_stride + qd) * es : 0, ((n - 1) * a.k_stride + kd) * es, ((n - 1) * a.v_stride + kd) * es, r->q ? n * qd * es : 0}};
+}
+// the new rows by themselves; strides and q_out into a.  nothing: there are none
+static ea_status check_rows(const Dims& d, const ea_new_rows* r, void* q_out, AppendArgs* a, bool* nothing) {
   if (!r || r->n_tokens < 0) return EA_ERR_INVALID_ARG;
   if (r->n_tokens > kAttendMaxTokens) return EA_ERR_UNSUPPORTED;
   const int64_t qd = (int64_t)d.Hq * d.D, kd = (int64_t)d.Hkv * d.D, per16 = d.dtype == EA_BF16 ? 8 : 4;
-  const size_t es = d.dtype == EA_BF16 ? 2 : 4, n = (size_t)r->n_tokens;
-  a.q_stride = r->q_stride ? r->q_stride : qd;
-  a.k_stride = r->k_stride ? r->k_stride : kd;
-  a.v_stride = r->v_stride ? r->v_stride : kd;
+  a->q_stride = r->q_stride ? r->q_stride : qd;
+  a->k_stride = r->k_stride ? r->k_stride : kd;
+  a->v_stride = r->v_stride ? r->v_stride : kd;
+  a->q_out = q_out;
   const int64_t far = (int64_t)1 << 40;
-  if (a.q_stride < qd || a.k_stride < kd || a.v_stride < kd || a.q_stride > far || a.k_stride > far || a.v_stride > far) return EA_ERR_INVALID_ARG;
-  if (a.q_stride % per16 || a.k_stride % per16 || a.v_stride % per16) return EA_ERR_INVALID_ARG;
-  if (!aligned(a.k_cache, 16) || !aligned(a.v_cache, 16) || a.k_cache == a.v_cache) return EA_ERR_INVALID_ARG;
-  if (overlap(a.k_cache, cache, a.v_cache, cache)) return EA_ERR_INVALID_ARG;
+  if (a->q_stride < qd || a->k_stride < kd || a->v_stride < kd || a->q_stride > far || a->k_stride > far || a->v_stride > far) return EA_ERR_INVALID_ARG;
+  if (a->q_stride % per16 || a->k_stride % per16 || a->v_stride % per16) return EA_ERR_INVALID_ARG;
   if (r->q && !r->inv_freq) return EA_ERR_INVALID_ARG;
-  if (n == 0) return EA_OK;
+  *nothing = r->n_tokens == 0;
+  if (*nothing) return EA_OK;
   if (!aligned(r->k, 16) || !aligned(r->v, 16) || (r->q && (!aligned(r->q, 16) || !aligned(q_out, 16)))) return EA_ERR_INVALID_ARG;
   if (r->inv_freq && (!aligned(r->inv_freq, 8) || !aligned(r->pos, 4))) return EA_ERR_INVALID_ARG;
-  const void* in[3] = {r->q, r->k, r->v};
-  const size_t bytes[3] = {r->q ? ((n - 1) * a.q_stride + qd) * es : 0, ((n - 1) * a.k_stride + kd) * es, ((n - 1) * a.v_stride + kd) * es};
-  const size_t q_bytes = r->q ? n * qd * es : 0;
+  const NewBytes b = bytes_of_rows(d, r, *a);
   for (int i = 0; i < 3; ++i) {
-    if (overlap(in[i], bytes[i], a.k_cache, cache) || overlap(in[i], bytes[i], a.v_cache, cache)) return EA_ERR_INVALID_ARG;
-    const bool itself = i == 0 && q_out == r->q && a.q_stride == qd;
-    if (!itself && overlap(in[i], bytes[i], q_out, q_bytes)) return EA_ERR_INVALID_ARG;
+    const bool itself = i == 0 && q_out == r->q && a->q_stride == qd;
+    if (!itself && overlap(b.at[i], b.bytes[i], q_out, b.bytes[3])) return EA_ERR_INVALID_ARG;
   }
-  if (overlap(q_out, q_bytes, a.k_cache, cache) || overlap(q_out, q_bytes, a.v_cache, cache)) return EA_ERR_INVALID_ARG;
-  a.q = r->q; a.k = r->k; a.v = r->v; a.q_out = q_out; a.pos = r->pos; a.inv_freq = r->inv_freq;
-  a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.n_tokens = (int)n; a.rope_layout = d.rope_layout;
+  return EA_OK;
+}
+
+static ea_status append(const Dims& d, const ea_new_rows* r, AppendArgs a, size_t cache, void* q_out, void* stream) {
+  bool nothing;
+  const ea_status s = check_rows(d, r, q_out, &a, &nothing);
+  if (s != EA_OK) return s;
+  if (!aligned(a.k_cache, 16) || !aligned(a.v_cache, 16) || a.k_cache == a.v_cache) return EA_ERR_INVALID_ARG;
+  if (overlap(a.k_cache, cache, a.v_cache, cache)) return EA_ERR_INVALID_ARG;
+  if (nothing) return EA_OK;
+  const NewBytes b = bytes_of_rows(d, r, a);
+  for (int i = 0; i < 4; ++i)
+    if (overlap(b.at[i], b.bytes[i], a.k_cache, cache) || overlap(b.at[i], b.bytes[i], a.v_cache, cache)) return EA_ERR_INVALID_ARG;
+  a.q = r->q; a.k = r->k; a.v = r->v; a.pos = r->pos; a.inv_freq = r->inv_freq;
+  a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.n_tokens = (int)r->n_tokens; a.rope_layout = d.rope_layout;
   return launch_append(a, d, (hipStream_t)stream) == hipSuccess ? EA_OK : EA_ERR_DEVICE;
+}
+
+// new rows into MX pools: the checks of append(), against four tensors
+static ea_status append_mx(const Dims& d, const ea_new_rows* r, const int64_t* slots, const ea_mx* mx, const PageMap& pm, void* q_out, void* stream) {
+  size_t bytes, scales;
+  ea_status s = check_mx(d, mx, pm, &bytes, &scales);
+  if (s != EA_OK) return s;
+  MxAppendArgs a = {};
+  AppendArgs rows = {};
+  bool nothing;
+  if ((s = check_rows(d, r, q_out, &rows, &nothing)) != EA_OK || nothing) return s;
+  if (!aligned(slots, 8)) return EA_ERR_INVALID_ARG;
+  const NewBytes in = bytes_of_rows(d, r, rows);
+  for (int i = 0; i < 4; ++i)
+    if (over_mx(in.at[i], in.bytes[i], mx, bytes, scales)) return EA_ERR_INVALID_ARG;
+  a.q = r->q; a.k = r->k; a.v = r->v; a.q_out = q_out; a.pos = r->pos; a.inv_freq = r->inv_freq; a.slots = slots;
+  a.k_pool = mx->k; a.v_pool = mx->v; a.k_scale = mx->k_scale; a.v_scale = mx->v_scale;
+  a.q_stride = rows.q_stride; a.k_stride = rows.k_stride; a.v_stride = rows.v_stride; a.num_blocks = pm.num_blocks;
+  a.Hq = d.Hq; a.Hkv = d.Hkv; a.n_tokens = (int)r->n_tokens; a.sh = pm.sh; a.rope_layout = d.rope_layout;
+  a.bits = mx->format == EA_MXFP8 ? 8 : 4;
+  return launch_append_mx(a, d, (hipStream_t)stream) == hipSuccess ? EA_OK : EA_ERR_DEVICE;
 }
 
 static ea_status append_heads(const Dims& d, const ea_new_rows* rows, const int32_t* cu_tokens, const int32_t* lengths, void* k, void* v,
@@ -92,6 +175,27 @@ static ea_status append_heads(const Dims& d, const ea_new_rows* rows, const int3
   AppendArgs a = {};
   a.k_cache = k; a.v_cache = v; a.cu = cu_tokens; a.lens = lengths; a.n_cap = n_cap; a.k_scale = k_scale; a.v_scale = v_scale;
   return append(d, rows, a, (size_t)d.units() * n_cap * d.D * d.esize(), q_out, stream);
+}
+
+// what a path's rows are moved in, and the step they are of
+static ea_status keep_path(const Dims& d, const ea_step* step, const int32_t* path, const int32_t* n_path, KeepArgs a, const size_t* bytes,
+                           const int32_t* lengths, int32_t* len_out, bool per_head, void* stream) {
+  const ea_status s = check_step(d, step, 0);
+  if (s != EA_OK) return s;
+  if (step->max_new > EA_TREE_MAX) return EA_ERR_UNSUPPORTED;
+  if (!aligned(path, 4) || !aligned(n_path, 4) || !aligned(lengths, 4) || !aligned(len_out, 4)) return EA_ERR_INVALID_ARG;
+  const size_t lens = (size_t)(per_head ? d.units() : d.B) * 4, b4 = (size_t)d.B * 4;
+  const struct { const void* at; size_t bytes; } in[] = {{lengths, lens}, {n_path, b4}, {path, b4 * step->max_new}, {step->cu_tokens, b4 + 4}};
+  for (const auto& x : in) {
+    if (overlap(len_out, lens, x.at, x.bytes)) return EA_ERR_INVALID_ARG;
+    for (int i = 0; i < a.count; ++i)
+      if (overlap(a.at[i], bytes[i], x.at, x.bytes)) return EA_ERR_INVALID_ARG;
+  }
+  for (int i = 0; i < a.count; ++i)
+    if (overlap(a.at[i], bytes[i], len_out, lens)) return EA_ERR_INVALID_ARG;
+  a.cu = step->cu_tokens; a.path = path; a.n_path = n_path; a.lens = lengths; a.len_out = len_out;
+  a.B = d.B; a.Hkv = d.Hkv; a.n_tokens = (int)step->n_tokens; a.max_new = (int)step->max_new; a.per_head = per_head;
+  return launch_keep_path(a, (hipStream_t)stream) == hipSuccess ? EA_OK : EA_ERR_DEVICE;
 }
 
 }  // namespace ea
@@ -182,7 +286,7 @@ ea_status ea_attend(const ea_params* p, const void* q, const ea_step* step, cons
   const ea_status s = check_params(p, &d);
   if (s != EA_OK) return s;
   if (n > n_cap || n_cap < 1 || n_cap > ((int64_t)1 << 40)) return EA_ERR_INVALID_ARG;
-  return attend(d, q, step, k, v, nullptr, nullptr, nullptr, lengths, true, n, n_cap, out, lse, ws, ws_bytes, stream);
+  return attend(d, q, step, nullptr, k, v, nullptr, nullptr, nullptr, nullptr, lengths, true, n, n_cap, out, lse, ws, ws_bytes, stream);
 }
 
 ea_status ea_attend_paged(const ea_params* p, const void* q, const ea_step* step, const void* k_pool, const void* v_pool,
@@ -193,7 +297,7 @@ ea_status ea_attend_paged(const ea_params* p, const void* q, const ea_step* step
   if (s != EA_OK) return s;
   PageMap pm;
   if ((s = check_paged(d, pg, n, &pm)) != EA_OK) return s;
-  return attend(d, q, step, k_pool, v_pool, &pm, nullptr, nullptr, lengths, false, n, 0, out, lse, ws, ws_bytes, stream);
+  return attend(d, q, step, nullptr, k_pool, v_pool, &pm, nullptr, nullptr, nullptr, lengths, false, n, 0, out, lse, ws, ws_bytes, stream);
 }
 
 ea_status ea_attend_fp8(const ea_params* p, const void* q, const ea_step* step, const void* k8, const void* v8,
@@ -205,7 +309,173 @@ ea_status ea_attend_fp8(const ea_params* p, const void* q, const ea_step* step, 
   if (d.dtype != EA_BF16 || d.D == 64) return EA_ERR_UNSUPPORTED;
   if (n > n_cap || n_cap < 1 || n_cap > ((int64_t)1 << 40)) return EA_ERR_INVALID_ARG;
   d.kv_fp8 = 1;
-  return attend(d, q, step, k8, v8, nullptr, k_scale, v_scale, lengths, true, n, n_cap, out, lse, ws, ws_bytes, stream);
+  return attend(d, q, step, nullptr, k8, v8, nullptr, k_scale, v_scale, nullptr, lengths, true, n, n_cap, out, lse, ws, ws_bytes, stream);
+}
+
+ea_status ea_append_mx(const ea_params* p, const ea_new_rows* rows, const int64_t* slots, const ea_mx* mx, const ea_paged* pg,
+                       void* q_out, void* stream) {
+  Dims d;
+  ea_status s = check_params(p, &d);
+  if (s != EA_OK) return s;
+  PageMap pm;
+  if ((s = check_paged(d, pg, 1, &pm)) != EA_OK) return s;
+  return append_mx(d, rows, slots, mx, pm, q_out, stream);
+}
+
+ea_status ea_read_mx(const ea_params* p, const ea_mx* mx, const ea_paged* pg, const int32_t* lengths, int64_t n, int64_t n_cap,
+                     void* k_out, void* v_out, void* stream) {
+  Dims d;
+  ea_status s = check_params(p, &d);
+  if (s != EA_OK) return s;
+  PageMap pm;
+  size_t bytes, scales;
+  if (n < 0 || n > kMaxN || n > n_cap || n_cap < 1 || n_cap > ((int64_t)1 << 40)) return EA_ERR_INVALID_ARG;
+  if ((s = check_paged(d, pg, n, &pm)) != EA_OK || (s = check_mx(d, mx, pm, &bytes, &scales)) != EA_OK) return s;
+  if (!aligned(lengths, 4) || (k_out && !aligned(k_out, 16)) || (v_out && !aligned(v_out, 16))) return EA_ERR_INVALID_ARG;
+  const size_t out = (size_t)d.units() * n_cap * d.D * 2;
+  if (k_out && v_out && overlap(k_out, out, v_out, out)) return EA_ERR_INVALID_ARG;
+  if ((k_out && over_mx(k_out, out, mx, bytes, scales)) || (v_out && over_mx(v_out, out, mx, bytes, scales))) return EA_ERR_INVALID_ARG;
+  if (n == 0 || (!k_out && !v_out)) return EA_OK;
+  MxReadArgs a = {};
+  a.k = mx->k; a.v = mx->v; a.k_scale = mx->k_scale; a.v_scale = mx->v_scale; a.lens = lengths; a.k_out = k_out; a.v_out = v_out;
+  a.pm = pm; a.n_cap = n_cap; a.B = d.B; a.Hkv = d.Hkv; a.n = (int)n; a.bits = mx->format == EA_MXFP8 ? 8 : 4;
+  return launch_read_mx(a, d, (hipStream_t)stream) == hipSuccess ? EA_OK : EA_ERR_DEVICE;
+}
+
+ea_status ea_attend_mx(const ea_params* p, const void* q, const ea_step* step, const ea_mx* mx, const ea_paged* pg,
+                       const int32_t* lengths, int64_t n, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  Dims d;
+  ea_status s = check_params(p, &d);
+  if (s != EA_OK) return s;
+  PageMap pm;
+  if ((s = check_paged(d, pg, n, &pm)) != EA_OK) return s;
+  if (!mx) return EA_ERR_INVALID_ARG;
+  return attend(d, q, step, nullptr, mx->k, mx->v, &pm, nullptr, nullptr, mx, lengths, false, n, 0, out, lse, ws, ws_bytes, stream);
+}
+
+ea_status ea_tree_masks(const ea_params* p, const ea_step* step, const int32_t* parents, const ea_tree* tree, const int32_t* seen,
+                        int32_t* pos, void* stream) {
+  Dims d;
+  ea_status s = check_params(p, &d, true);
+  if (s != EA_OK || (s = check_step(d, step, 0)) != EA_OK || (s = check_tree(step, tree)) != EA_OK) return s;
+  if (seen && !aligned(seen, 4)) return EA_ERR_INVALID_ARG;
+  if (step->n_tokens == 0) return EA_OK;
+  if (!aligned(parents, 4) || (pos && !aligned(pos, 4))) return EA_ERR_INVALID_ARG;
+  const size_t t4 = (size_t)step->n_tokens * 4, b4 = (size_t)d.B * 4;
+  const struct { const void* at; size_t bytes; } out[] = {{tree->sees, (size_t)step->n_tokens * tree->words * 8}, {pos, pos ? t4 : 0}},
+      in[] = {{parents, t4}, {seen, seen ? b4 : 0}, {step->cu_tokens, b4 + 4}};
+  for (const auto& o : out)
+    for (const auto& x : in)
+      if (overlap(o.at, o.bytes, x.at, x.bytes)) return EA_ERR_INVALID_ARG;
+  if (overlap(out[0].at, out[0].bytes, out[1].at, out[1].bytes)) return EA_ERR_INVALID_ARG;
+  TreeArgs a = {};
+  a.cu = step->cu_tokens; a.parents = parents; a.seen = seen; a.sees = tree->sees; a.pos = pos;
+  a.B = d.B; a.n_tokens = (int)step->n_tokens; a.words = tree->words;
+  return launch_tree_masks(a, (hipStream_t)stream) == hipSuccess ? EA_OK : EA_ERR_DEVICE;
+}
+
+ea_status ea_tree_accept(const ea_params* p, const ea_step* step, const int32_t* tokens, const int32_t* parents, const int32_t* target,
+                         int32_t* path, int32_t* n_path, int32_t* next, void* stream) {
+  Dims d;
+  ea_status s = check_params(p, &d, true);
+  if (s != EA_OK || (s = check_step(d, step, 0)) != EA_OK) return s;
+  if (step->max_new > EA_TREE_MAX) return EA_ERR_UNSUPPORTED;
+  if (!aligned(path, 4) || !aligned(n_path, 4) || !aligned(next, 4)) return EA_ERR_INVALID_ARG;
+  if (step->n_tokens > 0 && (!aligned(tokens, 4) || !aligned(parents, 4) || !aligned(target, 4))) return EA_ERR_INVALID_ARG;
+  const size_t t4 = (size_t)step->n_tokens * 4, b4 = (size_t)d.B * 4;
+  const struct { const void* at; size_t bytes; } out[] = {{path, b4 * step->max_new}, {n_path, b4}, {next, b4}},
+      in[] = {{tokens, t4}, {parents, t4}, {target, t4}, {step->cu_tokens, b4 + 4}};
+  for (int i = 0; i < 3; ++i) {
+    for (const auto& x : in)
+      if (overlap(out[i].at, out[i].bytes, x.at, x.bytes)) return EA_ERR_INVALID_ARG;
+    for (int j = i + 1; j < 3; ++j)
+      if (overlap(out[i].at, out[i].bytes, out[j].at, out[j].bytes)) return EA_ERR_INVALID_ARG;
+  }
+  TreeArgs a = {};
+  a.cu = step->cu_tokens; a.parents = parents; a.tokens = tokens; a.target = target; a.path = path; a.n_path = n_path; a.next = next;
+  a.B = d.B; a.n_tokens = (int)step->n_tokens; a.max_new = (int)step->max_new;
+  return launch_tree_accept(a, (hipStream_t)stream) == hipSuccess ? EA_OK : EA_ERR_DEVICE;
+}
+
+ea_status ea_attend_tree(const ea_params* p, const void* q, const ea_step* step, const ea_tree* tree, const void* k, const void* v,
+                         const int32_t* lengths, int64_t n, int64_t n_cap, void* out, float* lse, void* ws, size_t ws_bytes,
+                         void* stream) {
+  Dims d;
+  ea_status s = check_params(p, &d);
+  if (s != EA_OK || (s = check_tree(step, tree)) != EA_OK) return s;
+  if (n > n_cap || n_cap < 1 || n_cap > ((int64_t)1 << 40)) return EA_ERR_INVALID_ARG;
+  return attend(d, q, step, tree, k, v, nullptr, nullptr, nullptr, nullptr, lengths, true, n, n_cap, out, lse, ws, ws_bytes, stream);
+}
+
+ea_status ea_attend_tree_paged(const ea_params* p, const void* q, const ea_step* step, const ea_tree* tree, const void* k_pool,
+                               const void* v_pool, const ea_paged* pg, const int32_t* lengths, int64_t n, void* out, float* lse,
+                               void* ws, size_t ws_bytes, void* stream) {
+  Dims d;
+  ea_status s = check_params(p, &d);
+  if (s != EA_OK || (s = check_tree(step, tree)) != EA_OK) return s;
+  PageMap pm;
+  if ((s = check_paged(d, pg, n, &pm)) != EA_OK) return s;
+  return attend(d, q, step, tree, k_pool, v_pool, &pm, nullptr, nullptr, nullptr, lengths, false, n, 0, out, lse, ws, ws_bytes, stream);
+}
+
+ea_status ea_attend_tree_mx(const ea_params* p, const void* q, const ea_step* step, const ea_tree* tree, const ea_mx* mx,
+                            const ea_paged* pg, const int32_t* lengths, int64_t n, void* out, float* lse, void* ws, size_t ws_bytes,
+                            void* stream) {
+  Dims d;
+  ea_status s = check_params(p, &d);
+  if (s != EA_OK || (s = check_tree(step, tree)) != EA_OK) return s;
+  PageMap pm;
+  if ((s = check_paged(d, pg, n, &pm)) != EA_OK) return s;
+  if (!mx) return EA_ERR_INVALID_ARG;
+  return attend(d, q, step, tree, mx->k, mx->v, &pm, nullptr, nullptr, mx, lengths, false, n, 0, out, lse, ws, ws_bytes, stream);
+}
+
+ea_status ea_keep_path(const ea_params* p, const ea_step* step, const int32_t* path, const int32_t* n_path, void* k, void* v,
+                       const int32_t* lengths, int64_t n_cap, int32_t* len_out, void* stream) {
+  Dims d;
+  const ea_status s = check_params(p, &d, true);
+  if (s != EA_OK) return s;
+  if (!aligned(k, 16) || !aligned(v, 16) || n_cap < 1 || n_cap > ((int64_t)1 << 40)) return EA_ERR_INVALID_ARG;
+  const int row = d.D * d.esize();
+  const size_t bytes[2] = {(size_t)d.units() * n_cap * row, (size_t)d.units() * n_cap * row};
+  if (overlap(k, bytes[0], v, bytes[1])) return EA_ERR_INVALID_ARG;
+  KeepArgs a = {{(char*)k, (char*)v}, {row, row}, 2};
+  a.n_cap = n_cap;
+  return keep_path(d, step, path, n_path, a, bytes, lengths, len_out, true, stream);
+}
+
+ea_status ea_keep_path_paged(const ea_params* p, const ea_step* step, const int32_t* path, const int32_t* n_path, void* k_pool,
+                             void* v_pool, const ea_paged* pg, const int64_t* slots, const int32_t* lengths, int32_t* len_out,
+                             void* stream) {
+  Dims d;
+  ea_status s = check_params(p, &d);
+  if (s != EA_OK) return s;
+  PageMap pm;
+  if ((s = check_paged(d, pg, 1, &pm)) != EA_OK) return s;
+  if (!aligned(k_pool, 16) || !aligned(v_pool, 16) || (slots && !aligned(slots, 8))) return EA_ERR_INVALID_ARG;
+  const size_t pool = ((size_t)pm.num_blocks << pm.sh) * d.Hkv * d.D * 2, bytes[2] = {pool, pool};
+  if (overlap(k_pool, pool, v_pool, pool)) return EA_ERR_INVALID_ARG;
+  KeepArgs a = {{(char*)k_pool, (char*)v_pool}, {d.D * 2, d.D * 2}, 2};
+  a.pm = pm;
+  a.slots = slots;
+  return keep_path(d, step, path, n_path, a, bytes, lengths, len_out, false, stream);
+}
+
+ea_status ea_keep_path_mx(const ea_params* p, const ea_step* step, const int32_t* path, const int32_t* n_path, const ea_mx* mx,
+                          const ea_paged* pg, const int64_t* slots, const int32_t* lengths, int32_t* len_out, void* stream) {
+  Dims d;
+  ea_status s = check_params(p, &d);
+  if (s != EA_OK) return s;
+  PageMap pm;
+  size_t pool, scales;
+  if ((s = check_paged(d, pg, 1, &pm)) != EA_OK || (s = check_mx(d, mx, pm, &pool, &scales)) != EA_OK) return s;
+  if (slots && !aligned(slots, 8)) return EA_ERR_INVALID_ARG;
+  const size_t bytes[4] = {pool, pool, scales, scales};
+  const int row = mx->format == EA_MXFP8 ? d.D : d.D / 2;
+  KeepArgs a = {{(char*)mx->k, (char*)mx->v, (char*)mx->k_scale, (char*)mx->v_scale}, {row, row, d.D / 32, d.D / 32}, 4};
+  a.pm = pm;
+  a.slots = slots;
+  return keep_path(d, step, path, n_path, a, bytes, lengths, len_out, false, stream);
 }
 
 }  // extern "C"
