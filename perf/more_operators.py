@@ -525,7 +525,7 @@ def run(st):
             return dict(_held(st), q=q)
     if form in ("fill", "read"):
         if own:
-            ea.read_mx(st["p"], st["mx"], st["pg"], st["lens"], st["most"], st["cap"], st["k_out"], st["v_out"])
+            ea.read_mx(st["p"], st["mx"], st["pg"], st["lens"], min(st["most"], st["cap"]), st["cap"], st["k_out"], st["v_out"])
             k, v = st["k_out"], st["v_out"]
         else:
             k, v = _plain_read(st)
