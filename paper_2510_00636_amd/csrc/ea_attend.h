@@ -4,6 +4,7 @@
 
 #include "ea_kernels.h"
 #include "ea_lanes.h"
+#include "ea_mx.h"
 
 namespace ea {
 
@@ -36,6 +37,11 @@ struct AttendArgs {
   int f32;                        // rows are fp32
   AttendPlan plan;
 };
+
+// what cached rows are: bf16 numbers, e4m3 bytes with a scale per head, MX rows
+enum Rows { kRowsBf16, kRowsFp8, kRowsMx8, kRowsMx4 };
+enum { kKindF32 = -1 };                 // and fp32 ones, for add_not_finite()
+constexpr int kind_of(Rows r) { return (int)r; }
 
 // the tokens of a sequence, clamped so that no list of prefix sums leads outside q and out
 __device__ __forceinline__ int clamped(int t, int most) { return t < 0 ? 0 : t > most ? most : t; }
@@ -204,22 +210,29 @@ __device__ __forceinline__ uint32_t finite_pair(uint32_t w, bool& any) {
   any |= lo || hi;
   return (lo ? 0u : w & 0xffffu) | (hi ? 0u : w & 0xffff0000u);
 }
-// adds to x the four values at `channel` of rows lo .. hi - 1 that are not finite; kind 0 bf16, 1 e4m3, 2 fp32
-template <int D, int KIND>
-__device__ __forceinline__ void add_not_finite(const AttendArgs& a, int b, int h, int lo, int hi, int channel, float* x) {
+// adds to x the four values at `channel` of those rows lo .. hi - 1 for which seen(row) that are not finite; kind one of Rows, or fp32
+struct SeenAll { __device__ __forceinline__ bool operator()(int) const { return true; } };
+template <int D, int KIND, class SEEN = SeenAll>
+__device__ __forceinline__ void add_not_finite(const AttendArgs& a, int b, int h, int lo, int hi, int channel, float* x, SEEN seen = {}) {
   for (int key = lo; key < hi; ++key) {
-    const long long at = row_base(a, b, h, key, table_entry(a, b, key)) * D + channel;
+    if (!seen(key)) continue;
+    const long long row = row_base(a, b, h, key, table_entry(a, b, key)), at = row * D + channel;
     float v[4];
-    if constexpr (KIND == 2) {
+    if constexpr (KIND == kKindF32) {
       const float4 w = *(const float4*)((const float*)a.v + at);
       v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
     } else {
       uint2 w;
-      if constexpr (KIND == 1) {
+      if constexpr (KIND == kRowsBf16) {
+        w = *(const uint2*)((const __bf16*)a.v + at);
+      } else if constexpr (KIND == kRowsFp8) {
         const uint4 t = widen_fp8(make_uint2(*(const uint32_t*)((const char*)a.v + at), 0u));
         w = make_uint2(t.x, t.y);
       } else {
-        w = *(const uint2*)((const __bf16*)a.v + at);
+        const float scale = mx_scale(a.vscale8[row * (D / 32) + channel / 32]);
+        const uint4 t = KIND == kRowsMx8 ? widen_mx8(make_uint2(*(const uint32_t*)((const char*)a.v + at), 0u), scale)
+                                         : widen_mx4(*(const uint16_t*)((const char*)a.v + at / 2), scale);
+        w = make_uint2(t.x, t.y);
       }
       v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u);
       v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
@@ -246,7 +259,22 @@ __device__ __forceinline__ float natural_lse(float m, float l) {
   return l == 0.0f ? -__builtin_inff() : fmaf(m, 0.6931471805599453f, logf(l * 256.0f));
 }
 
+// four channels of a finished row, whose values have the scale vs
+template <int D>
+__device__ __forceinline__ void write_row(const AttendArgs& a, int t0, int h, int tok, int hd, int c4, float vs, float top, float sum, float4 acc) {
+  const long long at = (long long)(t0 + tok) * a.Hq + h * a.G + hd;
+  const bool any = sum > 0.0f || sum != sum;
+  const float f = vs / sum;
+  *(uint2*)((__bf16*)a.out + at * D + c4) =
+      any ? make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f)) : make_uint2(0u, 0u);
+  if (a.lse && c4 == 0) a.lse[at] = natural_lse(top, sum);
+}
+
 hipError_t launch_attend(const AttendArgs& a, const Dims& d, hipStream_t st);
+hipError_t launch_attend_rows_tree(const AttendArgs& a, const Dims& d, hipStream_t st);
+hipError_t launch_attend_rows_mx8(const AttendArgs& a, const Dims& d, hipStream_t st);
+hipError_t launch_attend_rows_mx4(const AttendArgs& a, const Dims& d, hipStream_t st);
+hipError_t launch_attend_rows_join(const AttendArgs& a, hipStream_t st);
 hipError_t launch_attend_wave(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_rows(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_tile(const AttendArgs& a, const Dims& d, hipStream_t st);

@@ -143,7 +143,7 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
     const int rw = row0 + r, tk = rw / a.G;
     if (one_bad) {
       float y[4] = {x.x, x.y, x.z, x.w};
-      add_not_finite<D, 2>(a, b, h, max(max(all_see, key_lo), 0), min(len - (m - 1 - tk), key_hi), c4, y);
+      add_not_finite<D, kKindF32>(a, b, h, max(max(all_see, key_lo), 0), min(len - (m - 1 - tk), key_hi), c4, y);
       x = make_float4(y[0], y[1], y[2], y[3]);
     }
     const bool any = sum > 0.0f || sum != sum;

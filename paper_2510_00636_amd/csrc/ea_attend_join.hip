@@ -1,4 +1,4 @@
-// The joining launch of stretches that are cut along the keys (bf16, 8-bit and fp32 rows).
+// The joining launch of stretches that are cut along the keys (16-, 8-, 4-bit and fp32 rows).
 #include "ea_attend.h"
 
 namespace ea {
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
     }
     if (token < t0 || token >= t0 + m || (a.only_long && m * a.G <= a.short_rows) || cut.y <= 1) continue;
     const int row = (token - t0) * a.G + (head - h * a.G), tile = row / a.plan.tile_rows;
-    const int vis = rows_of(a, b, h) - (m - 1 - (token - t0));
+    const int vis = rows_of(a, b, h) - (a.sees ? 0 : m - 1 - (token - t0));
     int n = (vis + cut.z - 1) / cut.z;
     n = n < 1 ? 0 : n > cut.y ? cut.y : n;
     const int first = cut.x + (cut.w - 1 - tile) * cut.y * a.Hkv + h;

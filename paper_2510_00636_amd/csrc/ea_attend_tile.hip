@@ -358,7 +358,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
         float x[4] = {o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]};
-        add_not_finite<D, FP8 ? 1 : 0>(a, b, h, max(max(all_see, key_lo), 0), min(vis, key_hi), c * 32 + r * 2 + hi * 4, x);
+        add_not_finite<D, FP8 ? kRowsFp8 : kRowsBf16>(a, b, h, max(max(all_see, key_lo), 0), min(vis, key_hi), c * 32 + r * 2 + hi * 4, x);
         o[c][r] = x[0]; o[c][r + 1] = x[1]; o[c][r + 2] = x[2]; o[c][r + 3] = x[3];
       }
   const long long at = (long long)(t0 + tok) * a.Hq + h * a.G + hd;

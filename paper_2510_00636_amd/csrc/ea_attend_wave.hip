@@ -38,6 +38,7 @@ __global__ __launch_bounds__(64) void k_attend_wave(AttendArgs a) {
   while (b < a.B && first_token(a, b + 1) <= token) ++b;
   if (b >= a.B || token < first_token(a, b)) return;
   const int t0 = first_token(a, b), m = first_token(a, b + 1) - t0, len = rows_of(a, b, h), old = len - m;
+  if (a.only_long && m * a.G <= a.short_rows) return;
   float q[kPer], o[kPer] = {};
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {

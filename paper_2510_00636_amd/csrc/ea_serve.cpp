@@ -15,10 +15,12 @@ static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 constexpr int kPlanCus = 256;      // a plan, and with it the size of its workspace, is the same wherever it is made
 
 hipError_t launch_attend(const AttendArgs& a, const Dims& d, hipStream_t st) {
-  if (a.mx || a.sees) return launch_attend_wave(a, d, st);
   hipError_t e = hipSuccess;
-  if (a.plan.rows) e = launch_attend_rows(a, d, st);
+  if (a.plan.rows)
+    e = a.mx == 8 ? launch_attend_rows_mx8(a, d, st) : a.mx == 4 ? launch_attend_rows_mx4(a, d, st)
+        : a.sees ? launch_attend_rows_tree(a, d, st) : launch_attend_rows(a, d, st);
   if (e != hipSuccess || !a.plan.tile) return e;
+  if (a.mx || a.sees) return launch_attend_wave(a, d, st);
   return d.dtype == EA_BF16 ? launch_attend_tile(a, d, st) : launch_attend_f32(a, st);
 }
 
