@@ -34,7 +34,6 @@ struct AttendArgs {
   int mx;                         // bits of an element of such pools, 0: others
   const uint64_t* sees;           // trees: which of its sequence's new rows a token sees, `words` words each; null: those up to its own
   int words;
-  int f32;                        // rows are fp32
   AttendPlan plan;
 };
 
@@ -274,8 +273,10 @@ hipError_t launch_attend(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_rows_tree(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_rows_mx8(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_rows_mx4(const AttendArgs& a, const Dims& d, hipStream_t st);
+hipError_t launch_attend_tile_tree(const AttendArgs& a, const Dims& d, hipStream_t st);
+hipError_t launch_attend_tile_mx8(const AttendArgs& a, const Dims& d, hipStream_t st);
+hipError_t launch_attend_tile_mx4(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_rows_join(const AttendArgs& a, hipStream_t st);
-hipError_t launch_attend_wave(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_rows(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_tile(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_f32(const AttendArgs& a, hipStream_t st);

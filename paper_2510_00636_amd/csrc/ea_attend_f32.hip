@@ -15,7 +15,8 @@ template <int D, bool KEYS> constexpr int f32_waves() { return KEYS && D < 256 ?
 template <int D, bool KEYS> constexpr int f32_rows() { return KEYS ? kAttendF32Rows : kAttendF32LongRows; }
 }  // namespace
 
-template <int D, bool KEYS>
+// TREE: which of its sequence's new rows a token sees is a mask; else they are those up to its own.
+template <int D, bool KEYS, bool TREE>
 __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) void k_attend_f32(AttendArgs a) {
   constexpr int kSteps = D / 16, kLoads = D / 64, kM = f32_rows<D, KEYS>(), kNW = f32_waves<D, KEYS>(), kPitch = D + 4;
   extern __shared__ __attribute__((aligned(16))) float pass_o[];          // KEYS: [wavefront][row][channel], and behind it maxima and sums
@@ -26,19 +27,32 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
   note_cuts(a, piece, blockIdx.x);
   const int b = piece.b, h = piece.h, t0 = piece.t0, m = piece.m, rows = m * a.G, row0 = piece.tile * kM;
   const int len = rows_of(a, b, h);
-  int key_hi = len - (m - 1 - (min(row0 + kM, rows) - 1) / a.G);
+  const int new_rows = len - m;                          // where the step's own begin
+  int key_hi = TREE ? len : len - (m - 1 - (min(row0 + kM, rows) - 1) / a.G);
   key_hi = key_hi < 0 ? 0 : key_hi;
   const int key_lo = piece.split * piece.chunk;
   if (piece.nsplit > 1) {
     if (key_lo >= key_hi) return;
     key_hi = min(key_hi, key_lo + piece.chunk);
   }
-  const int all_see = len - (m - 1 - row0 / a.G);        // rows from here on some of the tile's tokens do not see
+  const int all_see = TREE ? new_rows : len - (m - 1 - row0 / a.G);        // rows from here on some of the tile's tokens do not see
   bool bad = false;                                     // one of those has a value that is not finite
   const int my_rows = row0 + (KEYS ? 0 : wave * 16);
   const int row = my_rows + n16, tok = row / a.G, hd = row - tok * a.G;
   const bool in = row < rows;
-  const int vis = in ? len - (m - 1 - tok) : len, vis_min = len - (m - 1 - my_rows / a.G);
+  const int vis = in ? len - (m - 1 - tok) : len, vis_min = TREE ? new_rows : len - (m - 1 - my_rows / a.G);
+  // bits of the mask of token `of` from the one of row `key` on (TREE)
+  auto seen_from = [&](int of, int key) -> uint64_t {
+    const uint64_t* mask = a.sees + (long long)(t0 + of) * a.words;
+    auto word = [&](int w) -> uint64_t {
+      const int left = m - 64 * w;
+      const uint64_t x = w < a.words && left > 0 ? mask[w] : 0;
+      return left >= 64 || left <= 0 ? x : x & ((1ull << left) - 1);
+    };
+    const int from = key - new_rows, w = from >> 6, shift = from & 63;
+    if (from < 0) return from <= -64 ? ~0ull : word(0) << (-from & 63) | ((1ull << (-from & 63)) - 1);
+    return word(w) >> shift | (shift > 0 ? word(w + 1) << (64 - shift) : 0);
+  };
   float4 q[kSteps];
   {
     const float* src = (const float*)a.q + (long long)(t0 + (in ? tok : 0)) * a.q_stride + (h * a.G + (in ? hd : 0)) * D;
@@ -89,7 +103,13 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
     __builtin_amdgcn_sched_barrier(0);
     s0 += s1;
     s0 *= a.scale;
-    if (key + 16 > vis_min || key + 16 > key_hi)
+    if constexpr (TREE) {
+      if (key + 16 > vis_min || key + 16 > key_hi) {
+        const uint32_t bits = key < key_hi ? (uint32_t)seen_from(in ? tok : 0, key) & (key + 16 > key_hi ? (1u << (key_hi - key)) - 1 : 0xffffu) : 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s0[r] = bits >> (4 * g + r) & 1 ? s0[r] : -__builtin_inff();
+      }
+    } else if (key + 16 > vis_min || key + 16 > key_hi)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         if (key + 4 * g + r >= vis || key + 4 * g + r >= key_hi) s0[r] = -__builtin_inff();
@@ -143,7 +163,9 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
     const int rw = row0 + r, tk = rw / a.G;
     if (one_bad) {
       float y[4] = {x.x, x.y, x.z, x.w};
-      add_not_finite<D, kKindF32>(a, b, h, max(max(all_see, key_lo), 0), min(len - (m - 1 - tk), key_hi), c4, y);
+      const int lo = max(max(all_see, key_lo), 0);
+      if constexpr (TREE) add_not_finite<D, kKindF32>(a, b, h, lo, key_hi, c4, y, [&](int key) { return seen_from(tk, key) & 1; });
+      else add_not_finite<D, kKindF32>(a, b, h, lo, min(len - (m - 1 - tk), key_hi), c4, y);
       x = make_float4(y[0], y[1], y[2], y[3]);
     }
     const bool any = sum > 0.0f || sum != sum;
@@ -196,24 +218,25 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
   }
 }
 
-template <int D, bool KEYS>
+template <int D, bool KEYS, bool TREE>
 static hipError_t f32_of_shape(const AttendArgs& a, hipStream_t st) {
   static LdsOptIn opt;
   constexpr int kNW = f32_waves<D, KEYS>(), kM = f32_rows<D, KEYS>();
   const size_t lds = KEYS ? (size_t)kNW * kM * (D + 4 + 2) * sizeof(float) : 0;
-  hipError_t e = opt.ensure((const void*)k_attend_f32<D, KEYS>, lds);
+  hipError_t e = opt.ensure((const void*)k_attend_f32<D, KEYS, TREE>, lds);
   if (e != hipSuccess) return e;
-  k_attend_f32<D, KEYS><<<(unsigned)a.plan.grid, kNW * 64, lds, st>>>(a);
+  k_attend_f32<D, KEYS, TREE><<<(unsigned)a.plan.grid, kNW * 64, lds, st>>>(a);
   e = hipGetLastError();
   return e != hipSuccess || a.plan.most_pieces == 0 ? e : launch_attend_join(a, true, st);
 }
+template <int D>
+static hipError_t f32_of_size(const AttendArgs& a, hipStream_t st) {
+  if (a.sees) return a.plan.tile_rows == kAttendF32Rows ? f32_of_shape<D, true, true>(a, st) : f32_of_shape<D, false, true>(a, st);
+  return a.plan.tile_rows == kAttendF32Rows ? f32_of_shape<D, true, false>(a, st) : f32_of_shape<D, false, false>(a, st);
+}
 
 hipError_t launch_attend_f32(const AttendArgs& a, hipStream_t st) {
-#define EA_CASE(DD) if (a.D == DD) return a.plan.tile_rows == kAttendF32Rows ? f32_of_shape<DD, true>(a, st) : f32_of_shape<DD, false>(a, st)
-  EA_CASE(64);
-  EA_CASE(128);
-#undef EA_CASE
-  return a.plan.tile_rows == kAttendF32Rows ? f32_of_shape<256, true>(a, st) : f32_of_shape<256, false>(a, st);
+  return a.D == 64 ? f32_of_size<64>(a, st) : a.D == 128 ? f32_of_size<128>(a, st) : f32_of_size<256>(a, st);
 }
 
 }  // namespace ea

@@ -1,0 +1,14 @@
+// Attention of trees of many (token, head) rows, over bf16 rows.
+#include "ea_attend_tile.h"
+
+namespace ea {
+
+hipError_t launch_attend_tile_tree(const AttendArgs& a, const Dims& d, hipStream_t st) {
+#define EA_CASE(DD) if (d.D == DD) return a.pm.table ? tile_of_type<DD, kRowsBf16, true, true>(a, st) : tile_of_type<DD, kRowsBf16, false, true>(a, st)
+  EA_CASE(64);
+  EA_CASE(128);
+#undef EA_CASE
+  return a.pm.table ? tile_of_type<256, kRowsBf16, true, true>(a, st) : tile_of_type<256, kRowsBf16, false, true>(a, st);
+}
+
+}  // namespace ea

@@ -20,8 +20,9 @@ hipError_t launch_attend(const AttendArgs& a, const Dims& d, hipStream_t st) {
     e = a.mx == 8 ? launch_attend_rows_mx8(a, d, st) : a.mx == 4 ? launch_attend_rows_mx4(a, d, st)
         : a.sees ? launch_attend_rows_tree(a, d, st) : launch_attend_rows(a, d, st);
   if (e != hipSuccess || !a.plan.tile) return e;
-  if (a.mx || a.sees) return launch_attend_wave(a, d, st);
-  return d.dtype == EA_BF16 ? launch_attend_tile(a, d, st) : launch_attend_f32(a, st);
+  if (a.mx) return a.mx == 8 ? launch_attend_tile_mx8(a, d, st) : launch_attend_tile_mx4(a, d, st);
+  if (d.dtype != EA_BF16) return launch_attend_f32(a, st);
+  return a.sees ? launch_attend_tile_tree(a, d, st) : launch_attend_tile(a, d, st);
 }
 
 // MX pools: four tensors of their own
@@ -77,7 +78,8 @@ static ea_status attend(const Dims& d, const void* q, const ea_step* step, const
   // joining one than 512 times 64 rows; the stretches' joining one comes with few tiles only.)
   if (a.plan.tile && a.plan.grid > kAttendMaxGrid) return EA_ERR_UNSUPPORTED;
   // the stretches' kernel steps over a block by a 32-bit number of bytes
-  if (pm && a.plan.tile && (((uint64_t)d.Hkv << pm->sh) * d.D * d.esize()) >> 32) return EA_ERR_UNSUPPORTED;
+  const int per_channel = mx ? mx->format == EA_MXFP8 ? 8 : 4 : 8 * d.esize();      // bits
+  if (pm && a.plan.tile && (((uint64_t)d.Hkv << pm->sh) * d.D * per_channel / 8) >> 32) return EA_ERR_UNSUPPORTED;
   if (ws_bytes < a.plan.total) return EA_ERR_WORKSPACE;
   if (step->n_tokens == 0) return EA_OK;
   a.q = q; a.k = k; a.v = v; a.cu = step->cu_tokens; a.lens = lengths; a.kscale = kscale; a.vscale = vscale;
@@ -86,7 +88,6 @@ static ea_status attend(const Dims& d, const void* q, const ea_step* step, const
   a.n_cap = n_cap;
   a.B = d.B; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.G; a.D = d.D;
   a.n = (int)n; a.n_tokens = (int)step->n_tokens; a.per_head = per_head;
-  a.f32 = d.dtype == EA_F32;
   if (mx) {
     a.mx = mx->format == EA_MXFP8 ? 8 : 4;
     a.kscale8 = mx->k_scale;
