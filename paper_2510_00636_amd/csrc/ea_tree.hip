@@ -95,27 +95,29 @@ __global__ __launch_bounds__(64) void k_tree_accept(TreeArgs a) {
   if (lane == 0) a.n_path[b] = count, a.next[b] = want;
 }
 
-// A workgroup per KV head.  A thread has 16 bytes (or what a shorter row has) of every row that moves, and takes them in order: numbers
-// ascend, so that no row is written before it is read.
-__global__ __launch_bounds__(128) void k_keep_path(KeepArgs a) {
+// A workgroup per KV head.  What says which rows move is asked for together (lengths, counts, the path), then the table's entries, then
+// as many rows as the threads have room for, 16 bytes (or what a shorter row has) to a piece: three round trips to memory for a
+// branch.  Numbers ascend, so a round that is written leaves the rows of the next ones alone.
+__global__ __launch_bounds__(256) void k_keep_path(KeepArgs a) {
+  using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+  using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
+  constexpr int kThreads = 256, kPer = 4;
   __shared__ long long src[kTreeMost], dst[kTreeMost];
   const int unit = blockIdx.x, b = unit / a.Hkv, h = unit - b * a.Hkv, tid = threadIdx.x, lane = tid & 63;
-  const int t0 = token_bound(a.cu, b, a.n_tokens), m = max(token_bound(a.cu, b + 1, a.n_tokens) - t0, 0);
-  const int given = a.lens[a.per_head ? unit : b], len = max(given, 0);
-  const bool served = m > 0 && !(a.slots && a.slots[t0] < 0);
-  int n = served ? min(min(a.n_path[b], a.max_new), min(m, kTreeMost)) : 0;
-  n = max(n, 0);
   const int32_t* path = a.path + (long long)b * a.max_new;
+  const int t0 = token_bound(a.cu, b, a.n_tokens), m = max(token_bound(a.cu, b + 1, a.n_tokens) - t0, 0);
+  const int given = a.lens[a.per_head ? unit : b], len = max(given, 0), count = a.n_path[b];
+  const int x0 = lane < a.max_new ? path[lane] : -1;
+  const bool served = m > 0 && !(a.slots && a.slots[t0] < 0);
+  int n = served ? max(min(min(count, a.max_new), min(m, kTreeMost)), 0) : 0;
   // the path ends in front of its first number that makes no sense
+  int before = -1;
   for (int base = 0; base < n; base += 64) {
-    const int j = base + lane;
-    bool wrong = false;
-    if (j < n) {
-      const int x = path[j];
-      wrong = x >= m || x < 0 || (j > 0 && path[j - 1] >= x);
-    }
-    const uint64_t some = __ballot(wrong);
-    if (some) n = base + __builtin_ctzll(some);
+    const int j = base + lane, x = base == 0 ? x0 : j < n ? path[j] : -1;
+    const int left = lane == 0 ? before : __shfl_up(x, 1);
+    before = __shfl(x, 63);
+    const uint64_t wrong = __ballot(j < n && (x >= m || x < 0 || x <= left));
+    if (wrong) n = base + __builtin_ctzll(wrong);
   }
   if (tid == 0 && (a.per_head || h == 0)) a.len_out[a.per_head ? unit : b] = served ? max(len - m + n, 0) : given;
   auto row_at = [&](long long r) -> long long {      // -1: there is none
@@ -127,32 +129,55 @@ __global__ __launch_bounds__(128) void k_keep_path(KeepArgs a) {
     blk = blk < 0 ? 0 : blk < a.pm.num_blocks ? blk : a.pm.num_blocks - 1;
     return ((blk * a.Hkv + h) << a.pm.sh) + (r & ((1 << a.pm.sh) - 1));
   };
-  for (int j = tid; j < n; j += 128) {
-    const long long first = (long long)len - m;
-    src[j] = row_at(first + path[j]);
-    dst[j] = row_at(first + j);
+  // rows that stay where they are, or that are not there, are passed over
+  const long long first = (long long)len - m;
+  for (int j = tid; j < n; j += kThreads) {
+    const int x = j == lane ? x0 : path[j];
+    const long long s = x == j ? -1 : row_at(first + x), t = s < 0 ? -1 : row_at(first + j);
+    src[j] = t < 0 ? -1 : s;
+    dst[j] = t;
   }
   __syncthreads();
-  // rows in front that stay where they are, or that are not there, are passed over
-  int from = 0;
-  while (from < n && (src[from] == dst[from] || src[from] < 0 || dst[from] < 0)) ++from;
-  if (from == n) return;
-  int item = tid;
-  for (int i = 0; i < a.count; ++i) {
-    const int bytes = a.row_bytes[i], each = bytes < 16 ? bytes : 16, pieces = bytes / each;
-    for (; item < pieces; item += 128) {
-      char* base = a.at[i] + item * each;
-      for (int j = from; j < n; ++j) {
-        if (src[j] < 0 || dst[j] < 0) continue;
-        const char* s = base + src[j] * bytes;
-        char* t = base + dst[j] * bytes;
-        if (each == 16) *(uint4*)t = *(const uint4*)s;
-        else if (each == 8) *(uint2*)t = *(const uint2*)s;
-        else if (each == 4) *(uint32_t*)t = *(const uint32_t*)s;
-        else *(uint16_t*)t = *(const uint16_t*)s;
+  // A thread's pieces of the rows of a round: read, and written behind the barrier.
+  int pieces = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < a.count) pieces += a.row_bytes[i] < 16 ? 1 : a.row_bytes[i] / 16;
+  const int per_round = kPer * kThreads / pieces;          // rows (a row has up to 128 pieces)
+  for (int j0 = 0; j0 < n; j0 += per_round) {
+    const int rows = min(per_round, n - j0);
+    u32x4 x[kPer];
+    char* to[kPer];
+    int bytes[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int at = k * kThreads + tid, j = at / pieces;
+      bytes[k] = 0;
+      if (j >= rows || src[j0 + j] < 0) continue;
+      int piece = at - j * pieces, row_bytes = 0;
+      char* base = nullptr;
+#pragma unroll
+      for (int i = 3; i >= 0; --i) {                        // the tensors from the last on, pieces in that order
+        if (i >= a.count || row_bytes) continue;
+        const int mine = a.row_bytes[i] < 16 ? 1 : a.row_bytes[i] / 16;
+        if (piece < mine) base = a.at[i], row_bytes = a.row_bytes[i];
+        else piece -= mine;
       }
+      const char* from = base + src[j0 + j] * row_bytes + piece * 16;
+      to[k] = base + dst[j0 + j] * row_bytes + piece * 16;
+      bytes[k] = row_bytes < 16 ? row_bytes : 16;
+      if (bytes[k] == 16) x[k] = *(const u32x4*)from;
+      else if (bytes[k] == 8) x[k] = u32x4{((const uint32_t*)from)[0], ((const uint32_t*)from)[1], 0, 0};
+      else x[k] = u32x4{bytes[k] == 4 ? *(const uint32_t*)from : *(const uint16_t*)from, 0, 0, 0};
     }
-    item -= pieces;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      if (bytes[k] == 16) *(u32x4*)to[k] = x[k];
+      else if (bytes[k] == 8) *(u32x2*)to[k] = u32x2{x[k].x, x[k].y};
+      else if (bytes[k] == 4) *(uint32_t*)to[k] = x[k].x;
+      else if (bytes[k] == 2) *(uint16_t*)to[k] = (uint16_t)x[k].x;
+    }
   }
 }
 
@@ -165,7 +190,7 @@ hipError_t launch_tree_accept(const TreeArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 hipError_t launch_keep_path(const KeepArgs& a, hipStream_t st) {
-  k_keep_path<<<(unsigned)(a.B * a.Hkv), 128, 0, st>>>(a);
+  k_keep_path<<<(unsigned)(a.B * a.Hkv), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
