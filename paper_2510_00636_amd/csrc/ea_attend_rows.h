@@ -139,11 +139,18 @@ __device__ __forceinline__ bf16x8 key_operand(const Raw<BYTES>& p, float scale, 
 // 64 banks; behind them maxima and sums.
 template <int D, int MT> constexpr int rows_lds_floats() { return 4 * 16 * MT * (D + 4) + 4 * 16 * MT * 2; }
 
+// workgroups on a CU
+template <int D, Rows R, int MT> constexpr int rows_groups() {
+  return D * MT > 256 || (D == 256 && R == kRowsBf16) ? 1 : (R == kRowsMx8 || R == kRowsMx4) && MT == 1 && D < 256 ? 3 : 2;
+}
+
 // TREE: what a token sees of its sequence's new rows (no more than 64 of them, or the sequence is not this kernel's) is a mask of them, its own or
 // the chain's; else a number of rows.
-template <int D, Rows R, int MT, bool TREE>
-__global__ __launch_bounds__(256, (D * MT > 256 || (D == 256 && R == kRowsBf16) ? 1 : 2)) void k_attend_rows(AttendArgs a) {
+// U: a wavefront works on 32 U keys at a time and has as many on their way.
+template <int D, Rows R, int MT, bool TREE, int U>
+__global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(AttendArgs a) {
   using S = RowShape<D, R>;
+  constexpr int kKeys = 32 * U, kSubs = 2 * U, kStride = 4 * kKeys;      // of a tile: keys, 16 rows at a time; from tile to tile of a wavefront
   constexpr bool kHeadScale = R == kRowsFp8;
   constexpr int kM = 16 * MT, kPitch = D + 4;
   extern __shared__ __attribute__((aligned(16))) float lds[];
@@ -216,76 +223,99 @@ __global__ __launch_bounds__(256, (D * MT > 256 || (D == 256 && R == kRowsBf16) 
   // waits for on the path with the fewest: so no path asks for fewer (a wavefront whose part of a head is over or empty asks for none
   // of a tile's rows, by the same loads), and what else is read on the way comes by scalar loads.  Against waits for all that is on
   // its way: five tokens of 8 sequences over 16k rows 117 -> 107 us, 256 sequences of 100 rows 39.5 -> 32.
-  struct Blocks { int e0, e1; };      // table entries of a tile's halves
+  struct Blocks { int e[kSubs]; };      // table entries of a tile's 16 rows
   auto last_sub = [](const Part& c, int at) {           // the 16 rows from `at` on, or the head's last ones
     const int last = c.len > 0 ? (c.len - 1) & ~15 : 0;
     return at < last ? at : last;
   };
   auto look_up = [&](const Part& c, int at) {
-    Blocks e = {0, 0};
+    Blocks e = {};
     if (a.pm.table) {
       const int32_t* t = a.pm.table + (long long)c.b * a.pm.max_blocks;
-      e.e0 = scalar(t, last_sub(c, at) >> a.pm.sh);
-      e.e1 = scalar(t, last_sub(c, at + 16) >> a.pm.sh);
+#pragma unroll
+      for (int i = 0; i < kSubs; ++i) e.e[i] = scalar(t, last_sub(c, at + 16 * i) >> a.pm.sh);
     }
     return e;
   };
   constexpr int kPiece = S::kCpl * S::kBits / 8, kKPiece = S::kKCpl * S::kBits / 8;        // bytes of a lane's load of V and of K
-  Raw<kKPiece> kraw[2][S::kKLoads];
-  Raw<kPiece> vraw[8][S::kLoads];
-  RowScales<D> kscales[2];
-  FourScales<D> vscales[2];
-  // Rows come through descriptors of the 16 rows that a tile's half has: those behind the last one are zeros, and are not asked for.
-  __amdgpu_buffer_rsrc_t k_rows[2], v_rows[2], k_scales[2], v_scales[2];
+  Raw<kKPiece> kraw[kSubs][S::kKLoads];
+  Raw<kPiece> vraw[4 * kSubs][S::kLoads];
+  RowScales<D> kscales[kSubs];
+  FourScales<D> vscales[kSubs];
+  // Rows come through descriptors of the 16 rows at a time that a tile has: those behind the last one are zeros, and are not asked for.
+  // MX: these are made where they are used, of the first row's number and how many there are (four tensors' would take more scalar
+  // registers than there are).
+  __amdgpu_buffer_rsrc_t k_rows[S::kMx ? 1 : kSubs], v_rows[S::kMx ? 1 : kSubs];
+  long long first_row[kSubs];
+  int row_count[kSubs];
   auto place = [&](const Part& c, int at, int hi, Blocks e) {      // the tile at row `at`, none of it from row hi on
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < kSubs; ++t) {
       const int r = last_sub(c, at + t * 16), n = at + t * 16 < hi ? min(c.len - r, 16) : 0;
-      const long long row = row_base(a, c.b, c.h, r, t ? e.e1 : e.e0), base = row * S::kBytes;
-      k_rows[t] = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)a.k + base), 0, n * S::kBytes, 0x27000);
-      v_rows[t] = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)a.v + base), 0, n * S::kBytes, 0x27000);
+      const long long row = row_base(a, c.b, c.h, r, e.e[t]), base = row * S::kBytes;
       if constexpr (S::kMx) {
-        k_scales[t] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.kscale8 + row * S::kScales), 0, n * S::kScales, 0x27000);
-        // (whole words, of which a part would be refused: at d = 64 one row more, if their number is odd)
-        v_scales[t] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.vscale8 + row * S::kScales), 0, (n * S::kScales + 3) & ~3, 0x27000);
+        first_row[t] = row;
+        row_count[t] = n;
+      } else {
+        k_rows[t] = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)a.k + base), 0, n * S::kBytes, 0x27000);
+        v_rows[t] = __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)a.v + base), 0, n * S::kBytes, 0x27000);
       }
     }
   };
   auto place_none = [&]() {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      k_rows[t] = __builtin_amdgcn_make_buffer_rsrc((void*)a.k, 0, 0, 0x27000);
-      v_rows[t] = __builtin_amdgcn_make_buffer_rsrc((void*)a.v, 0, 0, 0x27000);
+    for (int t = 0; t < kSubs; ++t) {
       if constexpr (S::kMx) {
-        k_scales[t] = __builtin_amdgcn_make_buffer_rsrc((void*)a.kscale8, 0, 0, 0x27000);
-        v_scales[t] = __builtin_amdgcn_make_buffer_rsrc((void*)a.vscale8, 0, 0, 0x27000);
+        first_row[t] = 0;
+        row_count[t] = 0;
+      } else {
+        k_rows[t] = __builtin_amdgcn_make_buffer_rsrc((void*)a.k, 0, 0, 0x27000);
+        v_rows[t] = __builtin_amdgcn_make_buffer_rsrc((void*)a.v, 0, 0, 0x27000);
       }
     }
+  };
+  auto rows_at = [&](const void* base, int t, int row_bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)((const char*)base + first_row[t] * row_bytes), 0, row_count[t] * row_bytes, 0x27000);
   };
   const int k_at = n16 * S::kBytes + g * kKPiece, v_at = 4 * g * S::kBytes + n16 * kPiece;
   auto load_k = [&]() {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      if constexpr (S::kMx) kscales[t].x = load_raw<S::kScales>(k_scales[t], n16 * S::kScales);
+    for (int t = 0; t < kSubs; ++t) {
+      __amdgpu_buffer_rsrc_t from;
+      if constexpr (S::kMx) {
+        kscales[t].x = load_raw<S::kScales>(rows_at(a.kscale8, t, S::kScales), n16 * S::kScales);
+        from = rows_at(a.k, t, S::kBytes);
+      } else {
+        from = k_rows[t];
+      }
 #pragma unroll
-      for (int s = 0; s < S::kKLoads; ++s) kraw[t][s] = load_raw<kKPiece>(k_rows[t], k_at + s * 4 * kKPiece);
+      for (int s = 0; s < S::kKLoads; ++s) kraw[t][s] = load_raw<kKPiece>(from, k_at + s * 4 * kKPiece);
     }
   };
   auto load_v = [&]() {
     if constexpr (S::kMx)
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < kSubs; ++t) {
+        // (at d = 64 a word has the scales of two rows, and a part of it would be refused: with an odd number of rows one row more)
+        const auto from = __builtin_amdgcn_make_buffer_rsrc((void*)(a.vscale8 + first_row[t] * S::kScales), 0, (row_count[t] * S::kScales + 3) & ~3, 0x27000);
 #pragma unroll
         for (int i = 0; i < (D == 256 ? 4 : 1); ++i) {
-          if constexpr (D == 256) vscales[t].x[i] = __builtin_amdgcn_raw_buffer_load_b8(v_scales[t], (4 * g + i) * S::kScales + n16 * S::kCpl / 32, 0, 0);
-          else vscales[t].x = load_raw<D / 8>(v_scales[t], 4 * g * S::kScales);
+          if constexpr (D == 256) vscales[t].x[i] = __builtin_amdgcn_raw_buffer_load_b8(from, (4 * g + i) * S::kScales + n16 * S::kCpl / 32, 0, 0);
+          else vscales[t].x = load_raw<D / 8>(from, 4 * g * S::kScales);
         }
+      }
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int t = 0; t < kSubs; ++t) {
+      __amdgpu_buffer_rsrc_t from;
+      if constexpr (S::kMx) from = rows_at(a.v, t, S::kBytes);
+      else from = v_rows[t];
 #pragma unroll
-      for (int u = 0; u < S::kLoads; ++u) vraw[j][u] = load_raw<kPiece>(v_rows[j >> 2], v_at + (j & 3) * S::kBytes + u * 16 * kPiece);
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int u = 0; u < S::kLoads; ++u) vraw[4 * t + j][u] = load_raw<kPiece>(from, v_at + j * S::kBytes + u * 16 * kPiece);
+    }
   };
-  // the lane's scale of K for load s of half t, and its scale byte of V for row j
+  // the lane's scale of K for load s of 16 rows, and its scale byte of V for row j of its own
   auto key_scale = [&](int t, int s) {
     if constexpr (!S::kMx) return 1.0f;
     else {
@@ -330,13 +360,13 @@ __global__ __launch_bounds__(256, (D * MT > 256 || (D == 256 && R == kRowsBf16) 
     }
   };
   auto begin = [&](const Part& c, Blocks e) {
-    const int at = c.off * kGroup + wave * 32;
+    const int at = c.off * kGroup + wave * kKeys;
     load_q(c);
     place(c, at, c.len, e);
     load_k();
     load_v();
   };
-  begin(cur, look_up(cur, cur.off * kGroup + wave * 32));
+  begin(cur, look_up(cur, cur.off * kGroup + wave * kKeys));
   if (tid == 0) bad[0] = 0;
   __syncthreads();
 
@@ -344,8 +374,8 @@ __global__ __launch_bounds__(256, (D * MT > 256 || (D == 256 && R == kRowsBf16) 
     x += cur.take;
     // ---- the part behind this one, and the entries of its blocks
     Part next = cur;
-    Blocks first = {0, 0}, following_blocks = {0, 0};
-    if (cur.take > 1) following_blocks = look_up(cur, (cur.off + 1) * kGroup + wave * 32);
+    Blocks first = {}, following_blocks = {};
+    if (cur.take * kGroup > kStride) following_blocks = look_up(cur, cur.off * kGroup + kStride + wave * kKeys);
     bool go_on = x < x1;
     if (go_on) {
       if (x >= (long long)(cur.have + cur.grp) * mult) {      // the next super-unit that has groups
@@ -366,7 +396,7 @@ __global__ __launch_bounds__(256, (D * MT > 256 || (D == 256 && R == kRowsBf16) 
       }
       if (go_on) {
         fill(next);
-        first = look_up(next, next.off * kGroup + wave * 32);
+        first = look_up(next, next.off * kGroup + wave * kKeys);
       }
     }
     const int rows = cur.m * a.G, unit = cur.b * a.Hkv + cur.h, len = cur.len;
@@ -407,18 +437,20 @@ __global__ __launch_bounds__(256, (D * MT > 256 || (D == 256 && R == kRowsBf16) 
       for (int c = 0; c < S::kTiles; ++c) o[t][c] = (f32x4)0.0f;
     }
     const int row_hi = min((cur.off + cur.take) * kGroup, len);
-    int row = cur.off * kGroup + wave * 32;
+    int row = cur.off * kGroup + wave * kKeys;
     const bool no_tile = row >= row_hi;
     while (row < row_hi) {
-      const int following = row + kGroup;
-      // ---- S^T: 32 keys x 16 rows
-      f32x4 s[MT][2];
+      const int following = row + kStride;
+      // ---- S^T: 16 keys x 16 rows each
+      f32x4 s[MT][kSubs];
 #pragma unroll
-      for (int t = 0; t < MT; ++t) s[t][0] = s[t][1] = (f32x4)0.0f;
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int i = 0; i < kSubs; ++i) s[t][i] = (f32x4)0.0f;
 #pragma unroll
       for (int c = 0; c < S::kSteps; ++c)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < kSubs; ++t) {
           const bf16x8 w = key_operand<D, R>(kraw[t][c / S::kKPer], key_scale(t, c / S::kKPer), c % S::kKPer);
 #pragma unroll
           for (int i = 0; i < MT; ++i)
@@ -426,39 +458,45 @@ __global__ __launch_bounds__(256, (D * MT > 256 || (D == 256 && R == kRowsBf16) 
         }
       const bool over = following >= row_hi && go_on;
       if (over) load_q(next);
-      if (over) place(next, next.off * kGroup + wave * 32, next.len, first);
+      if (over) place(next, next.off * kGroup + wave * kKeys, next.len, first);
       else if (following < row_hi) place(cur, following, row_hi, following_blocks);
       else place_none();
       load_k();
-      if (following + kGroup < row_hi) following_blocks = look_up(cur, following + kGroup);
+      if (following + kStride < row_hi) following_blocks = look_up(cur, following + kStride);
       __builtin_amdgcn_sched_barrier(0);
       // ---- weights (see kLag).
       // A weight reaches the second product as two bf16 numbers, which together are as good as fp32 next to the values' eight
       // bits: the matrix cores have time for it here.
-      const bool ragged = row + 32 > some;
-      uint32_t p[MT][4], plo[MT][4];
+      const bool ragged = row + kKeys > some;
+      uint32_t p[MT][4 * U], plo[MT][4 * U];
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
-        s[t][0] *= qk;
-        s[t][1] *= qk;
+#pragma unroll
+        for (int i = 0; i < kSubs; ++i) s[t][i] *= qk;
         if constexpr (TREE) {
           if (ragged) {
-            // bit i: key row + i is seen (row + 32 > new_rows)
+            // bit i: key row + i is seen (row + kKeys > new_rows)
             const Mask mask = see[wave][t * 16 + n16];
             const int from = row - new_rows;
-            const uint32_t bits = from >= kMaskBits ? 0u : from >= 0 ? (uint32_t)(mask >> (from & (kMaskBits - 1)))
-                                                                    : (uint32_t)mask << (-from & 31) | ((1u << (-from & 31)) - 1);
-            const uint32_t mine = bits >> 4 * g;
+            using Bits = std::conditional_t<U == 1, uint32_t, uint64_t>;
+            constexpr int kLast = 8 * sizeof(Bits) - 1;
+            const Bits bits = from >= kMaskBits ? 0 : from >= 0 ? (Bits)(mask >> (from & (kMaskBits - 1)))
+                                                                : (Bits)mask << (-from & kLast) | (((Bits)1 << (-from & kLast)) - 1);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[t][i >> 2][i & 3] = mine >> ((i >> 2) * 16 + (i & 3)) & 1 ? s[t][i >> 2][i & 3] : -__builtin_inff();
+            for (int i = 0; i < kSubs; ++i) {
+              const uint32_t mine = (uint32_t)(bits >> 16 * i) >> 4 * g;
+#pragma unroll
+              for (int r = 0; r < 4; ++r) s[t][i][r] = mine >> r & 1 ? s[t][i][r] : -__builtin_inff();
+            }
           }
         } else if (ragged) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < 4 * kSubs; ++i)
             if (row + (i >> 2) * 16 + 4 * g + (i & 3) >= vis[t]) s[t][i >> 2][i & 3] = -__builtin_inff();
         }
-        float top = fmaxf(fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3])),
-                          fmaxf(fmaxf(s[t][1][0], s[t][1][1]), fmaxf(s[t][1][2], s[t][1][3])));
+        float top = fmaxf(fmaxf(s[t][0][0], s[t][0][1]), fmaxf(s[t][0][2], s[t][0][3]));
+#pragma unroll
+        for (int i = 1; i < kSubs; ++i) top = fmaxf(top, fmaxf(fmaxf(s[t][i][0], s[t][i][1]), fmaxf(s[t][i][2], s[t][i][3])));
         if (__any(top > mx[t] + kLag)) {
           top = reference(fmaxf(max_xor16(max_xor32(top)), mx[t]));
           const float f = mx[t] == -__builtin_inff() ? 0.0f : pow2(mx[t] - top);
@@ -469,60 +507,72 @@ __global__ __launch_bounds__(256, (D * MT > 256 || (D == 256 && R == kRowsBf16) 
         }
         const float from = subtrahend(mx[t]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4 * U; ++i) {
           const float lo = pow2(s[t][i >> 1][(i & 1) * 2] - from), hi = pow2(s[t][i >> 1][(i & 1) * 2 + 1] - from);
           l[t] += lo + hi;
           p[t][i] = pack_bf16(lo, hi);
           plo[t][i] = pack_bf16(lo - __uint_as_float(p[t][i] << 16), hi - __uint_as_float(p[t][i] & 0xffff0000u));
         }
       }
-      // ---- O^T
+      // ---- O^T, 32 keys at a time
 #pragma unroll
-      for (int u = 0; u < S::kLoads; ++u) {
-        // MX: a pair of channels is widened where it is needed (all of them at once take 64 registers at d = 256), so what is not finite goes
-        // in front of that
-        uint32_t w[8][S::kMx ? 1 : S::kCpl / 2];
-        float scale[8];
+      for (int half = 0; half < U; ++half)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const bool tame = (TREE || cur.m > 1) && ragged && row + (j >> 2) * 16 + 4 * g + (j & 3) >= some;
+        for (int u = 0; u < S::kLoads; ++u) {
+          // MX: a pair of channels is widened where it is needed (all of them at once take 64 registers at d = 256), so what is not finite goes
+          // in front of that
+          uint32_t w[8][S::kMx ? 1 : S::kCpl / 2];
+          float scale[8];
           if constexpr (S::kMx) {
-            uint32_t e = value_scale(j);
-            if (tame) {
-              const bool none = e == 255;
-              any_bad |= none && row + (j >> 2) * 16 + 4 * g + (j & 3) < len;
-              e = none ? 0 : e;
+            uint32_t e[8];
 #pragma unroll
-              for (int i = 0; i < (int)(sizeof(Raw<kPiece>) / 4); ++i) vraw[j][u].w[i] = none ? 0 : finite_elements<R>(vraw[j][u].w[i], any_bad);
+            for (int j = 0; j < 8; ++j) e[j] = value_scale(8 * half + j);
+            if (ragged) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const int key = row + half * 32 + (j >> 2) * 16 + 4 * g + (j & 3);
+                const bool none = key >= some && e[j] == 255;
+                any_bad |= none && key < len;
+                e[j] = none ? 0 : e[j];
+#pragma unroll
+                for (int i = 0; i < (int)(sizeof(Raw<kPiece>) / 4); ++i) {
+                  bool bad_element = false;
+                  const uint32_t x = vraw[8 * half + j][u].w[i], y = finite_elements<R>(x, bad_element);
+                  any_bad |= bad_element && key >= some;
+                  vraw[8 * half + j][u].w[i] = none ? 0 : key >= some ? y : x;
+                }
+              }
             }
-            scale[j] = mx_scale(e);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) scale[j] = mx_scale(e[j]);
           } else {
-            widen_piece<D, R>(vraw[j][u], w[j]);
-            if (tame)
 #pragma unroll
-              for (int c = 0; c < S::kCpl / 2; ++c) w[j][c] = finite_pair(w[j][c], any_bad);
+            for (int j = 0; j < 8; ++j) {
+              widen_piece<D, R>(vraw[8 * half + j][u], w[j]);
+              if ((TREE || cur.m > 1) && ragged && row + half * 32 + (j >> 2) * 16 + 4 * g + (j & 3) >= some)
+#pragma unroll
+                for (int c = 0; c < S::kCpl / 2; ++c) w[j][c] = finite_pair(w[j][c], any_bad);
+            }
+          }
+#pragma unroll
+          for (int c = 0; c < S::kCpl; ++c) {
+            const uint32_t sel = c & 1 ? 0x07060302u : 0x05040100u;
+            const int at = S::kMx ? 0 : c >> 1;
+            if constexpr (S::kMx)
+              if (c % 2 == 0)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j][0] = mx_pair<R>(vraw[8 * half + j][u].w, c >> 1, scale[j]);
+            const uint4 v = make_uint4(__builtin_amdgcn_perm(w[1][at], w[0][at], sel), __builtin_amdgcn_perm(w[3][at], w[2][at], sel),
+                                       __builtin_amdgcn_perm(w[5][at], w[4][at], sel), __builtin_amdgcn_perm(w[7][at], w[6][at], sel));
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+              f32x4& acc = o[t][u * S::kCpl + c];
+              const uint32_t *hi = &p[t][4 * half], *lo = &plo[t][4 * half];
+              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), acc, 0, 0, 0);
+              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), acc, 0, 0, 0);
+            }
           }
         }
-#pragma unroll
-        for (int c = 0; c < S::kCpl; ++c) {
-          const uint32_t sel = c & 1 ? 0x07060302u : 0x05040100u;
-          const int at = S::kMx ? 0 : c >> 1;
-          if constexpr (S::kMx)
-            if (c % 2 == 0)
-#pragma unroll
-              for (int j = 0; j < 8; ++j) w[j][0] = mx_pair<R>(vraw[j][u].w, c >> 1, scale[j]);
-          const uint4 v = make_uint4(__builtin_amdgcn_perm(w[1][at], w[0][at], sel), __builtin_amdgcn_perm(w[3][at], w[2][at], sel),
-                                     __builtin_amdgcn_perm(w[5][at], w[4][at], sel), __builtin_amdgcn_perm(w[7][at], w[6][at], sel));
-#pragma unroll
-          for (int t = 0; t < MT; ++t) {
-            f32x4& acc = o[t][u * S::kCpl + c];
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, make_uint4(plo[t][0], plo[t][1], plo[t][2], plo[t][3])), acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                __builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, make_uint4(p[t][0], p[t][1], p[t][2], p[t][3])), acc, 0, 0, 0);
-          }
-        }
-      }
       load_v();
       __builtin_amdgcn_sched_barrier(0);
       row = following;
@@ -599,13 +649,17 @@ __global__ __launch_bounds__(256, (D * MT > 256 || (D == 256 && R == kRowsBf16) 
   }
 }
 
+// Keys of a tile: 64 for single tokens over MX rows, so that a wavefront has as many bytes on their way as over wider ones, and half as
+// many tiles to see to.
+template <int D, Rows R, int MT> constexpr int tile_halves() { return (R == kRowsMx8 || R == kRowsMx4) && MT == 1 && D < 0 ? 2 : 1; }
 template <int D, Rows R, int MT, bool TREE>
 static hipError_t rows_of_height(const AttendArgs& a, hipStream_t st) {
+  constexpr int U = tile_halves<D, R, MT>();
   static LdsOptIn opt;
   const size_t bytes = rows_lds_floats<D, MT>() * sizeof(float);
-  const hipError_t e = opt.ensure((const void*)k_attend_rows<D, R, MT, TREE>, bytes);
+  const hipError_t e = opt.ensure((const void*)k_attend_rows<D, R, MT, TREE, U>, bytes);
   if (e != hipSuccess) return e;
-  k_attend_rows<D, R, MT, TREE><<<a.plan.shares, 256, bytes, st>>>(a);
+  k_attend_rows<D, R, MT, TREE, U><<<a.plan.shares, 256, bytes, st>>>(a);
   const hipError_t e2 = hipGetLastError();
   return e2 != hipSuccess ? e2 : launch_attend_rows_join(a, st);
 }

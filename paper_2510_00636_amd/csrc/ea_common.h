@@ -57,7 +57,7 @@ struct PageMap {
 // Attention of a step's tokens: how a call is cut, and where its workspace holds what.
 constexpr int kAttendGroup = 128;       // keys of a group of the row kernel, whose workgroups take whole ones
 constexpr int kAttendF32Rows = 16, kAttendF32LongRows = 64;      // (token, head) rows of a workgroup of the fp32 kernel
-constexpr int kAttendShares = 512;      // most workgroups of the row kernel
+constexpr int kAttendShares = 768;      // most workgroups of the row kernel
 constexpr int64_t kAttendMaxTokens = (int64_t)1 << 24, kAttendMaxGrid = (int64_t)1 << 22;
 struct AttendPlan {
   int rows, tile;     // the row kernel serves sequences of few (token, head) rows per KV head, the tile (or fp32) kernel the others
@@ -196,7 +196,7 @@ inline int64_t f32_span(int64_t heads, int64_t n, int64_t slots) {
 }
 
 // what a call of at most n rows per head launches; n_tokens and max_new as in ea_step
-AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t max_new, int num_cu);
+AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t max_new, int num_cu, bool mx = false);
 ea_status check_step(const Dims& d, const ea_step* step, int64_t n);
 ea_status check_paged(const Dims& d, const ea_paged* pg, int64_t n, PageMap* pm);
 

@@ -331,7 +331,7 @@ ea_status check_step(const Dims& d, const ea_step* step, int64_t n) {
   return EA_OK;
 }
 
-AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t max_new, int num_cu) {
+AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t max_new, int num_cu, bool mx) {
   AttendPlan a = {};
   const bool f32 = d.dtype != EA_BF16;
   if (max_new > n_tokens) max_new = n_tokens;
@@ -351,7 +351,7 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   a.rows = !f32 && a.short_rows >= d.G;
   a.tile = f32 || most > a.piece_rows;
   // as many as run at once (but at d = 256 over bf16 rows, whose registers let half of them in at a time)
-  a.shares = a.mt * d.D > 256 ? num_cu : 2 * num_cu;
+  a.shares = a.mt * d.D > 256 ? num_cu : mx && a.mt == 1 && d.D < 256 ? 3 * num_cu : 2 * num_cu;
   if (a.shares > kAttendShares) a.shares = kAttendShares;
   // fp32: wavefronts over rows where those give every CU a workgroup, else over keys (1024 tokens of 2 x 8 KV heads over 2048 rows 655
   // and 690 us, 64 tokens of 2 KV heads 21 and 14)
