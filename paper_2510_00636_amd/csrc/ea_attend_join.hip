@@ -4,13 +4,13 @@
 namespace ea {
 
 // The pieces of every (token, head) row together.  Few rows (WIDE) have a workgroup each, whose 256 threads request all the pieces at
-// once.  Many: D / 4 threads have one row after the other, kJoinRows in all, so that what leads to a row (its sequence, how that was
-// cut) is looked up once and not once a row.  Two pieces each of 22k rows at d = 256: 20 us with two or four rows, 22 with eight, 33
+// once.  Many: D / 4 threads have kJoinRows rows, of which they request two pieces each at a time; what leads to a row (its sequence, how that
+// was cut) is looked up once and not once a row.  Two pieces each of 22k rows at d = 256: 20 us with two or four rows, 22 with eight, 33
 // with sixteen or one; the bytes alone take 13.
 constexpr int kJoinRows = 4;
 template <int D, bool F32, bool WIDE>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
-  constexpr int kLanes = D / 4, kRounds = WIDE ? 8 : 4, kWays = WIDE ? 256 / kLanes : 1, kRows = WIDE ? 1 : kJoinRows, kGroups = 256 / kLanes;
+  constexpr int kLanes = D / 4, kRounds = WIDE ? 8 : 2, kWays = WIDE ? 256 / kLanes : 1, kRows = WIDE ? 1 : kJoinRows, kGroups = 256 / kLanes;
   __shared__ float4 pass[kWays][kLanes];
   __shared__ float2 pass_ml[kWays];
   const int lane = threadIdx.x & 63, c4 = threadIdx.x % kLanes * 4, way = WIDE ? threadIdx.x / kLanes : 0;
@@ -25,65 +25,91 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   int4 cut = ((const int4*)(a.ws + a.plan.cuts))[b];      // its first piece, cuts, keys of a stretch, tiles
   const float* po = (const float*)(a.ws + a.plan.split_o) + c4;
   const float2* part_ml = (const float2*)(a.ws + a.plan.split_ml);
-#pragma unroll 1
-  for (int nth = 0; nth < kRows; ++nth) {
-    const uint32_t at = at0 + nth * kGroups;
+  // where a row's pieces stand: how many (-1: none of this launch's rows), the first one's slot
+  auto find = [&](uint32_t at, int& unit, int& n) -> long long {
     const int token = (int)(at / hq), head = (int)(at - token * hq), h = head / a.G;
-    if (token >= all) return;
+    n = -1;
+    unit = 0;
+    if (token >= all) return 0;
     if (token >= t0 + m) {
       while (b + 1 < a.B && first_token(a, b + 1) <= token) ++b;
       t0 = first_token(a, b);
       m = first_token(a, b + 1) - t0;
       cut = ((const int4*)(a.ws + a.plan.cuts))[b];
     }
-    if (token < t0 || token >= t0 + m || (a.only_long && m * a.G <= a.short_rows) || cut.y <= 1) continue;
+    if (token < t0 || token >= t0 + m || (a.only_long && m * a.G <= a.short_rows) || cut.y <= 1) return 0;
     const int row = (token - t0) * a.G + (head - h * a.G), tile = row / a.plan.tile_rows;
     const int vis = rows_of(a, b, h) - (a.sees ? 0 : m - 1 - (token - t0));
-    int n = (vis + cut.z - 1) / cut.z;
-    n = n < 1 ? 0 : n > cut.y ? cut.y : n;
+    int k = (vis + cut.z - 1) / cut.z;
+    k = k < 1 ? 0 : k > cut.y ? cut.y : k;
     const int first = cut.x + (cut.w - 1 - tile) * cut.y * a.Hkv + h;
     // (prefix sums that do not ascend can count more pieces than there are: none is looked for outside the workspace)
-    if (cut.y > a.plan.most_pieces || first < 0 || first + (n - 1) * a.Hkv >= a.plan.most_pieces) continue;
-    float top = -__builtin_inff(), sum = 0.0f;
-    float4 acc = make_float4(0, 0, 0, 0);
-    auto take = [&](float2 ml, float4 y) {
-      const float t = fmaxf(top, ml.x), from = t == -__builtin_inff() ? 0.0f : t;
-      const float f = pow2(top - from), w = pow2(ml.x - from);
-      top = t;
-      sum = sum * f + ml.y * w;
-      acc.x = acc.x * f + y.x * w; acc.y = acc.y * f + y.y * w; acc.z = acc.z * f + y.z * w; acc.w = acc.w * f + y.w * w;
-    };
-    for (int i0 = way; i0 < n; i0 += kRounds * kWays) {
-      float2 ml[kRounds];
-      float4 y[kRounds];
+    if (cut.y > a.plan.most_pieces || first < 0 || first + (k - 1) * a.Hkv >= a.plan.most_pieces) return 0;
+    n = k;
+    unit = b * a.Hkv + h;
+    return (long long)first * a.plan.tile_rows + (row - tile * a.plan.tile_rows);
+  };
+  const long long step = (long long)a.Hkv * a.plan.tile_rows;      // from piece to piece of a row
+  long long slot[kRows];
+  int unit[kRows], n[kRows], most = 0;
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    slot[r] = find(at0 + r * kGroups, unit[r], n[r]);
+    most = max(most, n[r]);
+  }
+  float top[kRows], sum[kRows];
+  float4 acc[kRows];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    top[r] = -__builtin_inff();
+    sum[r] = 0.0f;
+    acc[r] = make_float4(0, 0, 0, 0);
+  }
+  auto take = [&](int r, float2 ml, float4 y) {
+    const float t = fmaxf(top[r], ml.x), from = t == -__builtin_inff() ? 0.0f : t;
+    const float f = pow2(top[r] - from), w = pow2(ml.x - from);
+    top[r] = t;
+    sum[r] = sum[r] * f + ml.y * w;
+    acc[r].x = acc[r].x * f + y.x * w; acc[r].y = acc[r].y * f + y.y * w; acc[r].z = acc[r].z * f + y.z * w; acc[r].w = acc[r].w * f + y.w * w;
+  };
+  for (int i0 = way; i0 < most; i0 += kRounds * kWays) {
+    float2 ml[kRows][kRounds];
+    float4 y[kRows][kRounds];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
 #pragma unroll
       for (int k = 0; k < kRounds; ++k) {
-        const int i = i0 + k * kWays;
-        if (i >= n) break;
-        const long long slot = (long long)(first + i * a.Hkv) * a.plan.tile_rows + (row - tile * a.plan.tile_rows);
-        ml[k] = part_ml[slot];
-        y[k] = *(const float4*)(po + slot * D);
+        const int i = min(i0 + k * kWays, n[r] - 1);          // (one that is there, asked for once more, if the row has no such piece)
+        const long long at = n[r] > 0 ? slot[r] + i * step : 0;
+        ml[r][k] = part_ml[at];
+        y[r][k] = *(const float4*)(po + at * D);
       }
 #pragma unroll
-      for (int k = 0; k < kRounds; ++k)
-        if (i0 + k * kWays < n) take(ml[k], y[k]);
-    }
-    if constexpr (WIDE) {
-      if (c4 == 0) pass_ml[way] = make_float2(top, sum);
-      pass[way][c4 / 4] = acc;
-      __syncthreads();
-      if (way != 0) return;
+    for (int r = 0; r < kRows; ++r)
 #pragma unroll
-      for (int w = 1; w < kWays; ++w) take(pass_ml[w], pass[w][c4 / 4]);
-    }
-    const bool any = sum > 0.0f || sum != sum;
-    const float f = (a.vscale ? a.vscale[b * a.Hkv + h] : 1.0f) / sum;
-    const size_t to = (size_t)at * D + c4;
+      for (int k = 0; k < kRounds; ++k)
+        if (i0 + k * kWays < n[r]) take(r, ml[r][k], y[r][k]);
+  }
+  if constexpr (WIDE) {
+    if (n[0] < 0) return;
+    if (c4 == 0) pass_ml[way] = make_float2(top[0], sum[0]);
+    pass[way][c4 / 4] = acc[0];
+    __syncthreads();
+    if (way != 0) return;
+#pragma unroll
+    for (int w = 1; w < kWays; ++w) take(0, pass_ml[w], pass[w][c4 / 4]);
+  }
+#pragma unroll
+  for (int r = 0; r < kRows; ++r) {
+    if (n[r] < 0) continue;
+    const bool any = sum[r] > 0.0f || sum[r] != sum[r];
+    const float f = (a.vscale ? a.vscale[unit[r]] : 1.0f) / sum[r];
+    const size_t row = at0 + r * kGroups, to = row * D + c4;
     if (F32)
-      *(float4*)((float*)a.out + to) = any ? make_float4(acc.x * f, acc.y * f, acc.z * f, acc.w * f) : make_float4(0, 0, 0, 0);
+      *(float4*)((float*)a.out + to) = any ? make_float4(acc[r].x * f, acc[r].y * f, acc[r].z * f, acc[r].w * f) : make_float4(0, 0, 0, 0);
     else
-      *(uint2*)((__bf16*)a.out + to) = any ? make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f)) : make_uint2(0u, 0u);
-    if (a.lse && c4 == 0) a.lse[at] = natural_lse(top, sum);
+      *(uint2*)((__bf16*)a.out + to) = any ? make_uint2(pack_bf16(acc[r].x * f, acc[r].y * f), pack_bf16(acc[r].z * f, acc[r].w * f)) : make_uint2(0u, 0u);
+    if (a.lse && c4 == 0) a.lse[row] = natural_lse(top[r], sum[r]);
   }
 }
 

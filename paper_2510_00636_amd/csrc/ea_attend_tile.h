@@ -160,19 +160,11 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
   const int vis_min = tree ? new_rows : len - (m - 1 - (row0 + wave * 32) / a.G);      // of the wavefront's rows
   constexpr int kWords = EA_TREE_MAX / 64;
   __shared__ uint64_t see[TREE ? kWords : 1][TREE ? kM : 1];         // of the new rows, by the workgroup's rows
-  if constexpr (TREE)
-    if (tree && hi == 0)
-#pragma unroll
-      for (int w = 0; w < kWords; ++w) {
-        const int left = m - 64 * w;
-        uint64_t x = in && w < a.words ? a.sees[(long long)(t0 + tok) * a.words + w] : 0;
-        see[w][wave * 32 + n32] = left >= 64 ? x : left > 0 ? x & ((1ull << left) - 1) : 0;
-      }
   // (a scale's sign goes to the queries, so that logits order like their products, and a scale of zero leaves masked ones -inf; so
   // does a scale that is not a number, which goes to the queries, too)
   const float scale = R == kRowsFp8 && a.kscale ? a.kscale[unit] : 1.0f, qk = a.scale * fmaxf(fabsf(scale), 1e-30f);
   bf16x8 q[kSteps];
-  {
+  auto load_q = [&]() {
     const __bf16* src = (const __bf16*)a.q + (long long)(t0 + (in ? tok : 0)) * a.q_stride + (h * a.G + (in ? hd : 0)) * D;
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
@@ -182,6 +174,22 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
       if (R == kRowsFp8 && scale != scale) w = (bf16x8)(__bf16)scale;
       q[s] = w;
     }
+  };
+  auto load_masks = [&]() {
+    if (TREE && tree && hi == 0)
+#pragma unroll
+      for (int w = 0; w < (TREE ? kWords : 0); ++w) {
+        const int left = m - 64 * w;
+        const uint64_t x = in && w < a.words ? a.sees[(long long)(t0 + tok) * a.words + w] : 0;
+        see[w][wave * 32 + n32] = left >= 64 ? x : left > 0 ? x & ((1ull << left) - 1) : 0;
+      }
+  };
+  // With masks, where there are few tiles, queries and masks are asked for behind the first tile, so that what leads to it does not wait for
+  // them (d = 256 has no registers for that).
+  constexpr bool kLate = TREE && D < 256;
+  if constexpr (!kLate) {
+    load_q();
+    load_masks();
   }
 
   // ---- loads of a tile: pass i of wavefront w covers rows (NW i + w) kPer .., which lie in one block.  Rows behind the last one are
@@ -299,6 +307,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
     }
     make_places(key_lo + kFirst * kN);
     look_up(key_lo + (kFirst + 1) * kN);
+    if constexpr (kLate) {
+      load_q();
+      load_masks();
+    }
     if constexpr (FP8) {
       stage(0);
       request(1);
@@ -316,6 +328,13 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
 #pragma unroll
   for (int c = 0; c < kVWays; ++c)
     v_at[c] = kKBytes + v_row * kVPitch + ((c * 4) ^ (FP8 ? 0 : v_piece<D>(v_row))) * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+  // (a register each, whatever they were made of)
+  if constexpr (kAgain) {
+#pragma unroll
+    for (int c = 0; c < kKWays; ++c) asm volatile("" : "+v"(k_at[c]));
+#pragma unroll
+    for (int c = 0; c < kVWays; ++c) asm volatile("" : "+v"(v_at[c]));
+  }
   int buf = 0;
   for (int key = key_lo; key < key_hi; key += kN, buf = buf + 1 < kStages ? buf + 1 : 0) {
     const char* kt = lds + buf * kBuffer;
