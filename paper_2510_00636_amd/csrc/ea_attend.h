@@ -34,6 +34,7 @@ struct AttendArgs {
   int mx;                         // bits of an element of such pools, 0: others
   const uint64_t* sees;           // trees: which of its sequence's new rows a token sees, `words` words each; null: those up to its own
   int words;
+  int by_head;                    // stretches are cut along the keys head by head (trees over caches with a length per head)
   AttendPlan plan;
 };
 
@@ -112,19 +113,21 @@ __device__ __forceinline__ int ceil_div(int x, int by) {      // x < 2^24, both 
   if ((k + 1) * by <= x + by - 1) ++k;
   return k;
 }
-template <int ROWS>
-__device__ __forceinline__ Piece find_piece(const AttendArgs& a, int index) {
+// WAVES > 1: that many wavefronts, the workgroup's, share out the sequences between them, their sums through LDS (24 sequences: 4.2 us of a piece's time -> 2.8).
+// HEADS: with a.by_head what is cut is a head, not a sequence whose heads have lengths of their own.
+template <int ROWS, int WAVES = 1, bool HEADS = false>
+__device__ __forceinline__ Piece find_piece(const AttendArgs& a, int index, float (*sums)[3][64] = nullptr) {
   const int lane = threadIdx.x & 63;
+  const bool by_head = HEADS && a.by_head;
+  const int supers = by_head ? a.B * a.Hkv : a.B, heads = by_head ? 1 : a.Hkv;      // that are cut each for itself, and heads of one
   auto look = [&](int b, int& tiles, int& steps) {
-    tiles = steps = 0;
-    if (b >= a.B) return;
-    const int rows = (first_token(a, b + 1) - first_token(a, b)) * a.G;
-    if (rows < 1 || (a.only_long && rows <= a.short_rows)) return;
-    tiles = (rows + ROWS - 1) / ROWS;
-    int len = rows_of(a, b, 0);
-    if (a.per_head)
-      for (int h = 1; h < a.Hkv; ++h) len = max(len, rows_of(a, b, h));
-    steps = len > 0 ? (len + 63) >> 6 : 1;
+    const int su = min(b, supers - 1), at = by_head ? su / a.Hkv : su, rows = b < supers ? (first_token(a, at + 1) - first_token(a, at)) * a.G : 0;
+    int len = rows_of(a, at, by_head ? su - at * a.Hkv : 0);
+    if (a.per_head && !by_head)
+      for (int h = 1; h < a.Hkv; ++h) len = max(len, rows_of(a, at, h));
+    const bool none = rows < 1 || (a.only_long && rows <= a.short_rows);
+    tiles = none ? 0 : (rows + ROWS - 1) / ROWS;
+    steps = none ? 0 : len > 0 ? (len + 63) >> 6 : 1;
   };
   int tiles, steps;
   look(lane, tiles, steps);
@@ -132,21 +135,38 @@ __device__ __forceinline__ Piece find_piece(const AttendArgs& a, int index) {
   int q = 1 << 24;              // most steps of a piece
   if (a.plan.most_pieces > 0) {
     int most = (int)wave_max((float)steps);
-    for (int base = 64; base < a.B; base += 64) {
+    for (int base = 64; base < supers; base += 64) {
       look(base + lane, tiles, steps);
       most = max(most, (int)wave_max((float)steps));
     }
     q = max(ceil_div(most, lane + 1), min(kLeastSteps, most));
     float pieces = 0.0f, cut = 0.0f, work = 0.0f;
-    for (int base = 0; base < a.B; base += 64) {
+    for (int base = 0; base < supers; base += 64) {
       if (base > 0) look(base + lane, tiles, steps); else tiles = tiles0, steps = steps0;
-      for (uint64_t left = __ballot(tiles > 0); left; left &= left - 1) {
-        const int l = __builtin_ctzll(left), n = __builtin_amdgcn_readlane(tiles, l) * a.Hkv, each = __builtin_amdgcn_readlane(steps, l);
+      uint64_t left = __ballot(tiles > 0);
+      if constexpr (WAVES > 1) left &= (~0ull / ((1ull << WAVES) - 1)) << (threadIdx.x >> 6);      // every WAVES-th
+      for (; left; left &= left - 1) {
+        const int l = __builtin_ctzll(left), n = __builtin_amdgcn_readlane(tiles, l) * heads, each = __builtin_amdgcn_readlane(steps, l);
         const int k = ceil_div(each, q);
         pieces += (float)(n * k);
         cut += k > 1 ? (float)(n * k) : 0.0f;
         work += (float)n * (float)each;
       }
+    }
+    if constexpr (WAVES > 1) {
+      const int wave = threadIdx.x >> 6;
+      sums[wave][0][lane] = pieces;
+      sums[wave][1][lane] = cut;
+      sums[wave][2][lane] = work;
+      __syncthreads();
+      pieces = cut = work = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        pieces += sums[w][0][lane];
+        cut += sums[w][1][lane];
+        work += sums[w][2][lane];
+      }
+      __syncthreads();      // what else stands there may be written again
     }
     // one round: its longest piece.  More: the work shared out, with a quarter of a piece at the end, but whole rounds where all
     // pieces are alike
@@ -164,24 +184,24 @@ __device__ __forceinline__ Piece find_piece(const AttendArgs& a, int index) {
   p.tile = -1;
   int have = 0;
   // sequences of long pieces first, so that short ones fill up the end
-  const int blocks = (a.B + 63) >> 6;
+  const int blocks = (supers + 63) >> 6;
   for (int turn = 0; turn < 2 * blocks; ++turn) {
     const int base = (turn >= blocks ? turn - blocks : turn) * 64;
     if (blocks > 1) look(base + lane, tiles, steps); else tiles = tiles0, steps = steps0;
     const int cuts = ceil_div(steps, q);
     if ((2 * ceil_div(steps, max(cuts, 1)) >= min(q, kLongSteps)) != (turn < blocks)) tiles = 0;
-    const int mine = tiles * cuts * a.Hkv, pre = wave_prefix(mine);
+    const int mine = tiles * cuts * heads, pre = wave_prefix(mine);
     const uint64_t in = __ballot(have + pre > index);
     if (in) {
       const int l = __builtin_ctzll(in);
-      p.b = base + l;
+      p.b = by_head ? (base + l) / a.Hkv : base + l;
       p.tiles = __builtin_amdgcn_readlane(tiles, l);
       p.nsplit = __builtin_amdgcn_readlane(cuts, l);
       p.chunk = ceil_div(__builtin_amdgcn_readlane(steps, l), p.nsplit) * 64;
       const int at = index - have - (__builtin_amdgcn_readlane(pre, l) - __builtin_amdgcn_readlane(mine, l));
       // heads next to each other (they run on different dies), the last tiles, which see most keys, first
-      p.h = at % a.Hkv;
-      const int rest = at / a.Hkv;
+      p.h = by_head ? base + l - p.b * a.Hkv : at % a.Hkv;
+      const int rest = at / heads;
       p.split = rest % p.nsplit;
       p.tile = p.tiles - 1 - rest / p.nsplit;
       p.first = at == 0;
@@ -194,8 +214,9 @@ __device__ __forceinline__ Piece find_piece(const AttendArgs& a, int index) {
   return p;
 }
 // where the rows of a piece's partial result stand, and what the joining launch needs to find them
+template <bool HEADS = false>
 __device__ __forceinline__ void note_cuts(const AttendArgs& a, const Piece& p, int index) {
-  if (a.plan.most_pieces > 0 && p.first && threadIdx.x == 0) ((int4*)(a.ws + a.plan.cuts))[p.b] = make_int4(index, p.nsplit, p.chunk, p.tiles);
+  if (a.plan.most_pieces > 0 && p.first && threadIdx.x == 0) ((int4*)(a.ws + a.plan.cuts))[HEADS && a.by_head ? p.b * a.Hkv + p.h : p.b] = make_int4(index, p.nsplit, p.chunk, p.tiles);
 }
 
 // ---- Values that a row does not see.  Behind the last cached row they are taken for zeros; but a step's own rows are seen by some of

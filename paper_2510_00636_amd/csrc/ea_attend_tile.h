@@ -125,9 +125,12 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n32 = lane & 31, hi = lane >> 5;
 
-  const Piece piece = find_piece<kM>(a, blockIdx.x);
+  constexpr int kWords = EA_TREE_MAX / 64;
+  __shared__ uint64_t see[TREE ? kWords : 1][TREE ? kM : 1];         // which of the new rows the workgroup's rows see
+  static_assert(!TREE || sizeof(see) >= sizeof(float[NW][3][64]), "the pieces' sums stand there first");
+  const Piece piece = find_piece<kM, TREE ? NW : 1, TREE>(a, blockIdx.x, (float(*)[3][64])see);
   if (piece.tile < 0) return;
-  note_cuts(a, piece, blockIdx.x);
+  note_cuts<TREE>(a, piece, blockIdx.x);
   const int b = piece.b, h = piece.h, t0 = piece.t0, m = piece.m, rows = m * a.G, row0 = piece.tile * kM;
   const int len = __builtin_amdgcn_readfirstlane(rows_of(a, b, h));
   const int last_row = min(row0 + kM, rows) - 1;
@@ -158,8 +161,6 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
     return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, (uint32_t)none));
   };
   const int vis_min = tree ? new_rows : len - (m - 1 - (row0 + wave * 32) / a.G);      // of the wavefront's rows
-  constexpr int kWords = EA_TREE_MAX / 64;
-  __shared__ uint64_t see[TREE ? kWords : 1][TREE ? kM : 1];         // of the new rows, by the workgroup's rows
   // (a scale's sign goes to the queries, so that logits order like their products, and a scale of zero leaves masked ones -inf; so
   // does a scale that is not a number, which goes to the queries, too)
   const float scale = R == kRowsFp8 && a.kscale ? a.kscale[unit] : 1.0f, qk = a.scale * fmaxf(fabsf(scale), 1e-30f);

@@ -384,7 +384,7 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   }
   if (a.tile && a.most_pieces > 0) {
     const size_t rows = (size_t)a.most_pieces * a.tile_rows;
-    a.cuts = take((size_t)d.B * 4 * sizeof(int32_t));
+    a.cuts = take((size_t)d.units() * 4 * sizeof(int32_t));      // (of sequences, or of heads)
     a.split_o = take(rows * d.D * sizeof(float));
     a.split_ml = take(rows * 2 * sizeof(float));
   }

@@ -12,6 +12,7 @@ static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return na && nb && x < y + nb && y < x + na;
 }
+constexpr int kCutHeads = 256;     // most heads of a call that are cut each for itself
 constexpr int kPlanCus = 256;      // a plan, and with it the size of its workspace, is the same wherever it is made
 
 hipError_t launch_attend(const AttendArgs& a, const Dims& d, hipStream_t st) {
@@ -101,6 +102,8 @@ static ea_status attend(const Dims& d, const void* q, const ea_step* step, const
   // their two launches cost more than they save: 16 sequences over 1024 rows, a third adding 60 tokens and the others one, 8 bits 50
   // -> 45 us, bf16 53 -> 40; over 4096 87 and 95, 99 and 92, over 16k 206 and 272, 250 and 280.  24 trees of 32 tokens 75 -> 66.
   if (tree && a.plan.tile && (d.B == 1 || n <= 2048 || step->n_tokens == d.B * step->max_new)) a.plan.rows = 0;
+  // (every workgroup looks at all that is cut)
+  a.by_head = tree && per_head && d.units() <= kCutHeads;
   a.only_long = a.plan.rows;
   a.short_rows = a.plan.short_rows;
   a.scale = (float)(1.4426950408889634074 / (d.D == 64 ? 8.0 : d.D == 256 ? 16.0 : 11.313708498984760390));
