@@ -146,12 +146,16 @@ template <int D, Rows R, int MT> constexpr int rows_groups() {
 
 // TREE: what a token sees of its sequence's new rows (no more than 64 of them, or the sequence is not this kernel's) is a mask of them, its own or
 // the chain's; else a number of rows.
-// U: a wavefront works on 32 U keys at a time and has as many on their way.
-template <int D, Rows R, int MT, bool TREE, int U>
+template <int D, Rows R, int MT, bool TREE>
 __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(AttendArgs a) {
   using S = RowShape<D, R>;
-  constexpr int kKeys = 32 * U, kSubs = 2 * U, kStride = 4 * kKeys;      // of a tile: keys, 16 rows at a time; from tile to tile of a wavefront
+  constexpr int kKeys = 32, kSubs = 2, kStride = 4 * kKeys;      // of a tile: keys, 16 rows at a time; from tile to tile of a wavefront
   constexpr bool kHeadScale = R == kRowsFp8;
+  // What a head costs besides its groups, in groups: shares are equal in both, or one of four short heads is done when the others have long
+  // been.  48 sequences of 17 .. 4419 rows of 8 bits: none 30.8 us, one group 24.6, two 25.0 (16-bit rows, 8 tokens each: 66.5, 54.5, 54.2;
+  // d = 256, 8 bits: 46.4, 40.3, 42.1); 8 sequences of 4608 rows 21.8, 22.7, 22.7.
+  constexpr int kLead = TREE ? 1 : 0;
+  auto units_of = [](int grp) { return grp > 0 ? grp + kLead : 0; };
   constexpr int kM = 16 * MT, kPitch = D + 4;
   extern __shared__ __attribute__((aligned(16))) float lds[];
   float* pass_o = lds;
@@ -163,8 +167,8 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
 
   // ---- the share: total of all groups, then the super-unit in which this workgroup's begins.  A lane holds one of 64 of them.
   Super mine = super_unit(a, lane, supers);
-  int pre = wave_prefix(mine.grp), total = last_lane(pre), block = 0;
-  for (int base = 64; base < supers; base += 64) total += last_lane(wave_prefix(super_unit(a, base + lane, supers).grp));
+  int pre = wave_prefix(units_of(mine.grp)), total = last_lane(pre), block = 0;
+  for (int base = 64; base < supers; base += 64) total += last_lane(wave_prefix(units_of(super_unit(a, base + lane, supers).grp)));
   const long long all = (long long)total * mult, wgs = all < gridDim.x ? all : gridDim.x;
   // for the joining launch, of a head that begins here: the head, this workgroup, and to how many the head falls from here on; by
   // heads, or by workgroups, in which no more than one head goes on behind the end (-1: none does)
@@ -184,7 +188,8 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
   struct Part {
     int su, have;             // super-unit, groups in front of it
     int grp, t0, m, len;      // its groups, first token, tokens, rows
-    int b, h, off, take;      // sequence, KV head, first group of the part and how many
+    int b, h, off, take;      // sequence, KV head, first group of the part and how many (none: the share ends in front of them)
+    int lead;                 // of what the head costs besides, how much lies in the share
   };
   long long x = x0;
   auto fill = [&](Part& c) {
@@ -193,9 +198,11 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
     c.t0 = from_lane(mine.t0, l);
     c.m = from_lane(mine.m, l);
     c.len = from_lane(mine.len, l);
-    const int rel = (int)(x - (long long)c.have * mult), hh = a.per_head ? 0 : rel / c.grp;
-    c.off = rel - hh * c.grp;
-    c.take = (int)(x1 - x < c.grp - c.off ? x1 - x : c.grp - c.off);
+    const int rel = (int)(x - (long long)c.have * mult), hh = a.per_head ? 0 : rel / (c.grp + kLead);
+    c.off = rel - hh * (c.grp + kLead) - kLead;
+    c.lead = c.off < 0 ? -c.off : 0;
+    c.off = c.off < 0 ? 0 : c.off;
+    c.take = (int)(x1 - x - c.lead < c.grp - c.off ? x1 - x - c.lead : c.grp - c.off);
     c.b = a.per_head ? c.su / a.Hkv : c.su;
     c.h = a.per_head ? c.su - c.b * a.Hkv : hh;
   };
@@ -207,16 +214,17 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
     if (in) {
       const int l = __builtin_ctzll(in);
       cur.su = block + l;
-      cur.have += from_lane(pre, l) - from_lane(mine.grp, l);
+      cur.have += from_lane(pre, l) - units_of(from_lane(mine.grp, l));
       break;
     }
     cur.have += last_lane(pre);
     block += 64;
     if (block >= supers) return nothing();
     mine = super_unit(a, block + lane, supers);
-    pre = wave_prefix(mine.grp);
+    pre = wave_prefix(units_of(mine.grp));
   }
   fill(cur);
+  if (kLead > 0 && cur.take <= 0) return nothing();
 
   // ---- What is in flight: always a tile of K and behind it a tile of V, of this part or, at its end, of the next one; the next part's
   // queries in front of them.  Loads are waited for in order, and the compiler counts what may be on its way behind the one that it
@@ -371,15 +379,15 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
   __syncthreads();
 
   for (int parity = 0;; parity ^= 1) {
-    x += cur.take;
+    x += cur.lead + cur.take;
     // ---- the part behind this one, and the entries of its blocks
     Part next = cur;
     Blocks first = {}, following_blocks = {};
     if (cur.take * kGroup > kStride) following_blocks = look_up(cur, cur.off * kGroup + kStride + wave * kKeys);
     bool go_on = x < x1;
     if (go_on) {
-      if (x >= (long long)(cur.have + cur.grp) * mult) {      // the next super-unit that has groups
-        next.have += cur.grp;
+      if (x >= (long long)(cur.have + units_of(cur.grp)) * mult) {      // the next super-unit that has groups
+        next.have += units_of(cur.grp);
         ++next.su;
         for (;;) {
           const uint64_t some = next.su - block < 64 ? __ballot(mine.grp > 0) >> (next.su - block) : 0;
@@ -396,7 +404,8 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
       }
       if (go_on) {
         fill(next);
-        first = look_up(next, next.off * kGroup + wave * kKeys);
+        if (kLead > 0 && next.take <= 0) go_on = false;
+        else first = look_up(next, next.off * kGroup + wave * kKeys);
       }
     }
     const int rows = cur.m * a.G, unit = cur.b * a.Hkv + cur.h, len = cur.len;
@@ -468,7 +477,7 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
       // A weight reaches the second product as two bf16 numbers, which together are as good as fp32 next to the values' eight
       // bits: the matrix cores have time for it here.
       const bool ragged = row + kKeys > some;
-      uint32_t p[MT][4 * U], plo[MT][4 * U];
+      uint32_t p[MT][4], plo[MT][4];
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
 #pragma unroll
@@ -478,13 +487,11 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
             // bit i: key row + i is seen (row + kKeys > new_rows)
             const Mask mask = see[wave][t * 16 + n16];
             const int from = row - new_rows;
-            using Bits = std::conditional_t<U == 1, uint32_t, uint64_t>;
-            constexpr int kLast = 8 * sizeof(Bits) - 1;
-            const Bits bits = from >= kMaskBits ? 0 : from >= 0 ? (Bits)(mask >> (from & (kMaskBits - 1)))
-                                                                : (Bits)mask << (-from & kLast) | (((Bits)1 << (-from & kLast)) - 1);
+            const uint32_t bits = from >= kMaskBits ? 0 : from >= 0 ? (uint32_t)(mask >> (from & (kMaskBits - 1)))
+                                                                    : (uint32_t)mask << (-from & 31) | ((1u << (-from & 31)) - 1);
 #pragma unroll
             for (int i = 0; i < kSubs; ++i) {
-              const uint32_t mine = (uint32_t)(bits >> 16 * i) >> 4 * g;
+              const uint32_t mine = bits >> 16 * i >> 4 * g;
 #pragma unroll
               for (int r = 0; r < 4; ++r) s[t][i][r] = mine >> r & 1 ? s[t][i][r] : -__builtin_inff();
             }
@@ -507,72 +514,70 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
         }
         const float from = subtrahend(mx[t]);
 #pragma unroll
-        for (int i = 0; i < 4 * U; ++i) {
+        for (int i = 0; i < 4; ++i) {
           const float lo = pow2(s[t][i >> 1][(i & 1) * 2] - from), hi = pow2(s[t][i >> 1][(i & 1) * 2 + 1] - from);
           l[t] += lo + hi;
           p[t][i] = pack_bf16(lo, hi);
           plo[t][i] = pack_bf16(lo - __uint_as_float(p[t][i] << 16), hi - __uint_as_float(p[t][i] & 0xffff0000u));
         }
       }
-      // ---- O^T, 32 keys at a time
+      // ---- O^T
 #pragma unroll
-      for (int half = 0; half < U; ++half)
+      for (int u = 0; u < S::kLoads; ++u) {
+        // MX: a pair of channels is widened where it is needed (all of them at once take 64 registers at d = 256), so what is not finite goes
+        // in front of that
+        uint32_t w[8][S::kMx ? 1 : S::kCpl / 2];
+        float scale[8];
+        if constexpr (S::kMx) {
+          uint32_t e[8];
 #pragma unroll
-        for (int u = 0; u < S::kLoads; ++u) {
-          // MX: a pair of channels is widened where it is needed (all of them at once take 64 registers at d = 256), so what is not finite goes
-          // in front of that
-          uint32_t w[8][S::kMx ? 1 : S::kCpl / 2];
-          float scale[8];
-          if constexpr (S::kMx) {
-            uint32_t e[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = value_scale(8 * half + j);
-            if (ragged) {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const int key = row + half * 32 + (j >> 2) * 16 + 4 * g + (j & 3);
-                const bool none = key >= some && e[j] == 255;
-                any_bad |= none && key < len;
-                e[j] = none ? 0 : e[j];
-#pragma unroll
-                for (int i = 0; i < (int)(sizeof(Raw<kPiece>) / 4); ++i) {
-                  bool bad_element = false;
-                  const uint32_t x = vraw[8 * half + j][u].w[i], y = finite_elements<R>(x, bad_element);
-                  any_bad |= bad_element && key >= some;
-                  vraw[8 * half + j][u].w[i] = none ? 0 : key >= some ? y : x;
-                }
-              }
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) scale[j] = mx_scale(e[j]);
-          } else {
+          for (int j = 0; j < 8; ++j) e[j] = value_scale(j);
+          if (ragged) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              widen_piece<D, R>(vraw[8 * half + j][u], w[j]);
-              if ((TREE || cur.m > 1) && ragged && row + half * 32 + (j >> 2) * 16 + 4 * g + (j & 3) >= some)
+              const int key = row + (j >> 2) * 16 + 4 * g + (j & 3);
+              const bool none = key >= some && e[j] == 255;
+              any_bad |= none && key < len;
+              e[j] = none ? 0 : e[j];
 #pragma unroll
-                for (int c = 0; c < S::kCpl / 2; ++c) w[j][c] = finite_pair(w[j][c], any_bad);
+              for (int i = 0; i < (int)(sizeof(Raw<kPiece>) / 4); ++i) {
+                bool bad_element = false;
+                const uint32_t x = vraw[j][u].w[i], y = finite_elements<R>(x, bad_element);
+                any_bad |= bad_element && key >= some;
+                vraw[j][u].w[i] = none ? 0 : key >= some ? y : x;
+              }
             }
           }
 #pragma unroll
-          for (int c = 0; c < S::kCpl; ++c) {
-            const uint32_t sel = c & 1 ? 0x07060302u : 0x05040100u;
-            const int at = S::kMx ? 0 : c >> 1;
-            if constexpr (S::kMx)
-              if (c % 2 == 0)
+          for (int j = 0; j < 8; ++j) scale[j] = mx_scale(e[j]);
+        } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w[j][0] = mx_pair<R>(vraw[8 * half + j][u].w, c >> 1, scale[j]);
-            const uint4 v = make_uint4(__builtin_amdgcn_perm(w[1][at], w[0][at], sel), __builtin_amdgcn_perm(w[3][at], w[2][at], sel),
-                                       __builtin_amdgcn_perm(w[5][at], w[4][at], sel), __builtin_amdgcn_perm(w[7][at], w[6][at], sel));
+          for (int j = 0; j < 8; ++j) {
+            widen_piece<D, R>(vraw[j][u], w[j]);
+            if ((TREE || cur.m > 1) && ragged && row + (j >> 2) * 16 + 4 * g + (j & 3) >= some)
 #pragma unroll
-            for (int t = 0; t < MT; ++t) {
-              f32x4& acc = o[t][u * S::kCpl + c];
-              const uint32_t *hi = &p[t][4 * half], *lo = &plo[t][4 * half];
-              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), acc, 0, 0, 0);
-              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), acc, 0, 0, 0);
-            }
+              for (int c = 0; c < S::kCpl / 2; ++c) w[j][c] = finite_pair(w[j][c], any_bad);
           }
         }
+#pragma unroll
+        for (int c = 0; c < S::kCpl; ++c) {
+          const uint32_t sel = c & 1 ? 0x07060302u : 0x05040100u;
+          const int at = S::kMx ? 0 : c >> 1;
+          if constexpr (S::kMx)
+            if (c % 2 == 0)
+#pragma unroll
+              for (int j = 0; j < 8; ++j) w[j][0] = mx_pair<R>(vraw[j][u].w, c >> 1, scale[j]);
+          const uint4 v = make_uint4(__builtin_amdgcn_perm(w[1][at], w[0][at], sel), __builtin_amdgcn_perm(w[3][at], w[2][at], sel),
+                                     __builtin_amdgcn_perm(w[5][at], w[4][at], sel), __builtin_amdgcn_perm(w[7][at], w[6][at], sel));
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            f32x4& acc = o[t][u * S::kCpl + c];
+            const uint32_t *hi = p[t], *lo = plo[t];
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3])), acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3])), acc, 0, 0, 0);
+          }
+        }
+      }
       load_v();
       __builtin_amdgcn_sched_barrier(0);
       row = following;
@@ -649,17 +654,13 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
   }
 }
 
-// Keys of a tile: 64 for single tokens over MX rows, so that a wavefront has as many bytes on their way as over wider ones, and half as
-// many tiles to see to.
-template <int D, Rows R, int MT> constexpr int tile_halves() { return (R == kRowsMx8 || R == kRowsMx4) && MT == 1 && D < 0 ? 2 : 1; }
 template <int D, Rows R, int MT, bool TREE>
 static hipError_t rows_of_height(const AttendArgs& a, hipStream_t st) {
-  constexpr int U = tile_halves<D, R, MT>();
   static LdsOptIn opt;
   const size_t bytes = rows_lds_floats<D, MT>() * sizeof(float);
-  const hipError_t e = opt.ensure((const void*)k_attend_rows<D, R, MT, TREE, U>, bytes);
+  const hipError_t e = opt.ensure((const void*)k_attend_rows<D, R, MT, TREE>, bytes);
   if (e != hipSuccess) return e;
-  k_attend_rows<D, R, MT, TREE, U><<<a.plan.shares, 256, bytes, st>>>(a);
+  k_attend_rows<D, R, MT, TREE><<<a.plan.shares, 256, bytes, st>>>(a);
   const hipError_t e2 = hipGetLastError();
   return e2 != hipSuccess ? e2 : launch_attend_rows_join(a, st);
 }
