@@ -54,7 +54,7 @@ typedef enum {
 typedef enum {
   EA_F32 = 0,
   EA_BF16 = 1,
-  EA_FP8_E4M3 = 2 /* rows of d bytes: accepted by ea_compact and ea_compact_unordered only (see ea_score_fp8) */
+  EA_FP8_E4M3 = 2 /* rows of d bytes: accepted by ea_compact, ea_compact_unordered and ea_keep_path only (see ea_score_fp8) */
 } ea_dtype;
 
 typedef struct {
@@ -396,9 +396,10 @@ ea_status ea_attend_fp8(const ea_params* p, const void* q, const ea_step* step, 
  * share a power of two that is made from the row itself when it is stored; no scale has to be known in advance.
  *   k, v              [num_blocks, Hkv, block_size, d] elements: e4m3 bytes (EA_MXFP8), or e2m1 (EA_MXFP4), two to a byte, the even
  *                     channel in its low half
- *   k_scale, v_scale  [num_blocks, Hkv, block_size, d / 32] bytes e; channel c of a row is element * 2^(e - 127) (exact in bf16 from 2^-126 on), and
- *                     NaN where e is 255.
- * All are DEVICE pointers, 16-byte aligned, and apart from each other.  p->dtype is the type of the model's own rows and must be EA_BF16; head_dim 64, 128 or 256. */
+ *   k_scale, v_scale  [num_blocks, Hkv, block_size, d / 32] bytes e; channel c of a row is element * 2^(e - 127) (exact in bf16 from
+ *                     2^-126 on), and NaN where e is 255.
+ * All are DEVICE pointers, 16-byte aligned, and apart from each other.  p->dtype is the type of the model's own rows and must be
+ * EA_BF16; head_dim 64, 128 or 256. */
 typedef enum { EA_MXFP8 = 0, EA_MXFP4 = 1 } ea_mx_format;
 typedef struct {
   void* k;
@@ -410,14 +411,15 @@ typedef struct {
 
 /* ea_append_paged into MX pools.  Keys are rotated in fp64 (angles as everywhere), rounded to fp32 as queries are, and quantised:
  * the 32 channels of a group get the least e from 10 on with max|x| <= 448 * 2^(e - 127) (e2m1: 6), elements are rounded to
- * nearest even.  Elements that would read back as more than bf16's largest number are the largest that does not.  A group that has a NaN or an
- * infinity (a rotated channel of 2^128 or more, too) gets e = 255.  Quantising what was read back gives the same values again. */
+ * nearest even.  Elements that would read back as more than bf16's largest number are the largest that does not.  A group that has
+ * a NaN or an infinity (a rotated channel of 2^128 or more, too) gets e = 255.  Quantising what was read back gives the same values
+ * again.  Two tokens with the same slot: the row holds elements and scales of either. */
 ea_status ea_append_mx(const ea_params* p, const ea_new_rows* rows, const int64_t* slots, const ea_mx* mx, const ea_paged* pg,
                        void* q_out, void* stream);
 
 /* Reads back: rows j < lengths[b] (at most n, HOST) of every sequence as bf16 into row j of k_out and v_out [B, Hkv, n_cap, d],
- * exactly (numbers below 2^-126, which ea_append_mx does not write, may be rounded or become zeros); rows from there on are left as they were.  k_out or v_out may be NULL.  What a compress pass scores, for instance.
- * n <= n_cap. */
+ * exactly (numbers below 2^-126, which ea_append_mx does not write, may be rounded or become zeros); rows from there on are left as
+ * they were.  k_out or v_out may be NULL.  What a compress pass scores, for instance.  n <= n_cap. */
 ea_status ea_read_mx(const ea_params* p, const ea_mx* mx, const ea_paged* pg, const int32_t* lengths, int64_t n, int64_t n_cap,
                      void* k_out, void* v_out, void* stream);
 
@@ -430,8 +432,8 @@ ea_status ea_attend_mx(const ea_params* p, const void* q, const ea_step* step, c
  * cache in that order. */
 #define EA_TREE_MAX 256 /* most tokens that a sequence adds */
 typedef struct {
-  uint64_t* sees; /* DEVICE [n_tokens, words], 8-byte aligned: bit j % 64 of word j / 64: the token sees the j-th of its sequence's tokens */
-  int32_t words;  /* 64 * words >= max_new, words <= EA_TREE_MAX / 64                                                          */
+  uint64_t* sees; /* DEVICE [n_tokens, words], 8-byte aligned: bit j % 64 of word j / 64: the token sees the j-th of its sequence's */
+  int32_t words;  /* 64 * words >= max_new, words <= EA_TREE_MAX / 64                                                             */
 } ea_tree;
 
 /* Masks and positions from parents.  parents [n_tokens] int32: of a token the number of its parent among its sequence's tokens; none
@@ -442,11 +444,14 @@ ea_status ea_tree_masks(const ea_params* p, const ea_step* step, const int32_t* 
                         int32_t* pos, void* stream);
 
 /* Attention of such a step: with m tokens of sequence b in the step, token i sees the rows j < len - m of its KV head, and row
- * len - m + j where bit j of its mask is set.  Else ea_attend (bf16 or fp32), ea_attend_paged and ea_attend_mx: empty rows, values
- * that are not finite in rows that a token does not see, workspaces and bounds.  Masks need not come from a tree. */
+ * len - m + j where bit j of its mask is set.  Else as ea_attend (bf16 or fp32), ea_attend_fp8, ea_attend_paged and ea_attend_mx: empty
+ * rows, values that are not finite in rows that a token does not see, workspaces and bounds.  Masks need not come from a tree. */
 ea_status ea_attend_tree(const ea_params* p, const void* q, const ea_step* step, const ea_tree* tree, const void* k, const void* v,
                          const int32_t* lengths, int64_t n, int64_t n_cap, void* out, float* lse, void* ws, size_t ws_bytes,
                          void* stream);
+ea_status ea_attend_tree_fp8(const ea_params* p, const void* q, const ea_step* step, const ea_tree* tree, const void* k8,
+                             const void* v8, const float* k_scale, const float* v_scale, const int32_t* lengths, int64_t n,
+                             int64_t n_cap, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 ea_status ea_attend_tree_paged(const ea_params* p, const void* q, const ea_step* step, const ea_tree* tree, const void* k_pool,
                                const void* v_pool, const ea_paged* pg, const int32_t* lengths, int64_t n, void* out, float* lse,
                                void* ws, size_t ws_bytes, void* stream);
@@ -457,7 +462,7 @@ ea_status ea_attend_tree_mx(const ea_params* p, const void* q, const ea_step* st
 /* The branch that the model confirms.  tokens [n_tokens] int32: what was drafted; target [n_tokens]: what the model answers behind
  * each of them.  A sequence's first token is accepted (it was the last answer); then, again and again, the first of the children
  * of the last accepted one that is what the model answers there.
- *   path [B, max_new] int32: numbers of the accepted tokens, ascending, -1 behind them is NOT written: entries stay as they were
+ *   path [B, max_new] int32: numbers of the accepted tokens, ascending; entries behind them are left as they were
  *   n_path [B] int32: how many; 0 where the sequence adds no token
  *   next [B] int32: the model's answer behind the last one; -1 where there is none
  * Tokens from the EA_TREE_MAX-th or max_new-th on are not looked at. */

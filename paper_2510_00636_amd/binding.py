@@ -139,6 +139,7 @@ def load_library():
                        ("attend_mx", [P, VP, ST, MX, PG, VP, I64, VP, VP, VP, SZ, VP]),
                        ("tree_masks", [P, ST, VP, TR, VP, VP, VP]), ("tree_accept", [P, ST, VP, VP, VP, VP, VP, VP, VP]),
                        ("attend_tree", [P, VP, ST, TR, VP, VP, VP, I64, I64, VP, VP, VP, SZ, VP]),
+                       ("attend_tree_fp8", [P, VP, ST, TR, VP, VP, VP, VP, VP, I64, I64, VP, VP, VP, SZ, VP]),
                        ("attend_tree_paged", [P, VP, ST, TR, VP, VP, PG, VP, I64, VP, VP, VP, SZ, VP]),
                        ("attend_tree_mx", [P, VP, ST, TR, MX, PG, VP, I64, VP, VP, VP, SZ, VP]),
                        ("keep_path", [P, ST, VP, VP, VP, VP, VP, I64, VP, VP]),
@@ -504,6 +505,12 @@ def tree_accept(p, step, tokens, parents, target, path, n_path, next_token, stre
 def attend_tree(p, q, step, tree, k, v, lengths, n, n_cap, out, lse, ws, stream=None):
     _check(load_library().ea_attend_tree(p, _addr(q), step, tree, _addr(k), _addr(v), _addr(lengths), int(n), int(n_cap), _addr(out),
                                          _addr(lse), _addr(ws), _nbytes(ws), _now(stream)), "ea_attend_tree")
+
+
+def attend_tree_fp8(p, q, step, tree, k8, v8, k_scale, v_scale, lengths, n, n_cap, out, lse, ws, stream=None):
+    _check(load_library().ea_attend_tree_fp8(p, _addr(q), step, tree, _addr(k8), _addr(v8), _addr(k_scale), _addr(v_scale),
+                                             _addr(lengths), int(n), int(n_cap), _addr(out), _addr(lse), _addr(ws), _nbytes(ws),
+                                             _now(stream)), "ea_attend_tree_fp8")
 
 
 def attend_tree_paged(p, q, step, tree, k_pool, v_pool, pg, lengths, n, out, lse, ws, stream=None):

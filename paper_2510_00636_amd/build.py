@@ -13,8 +13,10 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libea.so")
 SOURCES = ["ea_host.cpp", "ea_api.hip", "ea_stats.hip", "ea_score.hip", "ea_score_d64.hip", "ea_score_d128.hip", "ea_score_d128b.hip",
            "ea_score_d256.hip", "ea_score_fp8.hip", "ea_score_fp8b.hip", "ea_score_hw.hip", "ea_select.hip",
-           "ea_compact.hip", "ea_baselines.hip", "ea_frontend.hip", "ea_serve.cpp", "ea_step.hip", "ea_attend_rows.hip", "ea_attend_rows_tree.hip", "ea_attend_rows_mx8.hip", "ea_attend_rows_mx4.hip", "ea_attend_rows_join.hip",
-           "ea_attend_tile.hip", "ea_attend_tile_tree.hip", "ea_attend_tile_mx8.hip", "ea_attend_tile_mx4.hip", "ea_attend_f32.hip", "ea_attend_join.hip", "ea_mx.hip", "ea_tree.hip"]
+           "ea_compact.hip", "ea_baselines.hip", "ea_frontend.hip", "ea_serve.cpp", "ea_step.hip", "ea_mx.hip", "ea_tree.hip",
+           "ea_attend_rows.hip", "ea_attend_rows_tree.hip", "ea_attend_rows_mx8.hip", "ea_attend_rows_mx4.hip", "ea_attend_rows_join.hip",
+           "ea_attend_tile.hip", "ea_attend_tile_tree.hip", "ea_attend_tile_mx8.hip", "ea_attend_tile_mx4.hip", "ea_attend_join.hip",
+           "ea_attend_f32.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 instructions are switched off for the device pass (the host pass warns that it
 # does not know the feature; harmless)
@@ -27,10 +29,10 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-mllvm", "-amdgpu-atomic-optimizer-strategy=None",
          "-mllvm", "-amdgpu-mfma-vgpr-form"]
-# The bf16 and 8-bit attention kernels take numbers below 2^-126 for zeros, which makes exp2f the one instruction that it is (else
+# The attention kernels of bf16 and narrower rows take numbers below 2^-126 for zeros, which makes exp2f the one instruction that it is (else
 # six, with the scaling that such results need: 2048 tokens over 34k rows 998 -> 1180 us, of 64 channels 93 -> 117, 16 tokens over
 # 8 x 4096 rows 38 -> 42).  The fp32 kernel does not (2 x 256 tokens over 8192 rows 345 -> 360 us).
-MORE = {f: ["-fgpu-flush-denormals-to-zero"] for f in ("ea_attend_rows.hip", "ea_attend_rows_tree.hip", "ea_attend_rows_mx8.hip", "ea_attend_rows_mx4.hip", "ea_attend_rows_join.hip", "ea_attend_tile.hip", "ea_attend_tile_tree.hip", "ea_attend_tile_mx8.hip", "ea_attend_tile_mx4.hip")}
+MORE = {f: ["-fgpu-flush-denormals-to-zero"] for f in SOURCES if f.startswith(("ea_attend_rows", "ea_attend_tile"))}
 
 
 def _compile(src):

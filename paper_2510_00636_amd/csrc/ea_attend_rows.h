@@ -88,7 +88,7 @@ template <> struct FourScales<256> { uint32_t x[4]; };
 __device__ __forceinline__ uint32_t byte_of(uint32_t lo, int i) { return __builtin_amdgcn_ubfe(lo, i * 8, 8); }
 __device__ __forceinline__ uint32_t byte_of(uint32_t lo, uint32_t hi, int i) { return __builtin_amdgcn_ubfe(i & 4 ? hi : lo, (i & 3) * 8, 8); }
 
-// a loaded piece of V as bf16: all its channels, or (MX) the pair of channels 2 x, 2 x + 1
+// a loaded piece of V as bf16: all its channels, or (narrow rows with masks) the pair of channels 2 x, 2 x + 1
 template <int D, Rows R, int BYTES>
 __device__ __forceinline__ void widen_piece(const Raw<BYTES>& p, uint32_t* o) {
   if constexpr (R == kRowsBf16) {
@@ -104,7 +104,7 @@ __device__ __forceinline__ void widen_piece(const Raw<BYTES>& p, uint32_t* o) {
 }
 template <Rows R>
 __device__ __forceinline__ uint32_t mx_pair(const uint32_t* w, int x, float scale) {
-  if constexpr (R == kRowsMx8) return mx8_pair(w[x >> 1], scale, x & 1);
+  if constexpr (R != kRowsMx4) return mx8_pair(w[x >> 1], scale, x & 1);
   switch (x & 3) {
     case 0: return mx4_pair<0>(w[x >> 2], scale);
     case 1: return mx4_pair<1>(w[x >> 2], scale);
@@ -115,7 +115,7 @@ __device__ __forceinline__ uint32_t mx_pair(const uint32_t* w, int x, float scal
 // a word's elements without those that are not numbers (e4m3's are the bytes of all ones); `any` is set where there was one
 template <Rows R>
 __device__ __forceinline__ uint32_t finite_elements(uint32_t w, bool& any) {
-  if constexpr (R != kRowsMx8) return w;
+  if constexpr (R == kRowsMx4) return w;
   const uint32_t ones = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
   any |= ones != 0;
   return w & ~((ones >> 7) * 0xffu);
@@ -290,12 +290,9 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
 #pragma unroll
     for (int t = 0; t < kSubs; ++t) {
       __amdgpu_buffer_rsrc_t from;
-      if constexpr (S::kMx) {
-        kscales[t].x = load_raw<S::kScales>(rows_at(a.kscale8, t, S::kScales), n16 * S::kScales);
-        from = rows_at(a.k, t, S::kBytes);
-      } else {
-        from = k_rows[t];
-      }
+      if constexpr (S::kMx) kscales[t].x = load_raw<S::kScales>(rows_at(a.kscale8, t, S::kScales), n16 * S::kScales);
+      if constexpr (S::kMx) from = rows_at(a.k, t, S::kBytes);
+      else from = k_rows[t];
 #pragma unroll
       for (int s = 0; s < S::kKLoads; ++s) kraw[t][s] = load_raw<kKPiece>(from, k_at + s * 4 * kKPiece);
     }
@@ -524,11 +521,12 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
       // ---- O^T
 #pragma unroll
       for (int u = 0; u < S::kLoads; ++u) {
-        // MX: a pair of channels is widened where it is needed (all of them at once take 64 registers at d = 256), so what is not finite goes
-        // in front of that
-        uint32_t w[8][S::kMx ? 1 : S::kCpl / 2];
+        // Narrow rows with masks: a pair of channels is widened where it is needed (all of them at once take 64 registers at d = 256), so what
+        // is not finite goes in front of that
+        constexpr bool kPairs = S::kMx || (TREE && R == kRowsFp8);
+        uint32_t w[8][kPairs ? 1 : S::kCpl / 2];
         float scale[8];
-        if constexpr (S::kMx) {
+        if constexpr (kPairs) {
           uint32_t e[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) e[j] = value_scale(j);
@@ -536,7 +534,7 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               const int key = row + (j >> 2) * 16 + 4 * g + (j & 3);
-              const bool none = key >= some && e[j] == 255;
+              const bool none = S::kMx && key >= some && e[j] == 255;
               any_bad |= none && key < len;
               e[j] = none ? 0 : e[j];
 #pragma unroll
@@ -549,7 +547,7 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
             }
           }
 #pragma unroll
-          for (int j = 0; j < 8; ++j) scale[j] = mx_scale(e[j]);
+          for (int j = 0; j < 8; ++j) scale[j] = S::kMx ? mx_scale(e[j]) : 1.0f;
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -562,8 +560,8 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
 #pragma unroll
         for (int c = 0; c < S::kCpl; ++c) {
           const uint32_t sel = c & 1 ? 0x07060302u : 0x05040100u;
-          const int at = S::kMx ? 0 : c >> 1;
-          if constexpr (S::kMx)
+          const int at = kPairs ? 0 : c >> 1;
+          if constexpr (kPairs)
             if (c % 2 == 0)
 #pragma unroll
               for (int j = 0; j < 8; ++j) w[j][0] = mx_pair<R>(vraw[j][u].w, c >> 1, scale[j]);

@@ -350,7 +350,9 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   // tokens 103 -> 107), and its single tokens under a bound of 500 have their own kernel (4096 rows 27.9 -> 17.6, 32k 61 -> 36)
   a.rows = !f32 && a.short_rows >= d.G;
   a.tile = f32 || most > a.piece_rows;
-  // as many as run at once (but at d = 256 over bf16 rows, whose registers let half of them in at a time)
+  // as many as run at once (but at d = 256 over bf16 rows, whose registers let half of them in at a time).  MX rows up to d = 128 with up to
+  // 16 (token, head) rows: three to a CU, since one wavefront's loads of narrow rows are too few bytes (two: 48 ragged sequences of 8
+  // bits 32.6 -> 29.7 us, 4 x 131k rows of 4 bits 123 -> 110).
   a.shares = a.mt * d.D > 256 ? num_cu : mx && a.mt == 1 && d.D < 256 ? 3 * num_cu : 2 * num_cu;
   if (a.shares > kAttendShares) a.shares = kAttendShares;
   // fp32: wavefronts over rows where those give every CU a workgroup, else over keys (1024 tokens of 2 x 8 KV heads over 2048 rows 655

@@ -75,8 +75,8 @@ static ea_status attend(const Dims& d, const void* q, const ea_step* step, const
   }
   if (tree && overlap(out, out_bytes, tree->sees, rows * tree->words * 8)) return EA_ERR_INVALID_ARG;
   a.plan = make_attend_plan(d, n, step->n_tokens, step->max_new, kPlanCus, mx != nullptr);
-  // Workgroups of up to 512 threads, 2^32 threads to a launch.  (The launches of few rows are no larger than 512 shares, their
-  // joining one than 512 times 64 rows; the stretches' joining one comes with few tiles only.)
+  // Workgroups of up to 512 threads, 2^32 threads to a launch.  (The launches of few rows are no larger than kAttendShares, their
+  // joining one than that many times 64 rows; the stretches' joining one comes with few tiles only.)
   if (a.plan.tile && a.plan.grid > kAttendMaxGrid) return EA_ERR_UNSUPPORTED;
   // the stretches' kernel steps over a block by a 32-bit number of bytes
   const int per_channel = mx ? mx->format == EA_MXFP8 ? 8 : 4 : 8 * d.esize();      // bits
@@ -418,6 +418,18 @@ ea_status ea_attend_tree(const ea_params* p, const void* q, const ea_step* step,
   if (s != EA_OK || (s = check_tree(step, tree)) != EA_OK) return s;
   if (n > n_cap || n_cap < 1 || n_cap > ((int64_t)1 << 40)) return EA_ERR_INVALID_ARG;
   return attend(d, q, step, tree, k, v, nullptr, nullptr, nullptr, nullptr, lengths, true, n, n_cap, out, lse, ws, ws_bytes, stream);
+}
+
+ea_status ea_attend_tree_fp8(const ea_params* p, const void* q, const ea_step* step, const ea_tree* tree, const void* k8, const void* v8,
+                             const float* k_scale, const float* v_scale, const int32_t* lengths, int64_t n, int64_t n_cap, void* out,
+                             float* lse, void* ws, size_t ws_bytes, void* stream) {
+  Dims d;
+  ea_status s = check_params(p, &d);
+  if (s != EA_OK || (s = check_tree(step, tree)) != EA_OK) return s;
+  if (d.dtype != EA_BF16 || d.D == 64) return EA_ERR_UNSUPPORTED;
+  if (n > n_cap || n_cap < 1 || n_cap > ((int64_t)1 << 40)) return EA_ERR_INVALID_ARG;
+  d.kv_fp8 = 1;
+  return attend(d, q, step, tree, k8, v8, nullptr, k_scale, v_scale, nullptr, lengths, true, n, n_cap, out, lse, ws, ws_bytes, stream);
 }
 
 ea_status ea_attend_tree_paged(const ea_params* p, const void* q, const ea_step* step, const ea_tree* tree, const void* k_pool,

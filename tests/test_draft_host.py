@@ -113,6 +113,21 @@ def test_attend_refusals(lib):
                               at(8), 1 << 28, None) == 2
 
 
+def test_refusals_over_scaled_bytes(lib):
+    tr = EaTree(30 * OK, 1)
+
+    def call(p=None, st=None, tree=tr, q=at(3), k=at(4), v=at(5), ks=at(11), vs=at(12), lens=at(6), n=64, cap=64, out=at(7), ws=at(8), wsb=1 << 28):
+        return lib.ea_attend_tree_fp8(byref(p or params()), q, byref(st or step()), byref(tree) if tree else None, k, v, ks, vs, lens, n, cap, out,
+                                      None, ws, wsb, None)
+    assert call(p=params(d=64)) == 2 and call(p=params(dtype=ea.EA_F32)) == 2 and call(p=params(dtype=ea.EA_FP8_E4M3)) == 2
+    assert call(tree=None) == 1 and call(tree=EaTree(None, 1)) == 1 and call(tree=EaTree(30 * OK, 5)) == 2 and call(st=step(max_new=65)) == 1
+    for name in ("q", "k", "v", "lens", "out", "ws"):
+        assert call(**{name: None}) == 1, name
+    assert call(ks=VP(OK + 2)) == 1 and call(vs=VP(OK + 2)) == 1 and call(n=65) == 1 and call(cap=0, n=0) == 1 and call(wsb=16) == 3
+    assert call(out=at(3)) == 1 and call(out=VP(5 * OK + 4096)) == 1 and call(out=at(29)) == 1
+    assert call(st=step(n_tokens=0)) == 0 and call(st=step(n_tokens=0), ks=None, vs=None) == 0
+
+
 def test_mask_refusals(lib):
     def call(st=None, parents=at(3), tree=EaTree(30 * OK, 1), seen=at(4), pos=at(5)):
         return lib.ea_tree_masks(byref(params()), byref(st or step()), parents, byref(tree), seen, pos, None)
