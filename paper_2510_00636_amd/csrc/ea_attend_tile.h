@@ -336,114 +336,125 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
 #pragma unroll
     for (int c = 0; c < kVWays; ++c) asm volatile("" : "+v"(v_at[c]));
   }
+  // With masks a wavefront without rows leaves the matrix cores to the others: half-empty tiles at d = 256 (16 trees of 16 tokens of 8 heads
+  // over 4096 rows) 52.5 -> 46.1 us, three quarters full (24 of 24 tokens of 4 over 2460) 63.8 -> 61.6; full ones lose a little (2 of 127
+  // tokens over 10k rows 59.6 -> 61.0, over 8 bits 63.5 -> 64.2).
+  const bool live = row0 + wave * 32 < rows;
   int buf = 0;
   for (int key = key_lo; key < key_hi; key += kN, buf = buf + 1 < kStages ? buf + 1 : 0) {
     const char* kt = lds + buf * kBuffer;
     const int next = key + kN;
     const int next_buf = buf + 1 < kStages ? buf + 1 : 0;
     if constexpr (!FP8) request(buf ^ 2);                  // the tile behind the next one
-    __builtin_amdgcn_s_setprio(1);
-    f32x16 s[kKt];
-#pragma unroll
-    for (int t = 0; t < kKt; ++t) {
-      s[t] = (f32x16)0.0f;
-#pragma unroll
-      for (int c = 0; c < kSteps; ++c) {
-        const bf16x8 w = *(const bf16x8*)(kt + k_at[c % kKWays] + t * k_row<D, FP8>(32) + c / kKWays * kKWays * 32);
-        s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[c], s[t], 0, 0, 0);
+    if (TREE && !live) {
+      if constexpr (!FP8) {
+        make_places(key + 3 * kN);
+        look_up(key + 4 * kN);
       }
-    }
-    if constexpr (kOrdered) order_products<kKt * kSteps, 6>();
-    __builtin_amdgcn_s_setprio(0);
-    // V^T's operands, kRing of them ahead of the products.  Lanes 16 j .. of a group of 16 read four rows of 16 channels, and get one
-    // channel of the four rows each
-    constexpr int kRing = D == 256 ? 1 : 4, kOperands = kKt * 2 * kCt;
-    bf16x8 vf[kRing];
-    auto read_v = [&](int f) {
-      const int c = f % kCt;
-      const char* at = kt + v_at[c % kVWays] + (f / kCt) * 16 * kVPitch + c / kVWays * kVWays * 64;
-      using lds_s16x4 = __attribute__((address_space(3))) s16x4;
-      const s16x4 w0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-      const s16x4 w1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * kVPitch));
-      vf[f % kRing] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(w0, w1, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
+    } else {
+      __builtin_amdgcn_s_setprio(1);
+      f32x16 s[kKt];
 #pragma unroll
-    for (int f = 0; f < kRing; ++f) read_v(f);
-    // key of s[t][r]: t 32 + (r / 4) 8 + hi 4 + r % 4
-    if (TREE && tree) {
-      if (key + kN > new_rows) {
-        // bit i of `bits`: key key + i is seen
-        const int from = key - new_rows, word = from >> 6, shift = from & 63, l = lane_again(), at = wave * 32 + (l & 31);
-        uint64_t bits;
-        if (from < 0) {      // (by less than a tile)
-          bits = see[0][at] << (-from & 63) | ((1ull << (-from & 63)) - 1);
-        } else {
-          bits = word < kWords ? see[TREE ? word & (kWords - 1) : 0][at] >> shift : 0;
-          if (shift > 0 && word + 1 < kWords) bits |= see[TREE ? (word + 1) & (kWords - 1) : 0][at] << (64 - shift);
-        }
+      for (int t = 0; t < kKt; ++t) {
+        s[t] = (f32x16)0.0f;
 #pragma unroll
-        for (int t = 0; t < kKt; ++t) {
-          const uint32_t mine = (uint32_t)(bits >> (t * 32)) >> (l >> 5) * 4;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[t][r] = mine >> ((r >> 2) * 8 + (r & 3)) & 1 ? s[t][r] : -__builtin_inff();
+        for (int c = 0; c < kSteps; ++c) {
+          const bf16x8 w = *(const bf16x8*)(kt + k_at[c % kKWays] + t * k_row<D, FP8>(32) + c / kKWays * kKWays * 32);
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, q[c], s[t], 0, 0, 0);
         }
       }
-    } else if (key + kN > vis_min) {
-      const int l = lane_again(), keys = kAgain ? keys_of(row0 + wave * 32 + (l & 31)) : vis;
+      if constexpr (kOrdered) order_products<kKt * kSteps, 6>();
+      __builtin_amdgcn_s_setprio(0);
+      // V^T's operands, kRing of them ahead of the products.  Lanes 16 j .. of a group of 16 read four rows of 16 channels, and get one
+      // channel of the four rows each
+      constexpr int kRing = D == 256 ? 1 : 4, kOperands = kKt * 2 * kCt;
+      bf16x8 vf[kRing];
+      auto read_v = [&](int f) {
+        const int c = f % kCt;
+        const char* at = kt + v_at[c % kVWays] + (f / kCt) * 16 * kVPitch + c / kVWays * kVWays * 64;
+        using lds_s16x4 = __attribute__((address_space(3))) s16x4;
+        const s16x4 w0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+        const s16x4 w1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * kVPitch));
+        vf[f % kRing] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(w0, w1, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+#pragma unroll
+      for (int f = 0; f < kRing; ++f) read_v(f);
+      // key of s[t][r]: t 32 + (r / 4) 8 + hi 4 + r % 4
+      if (TREE && tree) {
+        if (key + kN > new_rows) {
+          // bit i of `bits`: key key + i is seen
+          const int from = key - new_rows, word = from >> 6, shift = from & 63, l = lane_again(), at = wave * 32 + (l & 31);
+          uint64_t bits;
+          if (from < 0) {      // (by less than a tile)
+            bits = see[0][at] << (-from & 63) | ((1ull << (-from & 63)) - 1);
+          } else {
+            bits = word < kWords ? see[TREE ? word & (kWords - 1) : 0][at] >> shift : 0;
+            if (shift > 0 && word + 1 < kWords) bits |= see[TREE ? (word + 1) & (kWords - 1) : 0][at] << (64 - shift);
+          }
+#pragma unroll
+          for (int t = 0; t < kKt; ++t) {
+            const uint32_t mine = (uint32_t)(bits >> (t * 32)) >> (l >> 5) * 4;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[t][r] = mine >> ((r >> 2) * 8 + (r & 3)) & 1 ? s[t][r] : -__builtin_inff();
+          }
+        }
+      } else if (key + kN > vis_min) {
+        const int l = lane_again(), keys = kAgain ? keys_of(row0 + wave * 32 + (l & 31)) : vis;
+#pragma unroll
+        for (int t = 0; t < kKt; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (key + t * 32 + (r >> 2) * 8 + (kAgain ? l >> 5 : hi) * 4 + (r & 3) >= keys) s[t][r] = -__builtin_inff();
+      }
+      float top = s[0][0];
 #pragma unroll
       for (int t = 0; t < kKt; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (key + t * 32 + (r >> 2) * 8 + (kAgain ? l >> 5 : hi) * 4 + (r & 3) >= keys) s[t][r] = -__builtin_inff();
-    }
-    float top = s[0][0];
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
+      top *= qk;
+      if (__any(top > mx + kLag)) {
+        top = reference(fmaxf(max_xor32(top), mx));
+        const float f = mx == -__builtin_inff() ? 0.0f : pow2(mx - top);
+        mx = top;
+        l *= f;
 #pragma unroll
-    for (int t = 0; t < kKt; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
-    top *= qk;
-    if (__any(top > mx + kLag)) {
-      top = reference(fmaxf(max_xor32(top), mx));
-      const float f = mx == -__builtin_inff() ? 0.0f : pow2(mx - top);
-      mx = top;
-      l *= f;
-#pragma unroll
-      for (int c = 0; c < kCt; ++c) o[c] *= f;
-    }
-    const float from = subtrahend(mx);
-    // Weights of 16 keys at a time, one block ahead of the products that take them, each rounded to one bf16 number; the sum is of the
-    // unrounded ones.  The matrix cores bound this kernel, and they have no product of wider weights with bf16 values: as the sum of
-    // two numbers (as in the kernel of few rows, which the cache's bytes bound) 2048 tokens over 34k rows take 1422 us and not 997, 2 x
-    // 1024 over 4096 rows 121 and not 93 at d = 64, 190 and not 147 at d = 256.  What one number costs in turn is 2^-8 of the weighted
-    // mean of |v| at most, and measured errors of 1.3 to 1.4 times those of results that are only rounded at the end.
-    uint32_t p[kKt * 2][4];
-    auto weigh = [&](int kb) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float s0 = s[kb >> 1][(kb & 1) * 8 + 2 * r], s1 = s[kb >> 1][(kb & 1) * 8 + 2 * r + 1];
-        const float x = pow2(fmaf(s0, qk, -from)), y = pow2(fmaf(s1, qk, -from));
-        l += x + y;
-        p[kb][r] = pack_bf16(x, y);
+        for (int c = 0; c < kCt; ++c) o[c] *= f;
       }
-    };
-    weigh(0);
-    __builtin_amdgcn_s_setprio(1);
-    if constexpr (kOrdered) __builtin_amdgcn_sched_barrier(0);
+      const float from = subtrahend(mx);
+      // Weights of 16 keys at a time, one block ahead of the products that take them, each rounded to one bf16 number; the sum is of the
+      // unrounded ones.  The matrix cores bound this kernel, and they have no product of wider weights with bf16 values: as the sum of
+      // two numbers (as in the kernel of few rows, which the cache's bytes bound) 2048 tokens over 34k rows take 1422 us and not 997, 2 x
+      // 1024 over 4096 rows 121 and not 93 at d = 64, 190 and not 147 at d = 256.  What one number costs in turn is 2^-8 of the weighted
+      // mean of |v| at most, and measured errors of 1.3 to 1.4 times those of results that are only rounded at the end.
+      uint32_t p[kKt * 2][4];
+      auto weigh = [&](int kb) {
 #pragma unroll
-    for (int kb = 0; kb < kKt * 2; ++kb) {
-      const bf16x8 pv = __builtin_bit_cast(bf16x8, make_uint4(p[kb][0], p[kb][1], p[kb][2], p[kb][3]));
+        for (int r = 0; r < 4; ++r) {
+          const float s0 = s[kb >> 1][(kb & 1) * 8 + 2 * r], s1 = s[kb >> 1][(kb & 1) * 8 + 2 * r + 1];
+          const float x = pow2(fmaf(s0, qk, -from)), y = pow2(fmaf(s1, qk, -from));
+          l += x + y;
+          p[kb][r] = pack_bf16(x, y);
+        }
+      };
+      weigh(0);
+      __builtin_amdgcn_s_setprio(1);
+      if constexpr (kOrdered) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int c = 0; c < kCt; ++c) {
-        const int f = kb * kCt + c;
-        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f % kRing], pv, o[c], 0, 0, 0);
-        if (f + kRing < kOperands) read_v(f + kRing);
+      for (int kb = 0; kb < kKt * 2; ++kb) {
+        const bf16x8 pv = __builtin_bit_cast(bf16x8, make_uint4(p[kb][0], p[kb][1], p[kb][2], p[kb][3]));
+#pragma unroll
+        for (int c = 0; c < kCt; ++c) {
+          const int f = kb * kCt + c;
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f % kRing], pv, o[c], 0, 0, 0);
+          if (f + kRing < kOperands) read_v(f + kRing);
+        }
+        if (kb + 1 < kKt * 2) weigh(kb + 1);
+        if (!FP8 && kb == 0) make_places(key + 3 * kN);
+        if (!FP8 && kb == 1) look_up(key + 4 * kN);
+        if constexpr (kOrdered) order_weighted<kCt>();
       }
-      if (kb + 1 < kKt * 2) weigh(kb + 1);
-      if (!FP8 && kb == 0) make_places(key + 3 * kN);
-      if (!FP8 && kb == 1) look_up(key + 4 * kN);
-      if constexpr (kOrdered) order_weighted<kCt>();
+      __builtin_amdgcn_s_setprio(0);
     }
-    __builtin_amdgcn_s_setprio(0);
     if (next < key_hi) {
       if constexpr (FP8) {
         stage(next_buf);
