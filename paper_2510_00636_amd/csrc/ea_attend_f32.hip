@@ -5,7 +5,7 @@
 // loads bring them, so nothing is staged.  Where there are rows enough for the chip, the four wavefronts of a workgroup have 16 of them
 // each and walk the same keys, which come to them out of the L1 cache; else all have the same rows and every eighth (d = 256: fourth)
 // 16 keys, and put their results together through LDS.  The matrix cores and the reads between their instructions bound it: 2 x 256
-// tokens of 32 heads of 64 channels over 8192 rows 359 us, 94 TFLOP/s.
+// tokens of 32 heads of 64 channels over 8192 rows 359 us, 94 TFLOP/s.  Masks are read where a tile reaches the step's own rows.
 #include "ea_attend.h"
 
 namespace ea {

@@ -15,6 +15,9 @@
 // So nothing passes through LDS but the four wavefronts' results at the end, and a wavefront's loads are only bound by its
 // registers: one tile of K and one of V in flight, 16 KiB at d = 128.
 //
+// MX rows: a lane's scale bytes come with its rows, and elements are widened (exactly) just where a product takes them: 4 sequences of 131k
+// rows of 4 bits 105 us, 5.4 TB/s; 48 of 17 to 4419 rows of 8 bits 20.
+//
 // The kernel by itself; the files that include it say for which rows and sizes it is made.
 #pragma once
 #include <type_traits>

