@@ -11,8 +11,8 @@
 // there with their scales: 8 bits 1010 to 1060 us, 4 bits 1030.
 //
 // Masks: 24 trees of 32 tokens over 59k rows of 8 bits 59 us, 2 of 127 tokens over heads of 15k bf16 rows on average 82.  Pieces are short there, and
-// what is around their keys counts: finding the piece 2.4 us, the first tile 3.8, the results 2.7; then 2.0 for 64 keys, of which the matrix
-// cores take 0.9.
+// what is around their keys counts: finding the piece 2.4 us, the first tile 3.8, the results 2.7; then 2.0 for 64 keys and 256 rows, 2.5 for
+// two workgroups' 128, of which the matrix cores take 1.9.
 //
 // The kernel by itself; the files that include it say for which rows and sizes it is made.
 #pragma once
