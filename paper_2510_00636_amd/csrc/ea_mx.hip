@@ -1,7 +1,7 @@
 // Rows into MX pools and back: quantised as they are written, read back as bf16 tensors.
 //
 // Both are copies: 8192 tokens of 8 heads of 128 channels in 4 bits are written in 41 us (their bytes at a copy's 4.89 TB/s take 38) and
-// read back in 10, 131k rows of 8 bits are read back in 164 us (166).  The rotation's fp64 hides under the copy; one token of each of 48
+// read back in 10, 131k rows of 8 bits are read back in 157 us (166).  The rotation's fp64 hides under the copy; one token of each of 48
 // sequences takes 3.9 us, one launch.
 #include "ea_mx.h"
 
@@ -160,7 +160,8 @@ hipError_t launch_append_mx(const MxAppendArgs& given, const Dims& d, hipStream_
 }
 
 // A lane reads eight channels of a row back and writes 16 bytes: the conversion takes the scale along and is exact.  A workgroup has
-// stretches of a head's rows, one after the other, of which those behind the head's length are passed over.
+// stretches of a head's rows, one after the other; a lane asks for its four rows of one together (one by one: 131k rows 164 us, so 157).
+// Those behind the head's length are asked for as the last one and not written.
 namespace {
 template <int D> constexpr int read_rows() { return 256 * 4 / (D / 8); }
 }
@@ -172,21 +173,43 @@ __global__ __launch_bounds__(256) void k_read_mx(MxReadArgs a) {
   for (long long w = blockIdx.x; w < total; w += gridDim.x) {
     const int unit = (int)(w / stretches), row0 = (int)(w - (long long)unit * stretches) * kRows, b = unit / a.Hkv, h = unit - b * a.Hkv;
     const int len = min(a.lens[b], a.n);
-    for (int i = threadIdx.x; i < kRows * kLanes; i += 256) {
-      const int row = row0 + i / kLanes, c = i % kLanes * 8;
-      if (row >= len) break;
-      long long blk = a.pm.table[(long long)b * a.pm.max_blocks + (row >> a.pm.sh)];
-      blk = blk < 0 ? 0 : blk < a.pm.num_blocks ? blk : a.pm.num_blocks - 1;
-      const long long from = ((blk * a.Hkv + h) << a.pm.sh) + (row & ((1 << a.pm.sh) - 1));
-      const long long to = ((long long)unit * a.n_cap + row) * D + c;
+    if (row0 >= len) continue;
+    // a lane's rows together: their blocks, their elements and scales, and then what they stand for
+    constexpr int kPer = kRows * kLanes / 256;
+    const int r0 = row0 + threadIdx.x / kLanes, c = threadIdx.x % kLanes * 8;
+    long long from[kPer];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        __bf16* out = (__bf16*)(s ? a.v_out : a.k_out);
-        if (!out) continue;
-        const char* pool = (const char*)(s ? a.v : a.k);
-        const float scale = mx_scale((s ? a.v_scale : a.k_scale)[from * (D / 32) + c / 32]);
-        if constexpr (BITS == 8) *(uint4*)(out + to) = widen_mx8(*(const uint2*)(pool + from * D + c), scale);
-        else *(uint4*)(out + to) = widen_mx4(*(const uint32_t*)(pool + (from * D + c) / 2), scale);
+    for (int i = 0; i < kPer; ++i) {
+      const int row = min(r0 + i * (256 / kLanes), len - 1);
+      from[i] = a.pm.table[(long long)b * a.pm.max_blocks + (row >> a.pm.sh)];
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int row = min(r0 + i * (256 / kLanes), len - 1);
+      const long long blk = from[i] < 0 ? 0 : from[i] < a.pm.num_blocks ? from[i] : a.pm.num_blocks - 1;
+      from[i] = ((blk * a.Hkv + h) << a.pm.sh) + (row & ((1 << a.pm.sh) - 1));
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      __bf16* out = (__bf16*)(s ? a.v_out : a.k_out);
+      if (!out) continue;
+      const char* pool = (const char*)(s ? a.v : a.k);
+      const uint8_t* scales = s ? a.v_scale : a.k_scale;
+      uint2 x[kPer];
+      uint32_t e[kPer];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        e[i] = scales[from[i] * (D / 32) + c / 32];
+        if constexpr (BITS == 8) x[i] = *(const uint2*)(pool + from[i] * D + c);
+        else x[i].x = *(const uint32_t*)(pool + (from[i] * D + c) / 2);
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int row = r0 + i * (256 / kLanes);
+        if (row >= len) continue;
+        const long long to = ((long long)unit * a.n_cap + row) * D + c;
+        if constexpr (BITS == 8) *(uint4*)(out + to) = widen_mx8(x[i], mx_scale(e[i]));
+        else *(uint4*)(out + to) = widen_mx4(x[i].x, mx_scale(e[i]));
       }
     }
   }
