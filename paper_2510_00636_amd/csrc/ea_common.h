@@ -67,6 +67,7 @@ struct AttendPlan {
   int by_share;       // the joining launch looks at every workgroup's last head, not at every head
   int piece_rows;     // rows reserved for a partial result
   int tile_rows;      // (token, head) rows of a workgroup of the tile kernel
+  int keys;           // fp32: its wavefronts share out the keys, not the rows
   int64_t grid;       // its workgroups: as many as there may be pieces
   int most_pieces;    // most pieces where tiles are cut along the keys, 0: none is
   float per_slot;     // 1 / workgroups that run at once
@@ -196,7 +197,7 @@ inline int64_t f32_span(int64_t heads, int64_t n, int64_t slots) {
 }
 
 // what a call of at most n rows per head launches; n_tokens and max_new as in ea_step
-AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t max_new, int num_cu, bool mx = false);
+AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t max_new, int num_cu, bool mx = false, bool tree = false);
 ea_status check_step(const Dims& d, const ea_step* step, int64_t n);
 ea_status check_paged(const Dims& d, const ea_paged* pg, int64_t n, PageMap* pm);
 

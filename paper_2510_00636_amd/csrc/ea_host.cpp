@@ -331,7 +331,7 @@ ea_status check_step(const Dims& d, const ea_step* step, int64_t n) {
   return EA_OK;
 }
 
-AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t max_new, int num_cu, bool mx) {
+AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t max_new, int num_cu, bool mx, bool tree) {
   AttendPlan a = {};
   const bool f32 = d.dtype != EA_BF16;
   if (max_new > n_tokens) max_new = n_tokens;
@@ -361,8 +361,14 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   // 35; 40 tokens 38 and 37) but at d = 256, where registers leave one workgroup to a CU either way (64 tokens of 2 heads 62 and 54)
   if (!f32) a.tile_rows = d.D < 256 && most <= 128 ? 128 : 256;
   else a.tile_rows = most >= kAttendF32LongRows && n_tokens * d.G / kAttendF32LongRows * d.Hkv >= num_cu ? kAttendF32LongRows : kAttendF32Rows;
+  a.keys = f32 && a.tile_rows == kAttendF32Rows;
+  // With masks, over keys: more than 16 rows to a wavefront, for which the keys are read once, where pieces of 256 keys half fill the chip (4 x 12
+  // tokens of 3 heads over 40k rows 438 -> 297 us, 2 x 64 of 4 over 8192 123 -> 101, at d = 256 over 4096 127 -> 99; 16 of 4 over 8 KV heads
+  // of 4096 rows, 128 pieces, 41.3 and 40.8; 16 of 4 over 2 of 700, 6 pieces, 17.7 and 36.1).
+  const int64_t wide_rows = kAttendF32Rows * (d.D == 256 ? 2 : 4), wide_pieces = (n_tokens * d.G / wide_rows + 1) * d.Hkv * ((n + 255) / 256);
+  if (a.keys && tree && most > kAttendF32Rows && wide_pieces >= num_cu / 2) a.tile_rows = (int)wide_rows;
   // a sequence's last tile may be short: one more for each
-  const int64_t tiles = n_tokens * d.G / a.tile_rows + d.B, slots = a.tile_rows == 256 ? num_cu : 2 * (int64_t)num_cu;
+  const int64_t tiles = n_tokens * d.G / a.tile_rows + d.B, slots = a.tile_rows == 256 || (a.keys && a.tile_rows > kAttendF32Rows && d.D > 64) ? num_cu : 2 * (int64_t)num_cu;
   a.grid = tiles * d.Hkv;
   a.per_slot = 1.0f / (float)slots;
   // More rounds of whole tiles than this share out the chip well enough, and keys that are this few are not worth a second launch (64

@@ -74,7 +74,7 @@ static ea_status attend(const Dims& d, const void* q, const ea_step* step, const
     if (overlap(out, out_bytes, k, cache) || overlap(out, out_bytes, v, cache)) return EA_ERR_INVALID_ARG;
   }
   if (tree && overlap(out, out_bytes, tree->sees, rows * tree->words * 8)) return EA_ERR_INVALID_ARG;
-  a.plan = make_attend_plan(d, n, step->n_tokens, step->max_new, kPlanCus, mx != nullptr);
+  a.plan = make_attend_plan(d, n, step->n_tokens, step->max_new, kPlanCus, mx != nullptr, tree != nullptr);
   // Workgroups of up to 512 threads, 2^32 threads to a launch.  (The launches of few rows are no larger than kAttendShares, their
   // joining one than that many times 64 rows; the stretches' joining one comes with few tiles only.)
   if (a.plan.tile && a.plan.grid > kAttendMaxGrid) return EA_ERR_UNSUPPORTED;
@@ -287,9 +287,10 @@ size_t ea_attend_workspace_bytes(const ea_params* p, const ea_step* step, int64_
   Dims d;
   if (check_params(p, &d) != EA_OK || check_step(d, step, n) != EA_OK) return 0;
   const size_t rows = make_attend_plan(d, n, step->n_tokens, step->max_new, kPlanCus).total;
-  if (d.dtype != EA_BF16) return rows;
-  const size_t mx = make_attend_plan(d, n, step->n_tokens, step->max_new, kPlanCus, true).total;
-  return rows > mx ? rows : mx;      // whatever the cache is
+  // whatever the cache is, with masks or without
+  const bool wide = d.dtype == EA_BF16;
+  const size_t other = make_attend_plan(d, n, step->n_tokens, step->max_new, kPlanCus, wide, !wide).total;
+  return rows > other ? rows : other;
 }
 
 ea_status ea_attend(const ea_params* p, const void* q, const ea_step* step, const void* k, const void* v,

@@ -311,3 +311,42 @@ def test_no_call_writes_behind_its_workspace(hq, hkv, d, m, n):
         ea.attend_tree_mx(p, q, step, tree, mx, pg, lens[:, 0].contiguous(), n, out, lse, ws)
         torch.cuda.synchronize()
     assert (room[size:] == 0x3C).all()
+
+
+@pytest.mark.parametrize("hq,hkv,d,m,lens", [(18, 6, 128, [12, 3, 9], [2600, 1700, 40]), (16, 4, 64, [64, 1, 33], [3000, 900, 33]), (8, 2, 256, [16, 5, 30], [4100, 5, 1999]),
+                                             (4, 1, 128, [256, 60, 17], [4500, 2000, 17]), (16, 4, 256, [70, 0, 2], [2300, 7, 1])])
+def test_many_rows_of_a_wavefront_over_fp32(hq, hkv, d, m, lens):
+    """Trees that have more than 16 rows to a KV head, over lengths at which a wavefront takes up to 64 (d = 256: 32) of them."""
+    r = np.random.default_rng(d + sum(m))
+    L = np.maximum(np.array(lens)[:, None] - r.integers(0, 60, (3, hkv)), 0)
+    q, cu, k, v, L = attend_inputs(d, hq, hkv, d, "f32", L, m, room=2)
+    for how in ("tree", "any"):
+        sees = some_masks(r, m, how)
+        words = -(-max(m) // 64)
+        got, lse = run("f32", q, cu, sees, words, k, v, L)
+        check(got, lse, q, cu, widen(k), widen(v), L, padded(sees, words), "f32")
+        assert (got[cu[-1]:] == 7.0).all() and (lse[cu[-1]:] == 7.0).all()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_values_that_are_not_finite_among_many_rows_of_a_wavefront(d):
+    hq, hkv, m = 8, 2, [20, 7, 30]
+    r = np.random.default_rng(d)
+    lens = np.array([4100, 2000, 30])
+    q, cu, k, v, L = attend_inputs(d, hq, hkv, d, "f32", lens, m)
+    sees = some_masks(r, m, "tree")
+    clean, clean_lse = run("f32", q, cu, sees, 1, k, v, L)
+    v = v.copy()
+    bad = [5, 2, 17]
+    for b in range(3):
+        v[b, :, lens[b] - m[b] + bad[b], 3] = np.inf
+    got, lse = run("f32", q, cu, sees, 1, k, v, L)
+    other = np.arange(d) != 3
+    assert np.array_equal(lse, clean_lse) and np.array_equal(got[:, :, other], clean[:, :, other])
+    for b in range(3):
+        for i in range(m[b]):
+            t = cu[b] + i
+            if sees[t, bad[b]]:
+                assert not np.isfinite(got[t, :, 3]).any()
+            else:
+                assert np.array_equal(got[t, :, 3], clean[t, :, 3])
