@@ -350,3 +350,58 @@ def test_values_that_are_not_finite_among_many_rows_of_a_wavefront(d):
                 assert not np.isfinite(got[t, :, 3]).any()
             else:
                 assert np.array_equal(got[t, :, 3], clean[t, :, 3])
+
+
+@pytest.mark.parametrize("form", ["paged", "heads", "fp8", "f32", "mx8", "mx4"])
+@pytest.mark.parametrize("m", [[3, 1, 2], [40, 90, 1]])
+def test_strided_queries_and_no_log_sums(form, m):
+    """Queries inside wider rows give the bits of queries by themselves, and so does a call that is not asked for log-sums."""
+    import torch
+    hq, hkv, d = 8, 2, 128
+    lens, cu = [700, 130, 300], sums(m)
+    dt = "f32" if form == "f32" else "bf16"
+    q, cu, k, v, L = attend_inputs(4, hq, hkv, d, dt, lens, m)
+    sees, words = some_masks(np.random.default_rng(1), m, "tree"), -(-max(m) // 64)
+    t, p = q.shape[0], ea.make_params(3, hq, hkv, d, kind(dt))
+    tree, cud = ea.make_tree(handle(sees, t, words)), i32(cu)
+    wide = torch.full((t, hq + 3, d), float("nan"), dtype=torch.float32 if dt == "f32" else torch.bfloat16, device="cuda")
+    wide[:, :hq] = to_dev(q)
+    if form.startswith("mx"):
+        c = Mx(7, lens, hkv, d, 32, int(form[2:]))
+    elif form == "paged":
+        kp, vp, table, nb = make_block_pools(k, v, 16, 1)
+        kd, vd, td = to_dev(kp), to_dev(vp), i32(table)
+        pg = ea.make_paged(td, 16, nb)
+    elif form == "fp8":
+        kd, vd = (to_dev(quantize_fp8(np.nan_to_num(widen(x)))[0]) for x in (k, v))
+    else:
+        kd, vd = to_dev(k), to_dev(v)
+    got = []
+    for qd, stride, with_lse in ((to_dev(q), 0, True), (wide, (hq + 3) * d, True), (to_dev(q), 0, False)):
+        step = ea.make_step(cud, t, max(m), stride)
+        out, lse = outputs(q, dt)
+        if not with_lse:
+            lse = None
+        if form.startswith("mx"):
+            args = (c.mx, c.pg, c.ld, c.n)
+            ws = torch.empty(ea.attend_workspace_bytes(p, step, c.n), dtype=torch.uint8, device="cuda")
+            ea.attend_tree_mx(p, qd, step, tree, *args, out, lse, ws)
+            plain = torch.empty_like(out)
+            ea.attend_mx(p, qd, step, *args, plain, lse, ws)
+            torch.cuda.synchronize()
+            got.append([out, plain, lse])
+            continue
+        n = table.shape[1] * 16 if form == "paged" else k.shape[2]
+        ws = torch.empty(ea.attend_workspace_bytes(p, step, n), dtype=torch.uint8, device="cuda")
+        if form == "paged":
+            ea.attend_tree_paged(p, qd, step, tree, kd, vd, pg, i32(lens), n, out, lse, ws)
+        elif form == "fp8":
+            ea.attend_tree_fp8(p, qd, step, tree, kd, vd, None, None, i32(L), n, n, out, lse, ws)
+        else:
+            ea.attend_tree(p, qd, step, tree, kd, vd, i32(L), n, n, out, lse, ws)
+        torch.cuda.synchronize()
+        got.append([out, lse])
+    for other in got[1:]:
+        for a, b in zip(got[0], other):
+            assert b is None or torch.equal(a, b)
+    assert torch.isfinite(got[0][0].float()).all()
