@@ -359,7 +359,11 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   // and 690 us, 64 tokens of 2 KV heads 21 and 14)
   // bf16: 256 rows to a workgroup, 128 where no sequence has more (d = 128, 32 tokens of 4 heads over 16k rows 32 us, in one tile of 256
   // 35; 40 tokens 38 and 37) but at d = 256, where registers leave one workgroup to a CU either way (64 tokens of 2 heads 62 and 54)
-  if (!f32) a.tile_rows = d.D < 256 && most <= 128 ? 128 : 256;
+  // MX rows up to 1024 keys: 128, too, so that one workgroup's beginning and end run beside another one's keys (48 x 170 tokens of 5 heads over 200
+  // rows of 8 bits 114 -> 89 us, 16 x 512 of 4 over 512 96 -> 88, 8 x 1024 over 1024 131 -> 122; 4 x 2048 over 2048 180 and 182, 16 x 100
+  // over 2048 87 and 90; trees alike).  Over bf16 rows, which pass through no registers, it depends (trees of 170 tokens over 200 rows 137
+  // and 120, at d = 64 35 and 43; 256 over 1024 58 and 60).
+  if (!f32) a.tile_rows = d.D < 256 && (most <= 128 || (mx && n <= 1024)) ? 128 : 256;
   else a.tile_rows = most >= kAttendF32LongRows && n_tokens * d.G / kAttendF32LongRows * d.Hkv >= num_cu ? kAttendF32LongRows : kAttendF32Rows;
   a.keys = f32 && a.tile_rows == kAttendF32Rows;
   // With masks, over keys: more than 16 rows to a wavefront, for which the keys are read once, where pieces of 256 keys half fill the chip (4 x 12
