@@ -485,7 +485,7 @@ def attend_mx(p, q, step, mx, pg, lengths, n, out, lse, ws, stream=None):
 
 def make_tree(sees):
     """ea_tree for a tensor of masks [n_tokens, words] int64 on the device."""
-    if sees.dim() != 2 or sees.element_size() != 8 or not sees.is_contiguous():
+    if sees.dim() != 2 or sees.element_size() != 8 or sees.is_floating_point() or sees.is_complex() or not sees.is_contiguous():
         raise ValueError("masks are [tokens, words] of 64 bits, contiguous")
     t = EaTree(sees.data_ptr(), int(sees.shape[1]))
     t.tensors = (sees,)

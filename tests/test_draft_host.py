@@ -177,6 +177,7 @@ def test_handles_check_their_tensors():
         with pytest.raises(ValueError):
             ea.make_mx(*bad)
     ea.make_tree(torch.zeros(5, 2, dtype=torch.int64))
-    for bad in (torch.zeros(5, dtype=torch.int64), torch.zeros(5, 2, dtype=torch.int32), torch.zeros(5, 4, dtype=torch.int64)[:, ::2]):
+    for bad in (torch.zeros(5, dtype=torch.int64), torch.zeros(5, 2, dtype=torch.int32), torch.zeros(5, 4, dtype=torch.int64)[:, ::2],
+                torch.zeros(5, 2, dtype=torch.float64), torch.zeros(5, 2, dtype=torch.complex64)):
         with pytest.raises(ValueError):
             ea.make_tree(bad)
