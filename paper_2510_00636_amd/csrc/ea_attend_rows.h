@@ -115,13 +115,21 @@ __device__ __forceinline__ uint32_t mx_pair(const uint32_t* w, int x, float scal
     default: return mx4_pair<3>(w[x >> 2], scale);
   }
 }
-// a word's elements without those that are not numbers (e4m3's are the bytes of all ones); `any` is set where there was one
+// A word's elements without those that widen to no finite number under scale byte e (not 255, which makes NaN of all of them): e4m3's
+// bytes of all ones, and elements of 2^(255 - e) and more, which are infinities as bf16.  Codes ascend with what they stand for, so
+// those begin at one code: e4m3's (262 - e) * 8, from e = 247 on, e2m1's 8 - 2 (e - 252), from 253 on.  `any` is set where there was one.
 template <Rows R>
-__device__ __forceinline__ uint32_t finite_elements(uint32_t w, bool& any) {
-  if constexpr (R == kRowsMx4) return w;
-  const uint32_t ones = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-  any |= ones != 0;
-  return w & ~((ones >> 7) * 0xffu);
+__device__ __forceinline__ uint32_t finite_elements(uint32_t w, uint32_t e, bool& any) {
+  if constexpr (R == kRowsMx4) {
+    const uint32_t up = e > 252 ? 2 * (e - 252) : 0;        // from the least such code to the sign bit
+    const uint32_t past = ((w & 0x77777777u) + up * 0x11111111u) & 0x88888888u;
+    any |= past != 0;
+    return w & ~((past >> 3) * 0xfu);
+  }
+  const uint32_t up = R == kRowsMx8 && e > 246 ? 8 * (e - 246) : 1;
+  const uint32_t past = ((w & 0x7f7f7f7fu) + up * 0x01010101u) & 0x80808080u;
+  any |= past != 0;
+  return w & ~((past >> 7) * 0xffu);
 }
 
 // eight channels of K for the products' step `sub` of those that the load serves
@@ -543,7 +551,7 @@ __global__ __launch_bounds__(256, (rows_groups<D, R, MT>())) void k_attend_rows(
 #pragma unroll
               for (int i = 0; i < (int)(sizeof(Raw<kPiece>) / 4); ++i) {
                 bool bad_element = false;
-                const uint32_t x = vraw[j][u].w[i], y = finite_elements<R>(x, bad_element);
+                const uint32_t x = vraw[j][u].w[i], y = finite_elements<R>(x, e[j], bad_element);
                 any_bad |= bad_element && key >= some;
                 vraw[j][u].w[i] = none ? 0 : key >= some ? y : x;
               }
