@@ -445,9 +445,9 @@ ea_status ea_tree_masks(const ea_params* p, const ea_step* step, const int32_t* 
 
 /* Attention of such a step: with m tokens of sequence b in the step, token i sees the rows j < len - m of its KV head, and row
  * len - m + j where bit j of its mask is set.  Else as ea_attend (bf16 or fp32), ea_attend_fp8, ea_attend_paged and ea_attend_mx: empty
- * rows, values that are not finite in rows that a token does not see, workspaces and bounds (with masks, which
- * sequences add few tokens may depend on n and B, too, and r of fp32 may be 32).  Masks need not come from a tree; bits from m on
- * name no row. */
+ * rows, values that are not finite in rows that a token does not see, workspaces and bounds (r of fp32 may be 32, too).  Which sequences
+ * add few tokens depends on n, B and Hkv as well: where max_new allows more, none does if n <= 2^14 and B * Hkv * n <= 2^17 (2^14 at
+ * d = 256 over 8- and 4-bit rows).  Masks need not come from a tree; bits from m on name no row. */
 ea_status ea_attend_tree(const ea_params* p, const void* q, const ea_step* step, const ea_tree* tree, const void* k, const void* v,
                          const int32_t* lengths, int64_t n, int64_t n_cap, void* out, float* lse, void* ws, size_t ws_bytes,
                          void* stream);

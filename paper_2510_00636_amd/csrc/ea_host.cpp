@@ -350,6 +350,19 @@ AttendPlan make_attend_plan(const Dims& d, int64_t n, int64_t n_tokens, int64_t 
   // tokens 103 -> 107), and its single tokens under a bound of 500 have their own kernel (4096 rows 27.9 -> 17.6, 32k 61 -> 36)
   a.rows = !f32 && a.short_rows >= d.G;
   a.tile = f32 || most > a.piece_rows;
+  // With masks a sequence of few rows goes with the others, which saves its two launches, in calls of few cached rows: 2^17 over all heads
+  // (2^14 of 8 and 4 bits at d = 256, which the stretches' kernel takes no faster than bf16 rows), and 2^14 in a head.  By bounds alone:
+  // n_tokens is room, and max_new what a captured step allows, so what is lost where no sequence adds more than one token has to stay
+  // small next to what is saved where all do, or some.  With launches of their own and with the others, us, all sequences adding 32
+  // tokens, every seventh, none (4 query heads to each of 4 KV heads, d = 128 and bf16 rows unless named):
+  //   within: 16 sequences over 1024 rows 30 and 26, 35 and 22, 24 and 19; one over 16k 26 and 22, none 22 and 17; 32 over 1024 at d = 256
+  //   57 and 52, 59 and 49, 41 and 45; 16 over 256 of 8 bits at d = 256 28 and 24, 34 and 22, 15 and 18;
+  //   beyond: 32 over 1024 of 4 bits at d = 256 64 and 60, 49 and 57, 29 and 49; 48 over 4096 of 8 bits 99 and 93, 70 and 67, 48 and 65,
+  //   adding 64 152 and 148, 81 and 101, 50 and 85; one head of 130k rows at d = 64 56 and 52, none 26 and 37; 16 over 16k of 4 bits at
+  //   d = 256 183 and 177, 101 and 167, 62 and 159.
+  // Their weights are one bf16 number then, as the others' are.
+  const int64_t cached = d.units() * n, few_cached = (mx || d.kv_fp8) && d.D == 256 ? 1 << 14 : 1 << 17;
+  if (tree && a.tile && n <= 1 << 14 && cached <= few_cached) a.rows = 0;
   // as many as run at once (but at d = 256 over bf16 rows, whose registers let half of them in at a time).  MX rows up to d = 128 with up to
   // 16 (token, head) rows: three to a CU, since one wavefront's loads of narrow rows are too few bytes (two: 48 ragged sequences of 8
   // bits 32.6 -> 29.7 us, 4 x 131k rows of 4 bits 123 -> 110).

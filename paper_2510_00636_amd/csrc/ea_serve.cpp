@@ -98,10 +98,6 @@ static ea_status attend(const Dims& d, const void* q, const ea_step* step, const
     a.sees = tree->sees;
     a.words = tree->words;
   }
-  // A tree's short sequences go with the others where the host sees none (one sequence, or as many tokens as there can be), or where
-  // their two launches cost more than they save: 16 sequences over 1024 rows, a third adding 60 tokens and the others one, 8 bits 50
-  // -> 45 us, bf16 53 -> 40; over 4096 87 and 95, 99 and 92, over 16k 206 and 272, 250 and 280.  24 trees of 32 tokens 75 -> 66.
-  if (tree && a.plan.tile && (d.B == 1 || n <= 2048 || step->n_tokens == d.B * step->max_new)) a.plan.rows = 0;
   // (every workgroup looks at all that is cut)
   a.by_head = tree && per_head && d.units() <= kCutHeads;
   a.only_long = a.plan.rows;
