@@ -405,3 +405,23 @@ def test_strided_queries_and_no_log_sums(form, m):
         for a, b in zip(got[0], other):
             assert b is None or torch.equal(a, b)
     assert torch.isfinite(got[0][0].float()).all()
+
+
+@pytest.mark.parametrize("hq,hkv,d,m,n", [(8, 2, 128, [16, 5], 9000), (8, 2, 64, [60, 3], 9000), (8, 4, 256, [9, 30], 5000), (18, 6, 128, [200, 1], 4000),
+                                          (8, 2, 128, [2, 1], 700), (4, 1, 64, [256, 256], 40000)])
+def test_no_call_over_fp32_writes_behind_its_workspace(hq, hkv, d, m, n):
+    """Trees of more than 16 rows in tiles of 32 and 64, cut along the keys, and of few."""
+    import torch
+    cu = sums(m)
+    t = int(cu[-1])
+    p, step = ea.make_params(2, hq, hkv, d, ea.EA_F32), ea.make_step(i32(cu), t, max(m))
+    size = ea.attend_workspace_bytes(p, step, n)
+    room = torch.full((size + 65536,), 0x3C, dtype=torch.uint8, device="cuda")
+    q = torch.randn(t, hq, d, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(t, hq, device="cuda")
+    k = torch.randn(2, 2, hkv, n, d, device="cuda")
+    tree = ea.make_tree(handle(some_masks(np.random.default_rng(0), m, "tree"), t, 4))
+    for lens in ([n, n], [n, n // 3 + m[1]], [max(m), max(m)]):
+        ea.attend_tree(p, q, step, tree, k[0], k[1], i32([[x] * hkv for x in lens]), n, n, out, lse, room[:size])
+        torch.cuda.synchronize()
+        assert (room[size:] == 0x3C).all() and torch.isfinite(out).all()
