@@ -16,7 +16,7 @@ SOURCES = ["ea_host.cpp", "ea_api.hip", "ea_stats.hip", "ea_score.hip", "ea_scor
            "ea_compact.hip", "ea_baselines.hip", "ea_frontend.hip", "ea_serve.cpp", "ea_step.hip", "ea_mx.hip", "ea_tree.hip",
            "ea_attend_rows.hip", "ea_attend_rows_tree.hip", "ea_attend_rows_mx8.hip", "ea_attend_rows_mx4.hip", "ea_attend_rows_join.hip",
            "ea_attend_tile.hip", "ea_attend_tile_tree.hip", "ea_attend_tile_mx8.hip", "ea_attend_tile_mx4.hip", "ea_attend_join.hip",
-           "ea_attend_f32.hip"]
+           "ea_attend_f32.hip", "ea_attend_f32_tree.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 instructions are switched off for the device pass (the host pass warns that it
 # does not know the feature; harmless)

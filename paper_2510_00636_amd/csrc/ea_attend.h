@@ -301,6 +301,7 @@ hipError_t launch_attend_rows_join(const AttendArgs& a, hipStream_t st);
 hipError_t launch_attend_rows(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_tile(const AttendArgs& a, const Dims& d, hipStream_t st);
 hipError_t launch_attend_f32(const AttendArgs& a, hipStream_t st);
+hipError_t launch_attend_f32_tree(const AttendArgs& a, hipStream_t st);
 hipError_t launch_attend_join(const AttendArgs& a, bool f32, hipStream_t st);
 
 }  // namespace ea

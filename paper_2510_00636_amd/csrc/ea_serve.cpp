@@ -22,7 +22,7 @@ hipError_t launch_attend(const AttendArgs& a, const Dims& d, hipStream_t st) {
         : a.sees ? launch_attend_rows_tree(a, d, st) : launch_attend_rows(a, d, st);
   if (e != hipSuccess || !a.plan.tile) return e;
   if (a.mx) return a.mx == 8 ? launch_attend_tile_mx8(a, d, st) : launch_attend_tile_mx4(a, d, st);
-  if (d.dtype != EA_BF16) return launch_attend_f32(a, st);
+  if (d.dtype != EA_BF16) return a.sees ? launch_attend_f32_tree(a, st) : launch_attend_f32(a, st);
   return a.sees ? launch_attend_tile_tree(a, d, st) : launch_attend_tile(a, d, st);
 }
 
