@@ -114,19 +114,19 @@ __device__ __forceinline__ int ceil_div(int x, int by) {      // x < 2^24, both 
   return k;
 }
 // WAVES > 1: that many wavefronts, the workgroup's, share out the sequences between them, their sums through LDS (24 sequences: 4.2 us of a piece's time -> 2.8).
-// HEADS: with a.by_head what is cut is a head, not a sequence whose heads have lengths of their own.
-template <int ROWS, int WAVES = 1, bool HEADS = false>
+// PER_HEAD: heads have lengths of their own (a.per_head).  HEADS: with a.by_head what is cut is such a head, not a sequence.
+template <int ROWS, bool PER_HEAD, int WAVES = 1, bool HEADS = false>
 __device__ __forceinline__ Piece find_piece(const AttendArgs& a, int index, float (*sums)[3][64] = nullptr) {
   const int lane = threadIdx.x & 63;
-  const bool by_head = HEADS && a.by_head;
+  const bool by_head = PER_HEAD && HEADS && a.by_head;
   const int supers = by_head ? a.B * a.Hkv : a.B, heads = by_head ? 1 : a.Hkv;      // that are cut each for itself, and heads of one
   auto look = [&](int b, int& tiles, int& steps) {
-    const int su = min(b, supers - 1), at = by_head ? su / a.Hkv : su, rows = b < supers ? (first_token(a, at + 1) - first_token(a, at)) * a.G : 0;
+    const int su = min(b, supers - 1), at = by_head ? su / a.Hkv : su;
+    const bool one = !PER_HEAD || by_head;      // length to look at
+    int len = one ? rows_of(a, at, by_head ? su - at * a.Hkv : 0) : 0;
+    const int rows = b < supers ? (first_token(a, at + 1) - first_token(a, at)) * a.G : 0;
     const bool none = rows < 1 || (a.only_long && rows <= a.short_rows);
-    int len = 0;
-    if (!a.per_head || by_head) {
-      len = rows_of(a, at, by_head ? su - at * a.Hkv : 0);
-    } else if (!none) {
+    if (!one && !none) {
       // A line of memory for each head and lane: only of sequences that are this kernel's, and four at a time (16 of 100 sequences of 8
       // heads add 40 tokens, the others one, at d = 128: of all sequences, one by one, 133 us, so 111).
       int h = 0;

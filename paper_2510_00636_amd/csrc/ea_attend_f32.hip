@@ -22,7 +22,7 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
   extern __shared__ __attribute__((aligned(16))) float pass_o[];          // KEYS: [wavefront][row][channel], and behind it maxima and sums
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n16 = lane & 15, g = lane >> 4;
-  const Piece piece = find_piece<kM>(a, blockIdx.x);
+  const Piece piece = find_piece<kM, true>(a, blockIdx.x);
   if (piece.tile < 0) return;
   note_cuts(a, piece, blockIdx.x);
   const int b = piece.b, h = piece.h, t0 = piece.t0, m = piece.m, rows = m * a.G, row0 = piece.tile * kM;

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
   constexpr int kWords = EA_TREE_MAX / 64;
   __shared__ uint64_t see[TREE ? kWords : 1][TREE ? kM : 1];         // which of the new rows the workgroup's rows see
   static_assert(!TREE || sizeof(see) >= sizeof(float[NW][3][64]), "the pieces' sums stand there first");
-  const Piece piece = find_piece<kM, TREE ? NW : 1, TREE>(a, blockIdx.x, (float(*)[3][64])see);
+  const Piece piece = find_piece<kM, !PAGED, TREE ? NW : 1, TREE>(a, blockIdx.x, (float(*)[3][64])see);
   if (piece.tile < 0) return;
   note_cuts<TREE>(a, piece, blockIdx.x);
   const int b = piece.b, h = piece.h, t0 = piece.t0, m = piece.m, rows = m * a.G, row0 = piece.tile * kM;
