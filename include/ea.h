@@ -397,7 +397,7 @@ ea_status ea_attend_fp8(const ea_params* p, const void* q, const ea_step* step, 
  *   k, v              [num_blocks, Hkv, block_size, d] elements: e4m3 bytes (EA_MXFP8), or e2m1 (EA_MXFP4), two to a byte, the even
  *                     channel in its low half
  *   k_scale, v_scale  [num_blocks, Hkv, block_size, d / 32] bytes e; channel c of a row is element * 2^(e - 127) (exact in bf16 from
- *                     2^-126 on), and NaN where e is 255.
+ *                     2^-126 on; infinite from 2^128 on, which ea_append_mx does not write), and NaN where e is 255.
  * All are DEVICE pointers, 16-byte aligned, and apart from each other.  p->dtype is the type of the model's own rows and must be
  * EA_BF16; head_dim 64, 128 or 256. */
 typedef enum { EA_MXFP8 = 0, EA_MXFP4 = 1 } ea_mx_format;

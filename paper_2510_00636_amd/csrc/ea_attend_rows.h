@@ -18,6 +18,9 @@
 // MX rows: a lane's scale bytes come with its rows, and elements are widened (exactly) just where a product takes them: 4 sequences of 131k
 // rows of 4 bits 105 us, 5.4 TB/s; 48 of 17 to 4419 rows of 8 bits 20.
 //
+// What a part of a head needs besides its tiles does not fit the scalar registers: 118 to 155 of them wait in lanes of vector registers,
+// where a part begins and ends, without memory.
+//
 // The kernel by itself; the files that include it say for which rows and sizes it is made.
 #pragma once
 #include <type_traits>
@@ -91,7 +94,7 @@ template <> struct FourScales<256> { uint32_t x[4]; };
 __device__ __forceinline__ uint32_t byte_of(uint32_t lo, int i) { return __builtin_amdgcn_ubfe(lo, i * 8, 8); }
 __device__ __forceinline__ uint32_t byte_of(uint32_t lo, uint32_t hi, int i) { return __builtin_amdgcn_ubfe(i & 4 ? hi : lo, (i & 3) * 8, 8); }
 
-// a loaded piece of V as bf16: all its channels, or (narrow rows with masks) the pair of channels 2 x, 2 x + 1
+// a loaded piece of V as bf16, all its channels
 template <int D, Rows R, int BYTES>
 __device__ __forceinline__ void widen_piece(const Raw<BYTES>& p, uint32_t* o) {
   if constexpr (R == kRowsBf16) {
@@ -105,6 +108,7 @@ __device__ __forceinline__ void widen_piece(const Raw<BYTES>& p, uint32_t* o) {
     }
   }
 }
+// narrow rows with masks, and MX rows: its channels 2 x, 2 x + 1
 template <Rows R>
 __device__ __forceinline__ uint32_t mx_pair(const uint32_t* w, int x, float scale) {
   if constexpr (R != kRowsMx4) return mx8_pair(w[x >> 1], scale, x & 1);

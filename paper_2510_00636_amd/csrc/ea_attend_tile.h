@@ -1,7 +1,7 @@
 // Attention of long stretches of new tokens (prompts read in pieces): the matrix cores bound it.
 //
-// A workgroup takes 256 (token, head) rows of a KV head, 32 for each wavefront, or 128 where no sequence has more, and walks the keys
-// in tiles that all wavefronts share through LDS, the next tiles requested while one is worked on.  S^T = K Q^T and O^T = V^T P^T by v_mfma_f32_32x32x16_bf16: a
+// A workgroup takes 256 (token, head) rows of a KV head, 32 for each wavefront, or 128 where no sequence has more and over MX rows up to
+// 1024 keys (not at d = 256), and walks the keys in tiles that all wavefronts share through LDS, the next tiles requested while one is worked on.  S^T = K Q^T and O^T = V^T P^T by v_mfma_f32_32x32x16_bf16: a
 // lane then holds half of the keys of its row, and what it holds is, as it stands, the operand of the second product if V^T has
 // its keys in the same order.  V^T comes out of the row-major tile by ds_read_b64_tr_b16.
 //
@@ -12,7 +12,7 @@
 //
 // Masks: 24 trees of 32 tokens over 59k rows of 8 bits 59 us, 2 of 127 tokens over heads of 15k bf16 rows on average 82.  Pieces are short there, and
 // what is around their keys counts: finding the piece 2.4 us, the first tile 3.8, the results 2.7; then 2.0 for 64 keys and 256 rows, 2.5 for
-// two workgroups' 128, of which the matrix cores take 1.9.
+// two workgroups' 128, of which the matrix cores take 1.9.  Of the whole launch they are busy in a fifth.
 //
 // The kernel by itself; the files that include it say for which rows and sizes it is made.
 #pragma once
@@ -429,8 +429,10 @@ __global__ __launch_bounds__(NW * 64, 2) void k_attend_tile(AttendArgs a) {
       // Weights of 16 keys at a time, one block ahead of the products that take them, each rounded to one bf16 number; the sum is of the
       // unrounded ones.  The matrix cores bound this kernel, and they have no product of wider weights with bf16 values: as the sum of
       // two numbers (as in the kernel of few rows, which the cache's bytes bound) 2048 tokens over 34k rows take 1422 us and not 997, 2 x
-      // 1024 over 4096 rows 121 and not 93 at d = 64, 190 and not 147 at d = 256.  What one number costs in turn is 2^-8 of the weighted
-      // mean of |v| at most, and measured errors of 1.3 to 1.4 times those of results that are only rounded at the end.
+      // 1024 over 4096 rows 121 and not 93 at d = 64, 190 and not 147 at d = 256.  Trees too, whose products bound them while keys are walked:
+      // 16 tokens of 40 heads over 4112 rows 22.3 and not 21.3, 4 x 24 of 32 over 4096 28.3 and 27.3, 24 x 32 over 8192 of 8 bits 196 and 162,
+      // 2 x 127 over 16k 101 and 80, 200 over 32k 147 and 113, 48 x 61 of 28 over 2048 at d = 64 96 and 75.  What one number costs in turn is
+      // 2^-8 of the weighted mean of |v| at most, and measured errors of 1.3 to 1.4 times those of results that are only rounded at the end.
       uint32_t p[kKt * 2][4];
       auto weigh = [&](int kb) {
 #pragma unroll
