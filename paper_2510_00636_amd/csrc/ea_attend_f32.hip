@@ -80,7 +80,7 @@ __global__ __launch_bounds__((64 * f32_waves<D, KEYS>()), (D == 256 ? 1 : 2)) vo
     const bool more = key + stride < key_hi;
     // Either block of products begins at a line of 64 bytes of the code (the first one 4 bytes behind it): where they came to stand else, by
     // what the compiler made of the lines above, moved the time by up to 7 % (520 tokens of 32 heads over 2048 rows at d = 128 333 to 357 us,
-    // so 332).
+    // so 321).
     if constexpr (D < 256) {
       __builtin_amdgcn_sched_barrier(0);
       asm volatile(".p2align 6\n\ts_nop 0");

@@ -3,9 +3,9 @@
 
 namespace ea {
 
-// The pieces of every (token, head) row together.  What leads to a row (its sequence, how that was cut, its length) is asked for at once, a
-// lane for a sequence where there are no more than lanes; then pieces, ROUNDS of them at a time.  WIDE: a workgroup per row, whose 256
-// threads request all the pieces at once; else D / 4 threads have ROWS, one after the other, so that a workgroup's lookups serve them all.
+// The pieces of every (token, head) row together, ROUNDS of them at a time.  WIDE: a workgroup per row, whose 256 threads request all the
+// pieces at once; else D / 4 threads have ROWS, one after the other, so that a workgroup's lookups serve them all.  What leads to a row
+// (its sequence, how that was cut, its length) is asked for at once for one row, a lane for a sequence where there are no more than lanes.
 template <int D, bool F32, bool WIDE, int ROUNDS, int ROWS>
 __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   constexpr int kLanes = D / 4, kWays = WIDE ? 256 / kLanes : 1, kGroups = 256 / kLanes;
@@ -15,9 +15,15 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   const uint32_t at0 = WIDE ? blockIdx.x : blockIdx.x * (kGroups * ROWS) + threadIdx.x / kLanes, hq = a.Hq;
   const int all = first_token(a, a.B);
   const int4* cuts = (const int4*)(a.ws + a.plan.cuts);      // of a sequence: its first piece, cuts, keys of a stretch, tiles
-  const int mine = min(lane, a.B - 1), my_first = first_token(a, mine), my_end = first_token(a, mine + 1);
-  const int my_len = a.per_head ? 0 : rows_of(a, mine, 0);
-  const int4 my_cut = cuts[mine];
+  constexpr bool kAtOnce = ROWS == 1;
+  const int mine = min(lane, a.B - 1), my_end = first_token(a, mine + 1);
+  int my_first = 0, my_len = 0;
+  int4 my_cut = make_int4(0, 0, 0, 0);
+  if constexpr (kAtOnce) {
+    my_first = first_token(a, mine);
+    my_len = a.per_head ? 0 : rows_of(a, mine, 0);
+    my_cut = cuts[mine];
+  }
   // the sequence of the wavefront's first token: behind those that end in front of it
   const int token0 = __builtin_amdgcn_readfirstlane((int)(at0 / hq));
   int b = __popcll(__ballot(lane < a.B && my_end <= token0));
@@ -26,7 +32,7 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   int t0, m, len;
   int4 cut;
   auto sequence = [&]() {
-    if (a.B <= 64) {
+    if (kAtOnce && a.B <= 64) {
       t0 = __shfl(my_first, b);
       m = __shfl(my_end, b) - t0;
       len = __shfl(my_len, b);
@@ -43,9 +49,13 @@ __global__ __launch_bounds__(256) void k_attend_join(AttendArgs a) {
   for (int nth = 0; nth < ROWS; ++nth) {
     const uint32_t at = at0 + nth * kGroups;      // token, head
     const int token = (int)(at / hq), head = (int)(at - token * hq), h = head / a.G;
-    // (all lanes go on together: they look at each other's)
-    while (__any(token < all && token >= t0 + m && b + 1 < a.B)) {
-      if (token < all && token >= t0 + m && b + 1 < a.B) ++b;
+    if constexpr (kAtOnce) {      // (all lanes go on together: they look at each other's)
+      while (__any(token < all && token >= t0 + m && b + 1 < a.B)) {
+        if (token < all && token >= t0 + m && b + 1 < a.B) ++b;
+        sequence();
+      }
+    } else if (token < all && token >= t0 + m) {
+      while (b + 1 < a.B && first_token(a, b + 1) <= token) ++b;
       sequence();
     }
     if (token >= all || token < t0 || token >= t0 + m || (a.only_long && m * a.G <= a.short_rows)) continue;
@@ -112,7 +122,7 @@ static hipError_t join_of_type(const AttendArgs& a, hipStream_t st) {
   // up to 4096 rows: the order of their sums, and with it their last bits, stays what it was.
   // Eight pieces at a time up to 8192 rows, four behind that, when the chip is full (2048 rows over 16k keys 43.2 and 43.9 us, 4096 66.1 and
   // 67.2, 8128 61.0 and 60.7, 16k 87.4 and 85.9, 32k 93.7 and 89.3).
-  // Four rows to a group of threads from 32768 on, where workgroups come in many rounds: two pieces each of 160k rows 35 us, so 18 (whole
+  // Four rows to a group of threads from 32768 on, where workgroups come in many rounds: two pieces each of 160k rows 35 us, so 21 (whole
   // calls, one and four: 38k rows 65.5 and 65.2, 61k 71.9 and 71.3, 160k 187 and 181, at d = 256 263 and 252, 460k 181 and 182; 17k 48.2 and
   // 51.0, 32k 70.9 and 72.5).
   constexpr int kMany = 4;
